@@ -1,0 +1,462 @@
+"""Speed of the 8-bit activation store and of the gated norms: what a training
+program has the library do between a block's products, each case one pass
+through the public entry points.
+
+A case is a dict of plain sizes. `listed()` gives the named ones, `draw(rng)`
+more of the same ranges, `prepare` what a program holds before the call, `run`
+one pass (in plain torch, or through the library where `own` is true), `exact`
+the same outputs in float64.
+
+The 8-bit store of a matrix X[rows, n]: groups of 32 consecutive columns of a
+row (the last may be shorter) share a power of two. With a the largest |x| of a
+group, E = max(7, min(254, (bits(a) + 0x10000) >> 23)) (bits: the float32 bit
+pattern) and codes q = rne(x 2^(133 - E)) within +-127; a value reads back as
+q 2^(E - 133). E = 255 marks a group that holds an infinity or a NaN and reads
+back as NaN. In memory: rows * n code bytes, from the next multiple of 256 on
+rows * ceil(n / 32) bytes E, the whole a multiple of 256 bytes.
+
+The gated norm of a sub-layer's output f on the residual stream x:
+    p = LN(f; post) or f;  y = x + scale gate p;  h = LN(y; pre)
+with one gate row of n values for all rows or for each of `gates` equal runs of
+rows (a sample each).
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-5
+GROUP = 32
+
+
+# ---------------------------------------------------------------------------
+# the cases
+# ---------------------------------------------------------------------------
+def _store(name, dtype, rows, n, pad=0):
+    c = {"kind": "store", "dtype": dtype, "rows": rows, "n": n, "pad": pad}
+    return dict(c, name=name) if name else c
+
+
+def _restore(name, dtype, rows, n):
+    c = {"kind": "restore", "dtype": dtype, "rows": rows, "n": n}
+    return dict(c, name=name) if name else c
+
+
+def _wgrad(name, dtype, rows, K, N):
+    c = {"kind": "wgrad", "dtype": dtype, "rows": rows, "n": K, "N": N}
+    return dict(c, name=name) if name else c
+
+
+def _norm(name, kind, dtype, rows, n, gates, post, pre, f8):
+    c = {"kind": kind, "dtype": dtype, "rows": rows, "n": n, "gates": gates, "post": post, "pre": pre, "f8": f8}
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one token's activation into the store and back: what a call costs
+        _store("store-token", "bf16", 1, 1024),
+        # the feed-forward's pre-activation of a 115M-scale block (4 samples of
+        # 2048 tokens) kept in 8 bits between the passes
+        _store("store-mlp-115m", "bf16", 8192, 4096),
+        # float32 columns of a wider buffer, a regional crop's ragged token
+        # count, the last group of a row short
+        _store("store-ragged-f32", "f32", 1770, 1000, 24),
+        # what the backward of a 10B-scale shard's feed-forward reads: the
+        # pre-activation and its GELU from the store
+        _restore("restore-mlp-10b", "bf16", 4096, 4096),
+        # the same in float32 on a regional crop
+        _restore("restore-ragged-f32", "f32", 1770, 2056),
+        # the output projection's weight and bias gradient from its input's
+        # store: a 115M-scale block
+        _wgrad("wgrad-proj-115m", "bf16", 8192, 1024, 1024),
+        # and a 10B-scale shard: 1024 local columns of heads, width 8192
+        _wgrad("wgrad-proj-10b", "bf16", 4096, 1024, 8192),
+        # gated norms of one token at the 1B-scale model's width
+        _norm("norm-token", "norm", "bf16", 1, 2048, 1, 1, 1, 0),
+        # forward of a 10B-scale block in training: a gate for each of 2
+        # samples, the sub-layer's output also into the store
+        _norm("norm-10b-train", "norm", "bf16", 4096, 8192, 2, 1, 1, 1),
+        # float32 on a regional crop, no norm after the sub-layer, one gate
+        _norm("norm-ragged-f32", "norm", "f32", 1770, 1000, 1, 0, 1, 0),
+        # backward of a 115M-scale block, gates of 4 samples, the sub-layer's
+        # output from the store
+        _norm("norm-grad-115m", "norm_grad", "bf16", 8192, 1024, 4, 1, 1, 1),
+        # backward at the 113B-scale width
+        _norm("norm-grad-113b", "norm_grad", "bf16", 2048, 16384, 1, 1, 1, 0),
+    ]
+
+
+def _logint(rng, lo, hi, step=1):
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return max(lo, min(hi, int(round(v / step)) * step))
+
+
+def draw(rng):
+    """One more case of the listed ones' ranges."""
+    while True:
+        kind = rng.choice(["store", "restore", "wgrad", "norm", "norm", "norm_grad", "norm_grad"])
+        dtype = rng.choice(["bf16", "bf16", "f32"])
+        rows = _logint(rng, 1, 8192)
+        n = 8 * _logint(rng, 16, 2048)
+        if kind == "store":
+            c = _store(None, dtype, rows, n, 8 * rng.choice([0, 0, rng.randint(1, 64)]))
+        elif kind == "restore":
+            c = _restore(None, dtype, rows, n)
+        elif kind == "wgrad":
+            c = _wgrad(None, dtype, _logint(rng, 64, 8192), 8 * _logint(rng, 32, 256), 8 * _logint(rng, 32, 1024))
+        else:
+            gates = rng.choice([0, 1, 1, 2, 3, 4])
+            rows = max(1, rows // max(1, gates)) * max(1, gates)
+            post, pre, f8 = rng.choice([1, 1, 0]), rng.choice([1, 1, 1, 0]), rng.choice([0, 1])
+            c = _norm(None, kind, dtype, rows, n, gates, post, pre, f8)
+        w = work(c)
+        if w["bytes"] <= 4.0e8 and w["flops"] <= (5e9 if c["kind"] == "wgrad" and dtype == "f32" else 7e10):
+            return c
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+def _dt(c):
+    return torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+
+
+def _code(c):
+    return 1 if c["dtype"] == "bf16" else 0
+
+
+class _Rand:
+    """Normal tensors from one seeded generator on the GPU."""
+
+    def __init__(self, seed):
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(6967 * int(seed) + 29)
+
+    def __call__(self, shape, dtype, std=1.0, mean=0.0):
+        t = torch.randn(shape, generator=self.g, device="cuda", dtype=torch.float32)
+        return t.mul_(std).add_(mean).to(dtype)
+
+    def activation(self, rows, n, dtype):
+        """Unit normal, a few channels far larger, rows of different size."""
+        t = torch.randn((rows, n), generator=self.g, device="cuda", dtype=torch.float32)
+        ch = torch.rand(n, generator=self.g, device="cuda")
+        t.mul_(torch.where(ch < 0.01, 12.0, 1.0))
+        return t.mul_(torch.rand((rows, 1), generator=self.g, device="cuda").add_(0.5)).to(dtype)
+
+
+def _sizes(rows, n):
+    """Bytes of the codes (rounded up to where the exponents start) and of the whole store."""
+    groups = -(-n // GROUP)
+    at = -(-rows * n // 256) * 256
+    return at, -(-(at + rows * groups) // 256) * 256
+
+
+def _grouped(x):
+    """[rows, n] -> [rows, groups, 32], zeros behind a short last group."""
+    rows, n = x.shape
+    return torch.nn.functional.pad(x, (0, -n % GROUP)).reshape(rows, -1, GROUP)
+
+
+def _encode(x):
+    """Codes [rows, n] int8 and exponents [rows, groups] uint8 of a float32 matrix."""
+    rows, n = x.shape
+    t = _grouped(x)
+    top = t.abs().amax(-1)
+    E = ((top.view(torch.int32) + 0x10000) >> 23).clamp(7, 254)
+    E = torch.where(torch.isfinite(t).all(-1), E, 255)
+    up = ((260 - E.clamp(max=254)) << 23).to(torch.int32).view(torch.float32)
+    q = torch.round(torch.nan_to_num(t * up[..., None])).clamp(-127, 127)
+    return q.to(torch.int8).reshape(rows, -1)[:, :n], E.to(torch.uint8)
+
+
+def _decode(q, E):
+    """The float32 values that codes and exponents stand for."""
+    rows, n = q.shape
+    e = E.to(torch.int32)
+    down = torch.where(e == 255, torch.full_like(e, 0x7FC00000), (e - 6) << 23).view(torch.float32)
+    return (_grouped(q.float()) * down[..., None]).reshape(rows, -1)[:, :n]
+
+
+def _fill(store, q, E):
+    """Lays codes and exponents out in a store."""
+    rows, n = q.shape
+    at = _sizes(rows, n)[0]
+    store[:rows * n] = q.contiguous().view(torch.uint8).reshape(-1)
+    store[at:at + E.numel()] = E.reshape(-1)
+    return store
+
+
+def _parts(store, rows, n):
+    at, _ = _sizes(rows, n)
+    groups = -(-n // GROUP)
+    return store[:rows * n].view(torch.int8).reshape(rows, n), store[at:at + rows * groups].reshape(rows, groups)
+
+
+def _new_store(rows, n):
+    return torch.zeros(_sizes(rows, n)[1], dtype=torch.uint8, device="cuda")
+
+
+def prepare(case, seed):
+    c, r = case, _Rand(seed)
+    dt, rows, n, kind = _dt(c), c["rows"], c["n"], c["kind"]
+    E = lambda *shape: torch.empty(*shape, dtype=dt, device="cuda")
+    F = lambda *shape: torch.zeros(*shape, dtype=torch.float32, device="cuda")
+    s = {"c": c}
+    if kind == "store":
+        s["x"] = r.activation(rows, n + c["pad"], dt)[:, :n]
+        s.update(store=_new_store(rows, n), back=E(rows, n))
+    elif kind == "restore":
+        s["store"] = _fill(_new_store(rows, n), *_encode(r.activation(rows, n, dt).float()))
+        s.update(u=E(rows, n), g=E(rows, n))
+    elif kind == "wgrad":
+        s["store"] = _fill(_new_store(rows, n), *_encode(r.activation(rows, n, dt).float()))
+        s["dy"] = r((rows, c["N"]), dt)
+        s.update(dw=F(n, c["N"]), db=F(c["N"]))
+    else:
+        p = {}
+        if c["gates"]:
+            p["gate"] = r((c["gates"], n), dt, 0.1, 0.3)
+        if c["post"]:
+            p.update(post_g=r((n,), dt, 0.02, 1.0), post_b=r((n,), dt, 0.02))
+        if c["pre"]:
+            p.update(pre_g=r((n,), dt, 0.02, 1.0), pre_b=r((n,), dt, 0.02))
+        s["p"] = p
+        f = r.activation(rows, n, dt)
+        s["scale"] = 0.5
+        if kind == "norm":
+            s["x"], s["f"] = r.activation(rows, n, dt), f
+            s.update(y=E(rows, n), stats=F(rows, 4), h=E(rows, n) if c["pre"] else None)
+            if c["f8"]:
+                s.update(store=_new_store(rows, n), back=E(rows, n))
+        else:
+            # the forward's output and the rows' statistics, as a program has them
+            # (mean and 1 / sqrt(variance + eps) of f, then of y)
+            if c["f8"]:
+                s["store"] = _fill(_new_store(rows, n), *_encode(f.float()))
+                f = _decode(*_parts(s["store"], rows, n)).to(dt)
+            else:
+                s["f"] = f
+            s["y"] = r.activation(rows, n, dt)
+            st = [torch.zeros(rows, dtype=torch.float64, device="cuda")] * 4
+            for k, t, on in ((0, f, c["post"]), (2, s["y"], c["pre"])):
+                if on:
+                    t = t.double()
+                    st[k:k + 2] = [t.mean(-1), (t.var(-1, unbiased=False) + EPS).rsqrt()]
+            s["stats"] = torch.stack(st, -1).float()
+            s["dy"] = r((rows, n), dt)
+            s["dh"] = r((rows, n), dt) if c["pre"] else None
+            s.update(dx=E(rows, n), df=E(rows, n), grads={k: F(*v.shape) for k, v in p.items()})
+    return s
+
+
+# ---------------------------------------------------------------------------
+# one pass, in plain operations
+# ---------------------------------------------------------------------------
+def _gelu(u):
+    return 0.5 * u * (1.0 + torch.erf(u * math.sqrt(0.5)))
+
+
+def _moments(t):
+    mu = t.mean(-1, keepdim=True)
+    d = t - mu
+    return d, torch.rsqrt((d * d).mean(-1, keepdim=True) + EPS)
+
+
+def _runs(c, t):
+    """[rows, n] -> [gates or 1, rows of a gate, n]"""
+    return t.reshape(max(1, c["gates"]), -1, c["n"])
+
+
+def _plain(s):
+    c = s["c"]
+    dt, kind = _dt(c), c["kind"]
+    if kind == "store":
+        return {"x": _decode(*_encode(s["x"].float())).to(dt)}
+    if kind == "restore":
+        u = _decode(*_parts(s["store"], c["rows"], c["n"]))
+        return {"u": u.to(dt), "g": _gelu(u).to(dt)}
+    if kind == "wgrad":
+        dy = s["dy"].float()
+        return {"dw": _decode(*_parts(s["store"], c["rows"], c["n"])).t() @ dy, "db": dy.sum(0)}
+    p = {k: v.float() for k, v in s["p"].items()}
+    gate = s["scale"] * p["gate"][:, None] if c["gates"] else torch.tensor(s["scale"], device="cuda")
+    if kind == "norm":
+        f = s["f"].float()
+        t = f
+        if c["post"]:
+            d, r = _moments(f)
+            t = d * r * p["post_g"] + p["post_b"]
+        y = s["x"].float() + (gate * _runs(c, t)).reshape(f.shape)
+        out = {"y": y.to(dt)}
+        if c["pre"]:
+            d, r = _moments(y)
+            out["h"] = (d * r * p["pre_g"] + p["pre_b"]).to(dt)
+        if c["f8"]:
+            out["f"] = _decode(*_encode(f)).to(dt)
+        return out
+    f = _decode(*_parts(s["store"], c["rows"], c["n"])) if c["f8"] else s["f"].float()
+    t, grads = s["dy"].float(), {}
+    if c["pre"]:
+        d, r = _moments(s["y"].float())
+        yh, dh = d * r, s["dh"].float()
+        grads["pre_g"], grads["pre_b"] = (dh * yh).sum(0), dh.sum(0)
+        w = dh * p["pre_g"]
+        t = t + r * (w - w.mean(-1, keepdim=True) - yh * (w * yh).mean(-1, keepdim=True))
+    w = (gate * _runs(c, t)).reshape(f.shape)
+    if c["post"]:
+        d, r = _moments(f)
+        fh = d * r
+        grads["post_g"], grads["post_b"] = (w * fh).sum(0), w.sum(0)
+        if c["gates"]:
+            grads["gate"] = s["scale"] * _runs(c, t * (fh * p["post_g"] + p["post_b"])).sum(1)
+        w = w * p["post_g"]
+        w = r * (w - w.mean(-1, keepdim=True) - fh * (w * fh).mean(-1, keepdim=True))
+    elif c["gates"]:
+        grads["gate"] = s["scale"] * _runs(c, t * f).sum(1)
+    return {"dx": t.to(dt), "df": w.to(dt), "grads": grads}
+
+
+# ---------------------------------------------------------------------------
+# one pass through the library
+# ---------------------------------------------------------------------------
+def _own(s):
+    from paper_2404_14712_amd import load
+    from paper_2404_14712_amd._lib import GatedNormDesc
+
+    lib, c = load(), s["c"]
+    code, kind, rows, n = _code(c), c["kind"], c["rows"], c["n"]
+    if kind == "store":
+        lib.orbit_act8_pack(code, rows, n, s["x"], n + c["pad"], s["store"])
+        lib.orbit_act8_unpack(code, rows, n, s["store"], s["back"], n)
+        return {"x": s["back"]}
+    if kind == "restore":
+        lib.orbit_act8_unpack(code, rows, n, s["store"], s["u"], n, s["g"], n)
+        return {"u": s["u"], "g": s["g"]}
+    if kind == "wgrad":
+        ws = torch.empty(lib.orbit_act8_weight_grad_workspace_bytes(code, rows, n, c["N"]), dtype=torch.uint8,
+                         device="cuda")
+        lib.orbit_act8_weight_grad(code, rows, n, c["N"], s["store"], s["dy"], c["N"], s["dw"], s["db"], 0, ws)
+        return {"dw": s["dw"], "db": s["db"]}
+    desc = GatedNormDesc(rows, n, c["gates"], c["post"], c["pre"], s["scale"], EPS, code)
+    if kind == "norm":
+        lib.orbit_gated_norm_fwd(desc, s["p"], s["x"], s["f"], s.get("store"), s["y"], s["h"], s["stats"])
+        out = {"y": s["y"]}
+        if c["pre"]:
+            out["h"] = s["h"]
+        if c["f8"]:
+            lib.orbit_act8_unpack(code, rows, n, s["store"], s["back"], n)
+            out["f"] = s["back"]
+        return out
+    ws = torch.empty(lib.orbit_gated_norm_bwd_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    lib.orbit_gated_norm_bwd(desc, s["p"], s.get("f"), s.get("store"), s["y"], s["stats"], s["dh"], s["dy"], s["dx"],
+                             s["df"], s["grads"], 0, ws)
+    return {"dx": s["dx"], "df": s["df"], "grads": s["grads"]}
+
+
+def run(state):
+    if own:
+        return _own(state)
+    return _plain(state)
+
+
+# ---------------------------------------------------------------------------
+# the work of one pass
+# ---------------------------------------------------------------------------
+def work(case):
+    c = case
+    e = 2.0 if c["dtype"] == "bf16" else 4.0
+    rows, n, kind = float(c["rows"]), float(c["n"]), c["kind"]
+    q = rows * (n + -(-c["n"] // GROUP))  # bytes of a store
+    if kind == "store":
+        # x read and the store written, the store read and x written
+        return {"bytes": 2.0 * (rows * n * e + q), "flops": 4.0 * rows * n}
+    if kind == "restore":
+        return {"bytes": q + 2.0 * rows * n * e, "flops": 20.0 * rows * n}
+    if kind == "wgrad":
+        return {"bytes": q + rows * c["N"] * e + 4.0 * (n + 1) * c["N"], "flops": 2.0 * rows * n * c["N"]}
+    par = n * (c["gates"] + 2 * c["post"] + 2 * c["pre"])
+    if kind == "norm":
+        # x and f read, y and h written; the store written and read back
+        by = rows * n * e * (3 + c["pre"]) + e * par + 16.0 * rows + (2 * q + rows * n * e if c["f8"] else 0)
+        return {"bytes": by, "flops": 16.0 * rows * n}
+    # f is read where its norm or a gate needs it, y and dh where there is a pre-norm
+    f = (q if c["f8"] else rows * n * e) if c["post"] or c["gates"] else 0.0
+    return {"bytes": f + rows * n * e * (3 + 2 * c["pre"]) + 16.0 * rows + (e + 4.0) * par, "flops": 30.0 * rows * n}
+
+
+# ---------------------------------------------------------------------------
+# float64 reference
+# ---------------------------------------------------------------------------
+def _power64(k):
+    """2^k in float64, exactly (a power function may be off by a rounding, which decides ties)."""
+    return ((k.to(torch.int64) + 1023) << 52).view(torch.float64)
+
+
+def _nearest64(x):
+    """The values that the store of a finite float64 matrix stands for: the
+    smallest step 2^k that keeps the rounded codes within 127 (k >= -126)."""
+    rows, n = x.shape
+    out = torch.empty_like(x)
+    for a in range(0, n, GROUP):
+        t = x[:, a:a + GROUP]
+        top = t.abs().amax(1, keepdim=True)
+        m, e = torch.frexp(top)  # top = m 2^e, m in [1/2, 1)
+        k = (e - 7 + (m * 128.0 >= 127.5)).clamp(-126, 121)
+        step = _power64(k)
+        out[:, a:a + GROUP] = torch.round(t / step).clamp(-127, 127) * step
+    return out
+
+
+def _values64(s):
+    """The values of a store, from its bytes."""
+    c = s["c"]
+    q, E = _parts(s["store"], c["rows"], c["n"])
+    step = _power64(E.to(torch.int64) - 133).repeat_interleave(GROUP, 1)[:, :c["n"]]
+    return q.double() * step
+
+
+def _ln64(t, g, b):
+    return torch.nn.functional.layer_norm(t, (t.shape[-1],), g, b, EPS)
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(c, seed)
+    kind = c["kind"]
+    if kind == "store":
+        return {"x": _nearest64(s["x"].double())}
+    if kind == "restore":
+        u = _values64(s)
+        return {"u": u, "g": u * torch.special.ndtr(u)}
+    if kind == "wgrad":
+        dy = s["dy"].double()
+        return {"dw": _values64(s).t().contiguous() @ dy, "db": dy.sum(0)}
+    p = {k: v.double().requires_grad_(True) for k, v in s["p"].items()}
+
+    def branch(f):
+        t = _ln64(f, p["post_g"], p["post_b"]) if c["post"] else f
+        if c["gates"]:
+            t = t * p["gate"].repeat_interleave(c["rows"] // c["gates"], 0)
+        return s["scale"] * t
+
+    if kind == "norm":
+        with torch.no_grad():
+            y = s["x"].double() + branch(s["f"].double())
+            out = {"y": y}
+            if c["pre"]:
+                out["h"] = _ln64(y, p["pre_g"], p["pre_b"])
+            if c["f8"]:
+                out["f"] = _nearest64(s["f"].double())
+        return out
+    f = (_values64(s) if c["f8"] else s["f"].double()).requires_grad_(True)
+    y = s["y"].double().requires_grad_(True)
+    value = (s["dy"].double() * y).sum()
+    if c["pre"]:
+        value = value + (s["dh"].double() * _ln64(y, p["pre_g"], p["pre_b"])).sum()
+    value.backward()
+    (branch(f) * y.grad).sum().backward()
+    return {"dx": y.grad, "df": f.grad, "grads": {k: v.grad for k, v in p.items()}}
