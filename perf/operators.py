@@ -9,9 +9,9 @@ the same outputs in float64.
 
 The 8-bit store of a matrix X[rows, n]: groups of 32 consecutive columns of a
 row (the last may be shorter) share a power of two. With a the largest |x| of a
-group, E = max(7, min(254, (bits(a) + 0x10000) >> 23)) (bits: the float32 bit
-pattern) and codes q = rne(x 2^(133 - E)) within +-127; a value reads back as
-q 2^(E - 133). E = 255 marks a group that holds an infinity or a NaN and reads
+group, E = max(7, (bits(a) + 0x10000) >> 23) (bits: the float32 bit pattern) and
+codes q = rne(x 2^(133 - E)), which lie within +-127; a value reads back as
+q 2^(E - 133). E = 0 marks a group that holds an infinity or a NaN and reads
 back as NaN. In memory: rows * n code bytes, from the next multiple of 256 on
 rows * ceil(n / 32) bytes E, the whole a multiple of 256 bytes.
 
@@ -166,10 +166,10 @@ def _encode(x):
     rows, n = x.shape
     t = _grouped(x)
     top = t.abs().amax(-1)
-    E = ((top.view(torch.int32) + 0x10000) >> 23).clamp(7, 254)
-    E = torch.where(torch.isfinite(t).all(-1), E, 255)
-    up = ((260 - E.clamp(max=254)) << 23).to(torch.int32).view(torch.float32)
-    q = torch.round(torch.nan_to_num(t * up[..., None])).clamp(-127, 127)
+    fine = torch.isfinite(top)
+    E = torch.where(fine, ((top.view(torch.int32) + 0x10000) >> 23).clamp(min=7), 0)
+    up = ((260 - E.clamp(min=7)) << 23).to(torch.int32).view(torch.float32)
+    q = torch.round(torch.where(fine[..., None], t * up[..., None], 0.0))
     return q.to(torch.int8).reshape(rows, -1)[:, :n], E.to(torch.uint8)
 
 
@@ -177,7 +177,7 @@ def _decode(q, E):
     """The float32 values that codes and exponents stand for."""
     rows, n = q.shape
     e = E.to(torch.int32)
-    down = torch.where(e == 255, torch.full_like(e, 0x7FC00000), (e - 6) << 23).view(torch.float32)
+    down = torch.where(e == 0, torch.full_like(e, 0x7FC00000), (e - 6) << 23).view(torch.float32)
     return (_grouped(q.float()) * down[..., None]).reshape(rows, -1)[:, :n]
 
 
@@ -405,9 +405,8 @@ def _nearest64(x):
         t = x[:, a:a + GROUP]
         top = t.abs().amax(1, keepdim=True)
         m, e = torch.frexp(top)  # top = m 2^e, m in [1/2, 1)
-        k = (e - 7 + (m * 128.0 >= 127.5)).clamp(-126, 121)
-        step = _power64(k)
-        out[:, a:a + GROUP] = torch.round(t / step).clamp(-127, 127) * step
+        step = _power64((e - 7 + (m * 128.0 >= 127.5)).clamp(min=-126))
+        out[:, a:a + GROUP] = torch.round(t / step) * step
     return out
 
 
