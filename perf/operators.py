@@ -9,10 +9,10 @@ the same outputs in float64.
 
 The 8-bit store of a matrix X[rows, n]: groups of 32 consecutive columns of a
 row (the last may be shorter) share a power of two. With a the largest |x| of a
-group, E = max(7, (bits(a) + 0x10000) >> 23) (bits: the float32 bit pattern) and
-codes q = rne(x 2^(133 - E)), which lie within +-127; a value reads back as
-q 2^(E - 133). E = 0 marks a group that holds an infinity or a NaN and reads
-back as NaN. In memory: rows * n code bytes, from the next multiple of 256 on
+group, E = max(7, min(254, (bits(a) + 0x10000) >> 23)) (bits: the float32 bit
+pattern) and codes q = rne(x 2^(133 - E)), which only the largest finite values
+take past +-127, where they end; a value reads back as q 2^(E - 133). E = 0
+marks a group that holds an infinity or a NaN and reads back as NaN. In memory: rows * n code bytes, from the next multiple of 256 on
 rows * ceil(n / 32) bytes E, the whole a multiple of 256 bytes.
 
 The gated norm of a sub-layer's output f on the residual stream x:
@@ -167,9 +167,9 @@ def _encode(x):
     t = _grouped(x)
     top = t.abs().amax(-1)
     fine = torch.isfinite(top)
-    E = torch.where(fine, ((top.view(torch.int32) + 0x10000) >> 23).clamp(min=7), 0)
+    E = torch.where(fine, ((top.view(torch.int32) + 0x10000) >> 23).clamp(7, 254), 0)
     up = ((260 - E.clamp(min=7)) << 23).to(torch.int32).view(torch.float32)
-    q = torch.round(torch.where(fine[..., None], t * up[..., None], 0.0))
+    q = torch.round(torch.where(fine[..., None], t * up[..., None], 0.0)).clamp(-127, 127)
     return q.to(torch.int8).reshape(rows, -1)[:, :n], E.to(torch.uint8)
 
 
@@ -405,8 +405,8 @@ def _nearest64(x):
         t = x[:, a:a + GROUP]
         top = t.abs().amax(1, keepdim=True)
         m, e = torch.frexp(top)  # top = m 2^e, m in [1/2, 1)
-        step = _power64((e - 7 + (m * 128.0 >= 127.5)).clamp(min=-126))
-        out[:, a:a + GROUP] = torch.round(t / step) * step
+        step = _power64((e - 7 + (m * 128.0 >= 127.5)).clamp(-126, 121))
+        out[:, a:a + GROUP] = torch.round(t / step).clamp(-127, 127) * step
     return out
 
 
