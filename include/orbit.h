@@ -319,6 +319,84 @@ orbit_status orbit_layernorm_fwd(int32_t dtype, int32_t rows, int32_t n, const v
                                  void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Activations stored in 8 bits                                              */
+/* ------------------------------------------------------------------------ */
+
+/* The store of a matrix X[rows, n] (n a multiple of 8) keeps one signed byte
+ * per value and one byte E per group of 32 consecutive columns of a row (the
+ * last group of a row may be shorter). With a the float32 bits of a group's
+ * largest |x|,
+ *   E = max(7, min(254, (a + 0x10000) >> 23)),  code = round(x 2^(133 - E))
+ * (nearest, ties to even, within +-127), and a value reads back as
+ * code 2^(E - 133): off by at most half a step 2^(E - 133), that is by less
+ * than 2^-7 of the group's largest |x| (float32 values above 127.5 2^121 end
+ * at 127 2^121, those below 2^-127 at 0), and exact in both dtypes. A group that
+ * holds an infinity or a NaN has E = 0 and reads back as NaN.
+ * In memory: the codes [rows, n], from the next multiple of 256 bytes on the
+ * E [rows, (n + 31) / 32], the whole a multiple of 256 bytes. */
+size_t orbit_act8_bytes(int64_t rows, int32_t n); /* 0 on bad sizes */
+/* x[rows, n] (dtype, leading dimension ldx >= n, a multiple of 8) -> store */
+orbit_status orbit_act8_pack(int32_t dtype, int64_t rows, int32_t n, const void* x, int64_t ldx, void* store,
+                             size_t store_bytes, void* stream);
+/* store -> x[rows, n] and / or GELU(x) (dtype; leading dimensions >= n,
+ * multiples of 8; either pointer may be NULL, not both) */
+orbit_status orbit_act8_unpack(int32_t dtype, int64_t rows, int32_t n, const void* store, size_t store_bytes, void* x,
+                               int64_t ldx, void* gelu, int64_t ldgelu, void* stream);
+/* Weight and bias gradient of a linear layer whose input x[rows, K] is in a
+ * store: dw[K, N] = X^T dy, db[N] = column sums of dy (db may be NULL), with
+ * dy[rows, N] of dtype, leading dimension lddy. K and N are multiples of 8. */
+size_t orbit_act8_weight_grad_workspace_bytes(int32_t dtype, int32_t rows, int32_t K, int32_t N);
+orbit_status orbit_act8_weight_grad(int32_t dtype, int32_t rows, int32_t K, int32_t N, const void* store,
+                                    size_t store_bytes, const void* dy, int64_t lddy, float* dw, float* db,
+                                    int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Norms around a sub-layer with its gate and residual scale                 */
+/* ------------------------------------------------------------------------ */
+
+/* With x the residual stream and f a sub-layer's output, [rows, n] each:
+ *   p = post_norm ? LN(f) post_g + post_b : f
+ *   y = x + scale gate p          (gate: ones when gate_rows == 0)
+ *   h = LN(y) pre_g + pre_b       (only with pre_norm: the next product's input)
+ * gate [gate_rows, n]: row t uses gate row t / (rows / gate_rows), so that 1 is
+ * a learned gate per channel and B one per sample of [B, L, n]; gate_rows
+ * divides rows. n is a multiple of 8 up to 16384. LayerNorms use the biased
+ * variance and eps. Each LayerNorm normalises the float32 value. */
+typedef struct {
+  int32_t rows, n, gate_rows, post_norm, pre_norm;
+  float scale, eps;
+  int32_t dtype;
+} orbit_gated_norm_desc;
+
+typedef struct {
+  const void *gate;             /* [gate_rows, n] (ignored if gate_rows == 0) */
+  const void *post_g, *post_b;  /* [n] (ignored if !post_norm)                */
+  const void *pre_g, *pre_b;    /* [n] (ignored if !pre_norm)                 */
+} orbit_gated_norm_params;
+typedef struct { float *gate, *post_g, *post_b, *pre_g, *pre_b; } orbit_gated_norm_grads;
+
+/* f given: read from f; store (may be NULL) receives f in 8 bits. f NULL: f is
+ * read from the store. x may not alias y or h. h: NULL without pre_norm.
+ * stats [rows, 4] float32 receives mean and 1 / sqrt(variance + eps) of f
+ * (zeros without post_norm) and of y (zeros without pre_norm). */
+orbit_status orbit_gated_norm_fwd(const orbit_gated_norm_desc* desc, const orbit_gated_norm_params* p, const void* x,
+                                  const void* f, void* store, size_t store_bytes, void* y, void* h, float* stats,
+                                  void* stream);
+
+size_t orbit_gated_norm_bwd_workspace_bytes(const orbit_gated_norm_desc* desc);
+/* Gradients dx, df [rows, n] (dtype) and of the parameters from dh (gradient
+ * of h; NULL without pre_norm) and dy (gradient of y from its other readers;
+ * NULL: none, with pre_norm only), given f or its store (as in the forward;
+ * both may be NULL without post_norm and gate), the forward's y (may be NULL
+ * without pre_norm) and stats. dx is the whole gradient of y and may be NULL.
+ * dx may alias dy, df may alias dh or f. Gradients of absent parameters are not
+ * touched. Sums are formed in a fixed order (bitwise reproducible). */
+orbit_status orbit_gated_norm_bwd(const orbit_gated_norm_desc* desc, const orbit_gated_norm_params* p, const void* f,
+                                  const void* store, size_t store_bytes, const void* y, const float* stats,
+                                  const void* dh, const void* dy, void* dx, void* df, const orbit_gated_norm_grads* g,
+                                  int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Diagnostics and measurement support                                       */
 /* ------------------------------------------------------------------------ */
 

@@ -22,6 +22,7 @@ ABI_VERSION = 2
 BLOCK_PARAMS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "qn_g", "qn_b", "kn_g", "kn_b",
                 "w_proj", "b_proj", "ln2_g", "ln2_b", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
 AGG_PARAMS = ("q0", "w_q", "b_q", "w_k", "b_k", "w_v", "b_v", "w_o", "b_o", "pos")
+GATED_NORM_PARAMS = ("gate", "post_g", "post_b", "pre_g", "pre_b")
 HEAD_PARAMS = ("lnf_g", "lnf_b", "w_h", "b_h", "w_hid", "b_hid")
 
 
@@ -74,6 +75,19 @@ class HeadGrads(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in HEAD_PARAMS]
 
 
+class GatedNormDesc(ctypes.Structure):
+    _fields_ = [("rows", c_int32), ("n", c_int32), ("gate_rows", c_int32), ("post_norm", c_int32),
+                ("pre_norm", c_int32), ("scale", c_float), ("eps", c_float), ("dtype", c_int32)]
+
+
+class GatedNormParams(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in GATED_NORM_PARAMS]
+
+
+class GatedNormGrads(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in GATED_NORM_PARAMS]
+
+
 class OrbitError(RuntimeError):
     def __init__(self, fn: str, status: int, detail: str):
         super().__init__(f"{fn} failed with status {status}: {detail}")
@@ -117,6 +131,15 @@ _PROTOS = {
     "orbit_attention_bwd_noalloc": (c_int, [c_int32] * 5 + [P, c_int64, P, c_int64, P, c_int64, P, c_int64, c_int32,
                                                             P, P, c_int64, P, P, P, c_int64, P]),
     "orbit_layernorm_fwd": (c_int, [c_int32, c_int32, c_int32, P, P, P, c_float, P, P, P, P]),
+    "orbit_act8_bytes": (c_size_t, [c_int64, c_int32]),
+    "orbit_act8_pack": (c_int, [c_int32, c_int64, c_int32, P, c_int64, P, c_size_t, P]),
+    "orbit_act8_unpack": (c_int, [c_int32, c_int64, c_int32, P, c_size_t, P, c_int64, P, c_int64, P]),
+    "orbit_act8_weight_grad_workspace_bytes": (c_size_t, [c_int32] * 4),
+    "orbit_act8_weight_grad": (c_int, [c_int32] * 4 + [P, c_size_t, P, c_int64, P, P, c_int32, P, c_size_t, P]),
+    "orbit_gated_norm_fwd": (c_int, [POINTER(GatedNormDesc), POINTER(GatedNormParams), P, P, P, c_size_t, P, P, P, P]),
+    "orbit_gated_norm_bwd_workspace_bytes": (c_size_t, [POINTER(GatedNormDesc)]),
+    "orbit_gated_norm_bwd": (c_int, [POINTER(GatedNormDesc), POINTER(GatedNormParams), P, P, c_size_t, P, P, P, P, P,
+                                     P, POINTER(GatedNormGrads), c_int, P, c_size_t, P]),
     "orbit_status_string": (c_char_p, [c_int]),
     "orbit_last_error": (c_char_p, []),
     "orbit_abi_version": (c_int, []),
@@ -137,6 +160,10 @@ def _ptr(t) -> Optional[int]:
     if isinstance(t, int):
         return t
     return t.data_ptr()
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _stream(stream) -> Optional[int]:
@@ -307,6 +334,44 @@ class OrbitLib:
         self._check("orbit_layernorm_fwd", self.lib.orbit_layernorm_fwd(
             dtype, rows, n, _ptr(x), _ptr(g), _ptr(b), float(eps), _ptr(y), _ptr(mean), _ptr(rstd),
             _stream(stream)))
+
+    # -- 8-bit activation store ------------------------------------------------
+    def orbit_act8_bytes(self, rows, n) -> int:
+        return self.lib.orbit_act8_bytes(int(rows), int(n))
+
+    def orbit_act8_pack(self, dtype, rows, n, x, ldx, store, stream=None):
+        self._check("orbit_act8_pack", self.lib.orbit_act8_pack(
+            dtype, rows, n, _ptr(x), ldx, _ptr(store), _nbytes(store), _stream(stream)))
+
+    def orbit_act8_unpack(self, dtype, rows, n, store, x, ldx, gelu=None, ldgelu=0, stream=None):
+        self._check("orbit_act8_unpack", self.lib.orbit_act8_unpack(
+            dtype, rows, n, _ptr(store), _nbytes(store), _ptr(x), ldx, _ptr(gelu), ldgelu, _stream(stream)))
+
+    def orbit_act8_weight_grad_workspace_bytes(self, dtype, rows, K, N) -> int:
+        return self.lib.orbit_act8_weight_grad_workspace_bytes(dtype, rows, K, N)
+
+    def orbit_act8_weight_grad(self, dtype, rows, K, N, store, dy, lddy, dw, db, accumulate, ws, stream=None):
+        self._check("orbit_act8_weight_grad", self.lib.orbit_act8_weight_grad(
+            dtype, rows, K, N, _ptr(store), _nbytes(store), _ptr(dy), lddy, _ptr(dw), _ptr(db), int(accumulate),
+            _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    # -- gated norms -----------------------------------------------------------
+    def orbit_gated_norm_fwd(self, desc, params, x, f, store, y, h, stats, stream=None):
+        p = self._struct(GatedNormParams, params)
+        self._check("orbit_gated_norm_fwd", self.lib.orbit_gated_norm_fwd(
+            ctypes.byref(desc), ctypes.byref(p), _ptr(x), _ptr(f), _ptr(store), _nbytes(store), _ptr(y), _ptr(h),
+            _ptr(stats), _stream(stream)))
+
+    def orbit_gated_norm_bwd_workspace_bytes(self, desc) -> int:
+        return self.lib.orbit_gated_norm_bwd_workspace_bytes(ctypes.byref(desc))
+
+    def orbit_gated_norm_bwd(self, desc, params, f, store, y, stats, dh, dy, dx, df, grads, accumulate, ws,
+                             stream=None):
+        p = self._struct(GatedNormParams, params)
+        g = self._struct(GatedNormGrads, grads)
+        self._check("orbit_gated_norm_bwd", self.lib.orbit_gated_norm_bwd(
+            ctypes.byref(desc), ctypes.byref(p), _ptr(f), _ptr(store), _nbytes(store), _ptr(y), _ptr(stats), _ptr(dh),
+            _ptr(dy), _ptr(dx), _ptr(df), ctypes.byref(g), int(accumulate), _ptr(ws), _nbytes(ws), _stream(stream)))
 
     # -- measurement aid -------------------------------------------------------
     def orbit_mfma_probe(self, blocks, iters, seed, x, out, stream=None):

@@ -4,8 +4,10 @@
 
 #include <algorithm>
 
+#include "act8.h"
 #include "agg.h"
 #include "gemm.h"
+#include "gnorm.h"
 #include "kernels.h"
 
 using namespace orbit;
@@ -938,6 +940,215 @@ orbit_status orbit_layernorm_fwd(int32_t dtype, int32_t rows, int32_t n, const v
   REQ(eps > 0.f, ORBIT_E_ARG, "%s: eps must be positive", fn);
   PTR(x, "x"); PTR(g, "g"); PTR(b, "b"); PTR(y, "y"); OPT_PTR(mean, "mean"); OPT_PTR(rstd, "rstd");
   return layernorm_fwd((orbit_dtype)dtype, x, n, g, b, y, n, mean, rstd, rows, n, eps, S(stream));
+}
+
+// ---------------------------------------------------------------------------
+// activations stored in 8 bits
+// ---------------------------------------------------------------------------
+static orbit_status act8_check(const char* fn, int64_t rows, int32_t n, const void* store, size_t bytes) {
+  REQ(rows > 0 && n > 0 && n % 8 == 0, ORBIT_E_ARG, "%s: bad sizes rows=%lld n=%d (n must be a multiple of 8)", fn,
+      (long long)rows, n);
+  REQ(rows < (1ll << 40) / n, ORBIT_E_UNSUPPORTED, "%s: rows=%lld x n=%d exceeds 2^40 values", fn, (long long)rows, n);
+  PTR(store, "store");
+  REQ(bytes >= act8_store_bytes(rows, n), ORBIT_E_ARG, "%s: store of %zu bytes is smaller than the %zu required", fn,
+      bytes, act8_store_bytes(rows, n));
+  return ORBIT_OK;
+}
+
+size_t orbit_act8_bytes(int64_t rows, int32_t n) {
+  if (rows <= 0 || n <= 0 || n % 8 != 0 || rows >= (1ll << 40) / n) {
+    set_error("orbit_act8_bytes: bad sizes rows=%lld n=%d", (long long)rows, n);
+    return 0;
+  }
+  return act8_store_bytes(rows, n);
+}
+
+orbit_status orbit_act8_pack(int32_t dtype, int64_t rows, int32_t n, const void* x, int64_t ldx, void* store,
+                             size_t store_bytes, void* stream) {
+  const char* fn = "orbit_act8_pack";
+  clear_error();
+  ORBIT_TRY(check_dtype(fn, dtype));
+  ORBIT_TRY(act8_check(fn, rows, n, store, store_bytes));
+  PTR(x, "x");
+  REQ(ldx >= n && ldx % 8 == 0, ORBIT_E_ARG, "%s: ldx must be >= n and a multiple of 8", fn);
+  return act8_pack((orbit_dtype)dtype, x, ldx, rows, n, store, S(stream));
+}
+
+orbit_status orbit_act8_unpack(int32_t dtype, int64_t rows, int32_t n, const void* store, size_t store_bytes, void* x,
+                               int64_t ldx, void* gelu, int64_t ldgelu, void* stream) {
+  const char* fn = "orbit_act8_unpack";
+  clear_error();
+  ORBIT_TRY(check_dtype(fn, dtype));
+  ORBIT_TRY(act8_check(fn, rows, n, store, store_bytes));
+  REQ(x || gelu, ORBIT_E_ARG, "%s: x and gelu are both NULL", fn);
+  OPT_PTR(x, "x");
+  OPT_PTR(gelu, "gelu");
+  REQ(x != gelu, ORBIT_E_ARG, "%s: gelu must not alias x", fn);
+  REQ(!x || (ldx >= n && ldx % 8 == 0), ORBIT_E_ARG, "%s: ldx must be >= n and a multiple of 8", fn);
+  REQ(!gelu || (ldgelu >= n && ldgelu % 8 == 0), ORBIT_E_ARG, "%s: ldgelu must be >= n and a multiple of 8", fn);
+  return act8_unpack((orbit_dtype)dtype, store, rows, n, x, ldx, gelu, ldgelu, S(stream));
+}
+
+namespace {
+
+struct Act8GradWs {
+  void* x;      // [rows, K] read back from the store
+  float* bias;  // partials of the column sums of dy
+  void* gws;
+  size_t gws_bytes;
+};
+
+Gemm act8_grad_gemm(int32_t dtype, int32_t rows, int32_t K, int32_t N) {
+  Gemm g;
+  g.dtype = (orbit_dtype)dtype; g.tag = "act8_dw";
+  g.lda = K; g.a_kmajor = false; g.b_kmajor = false;
+  g.ldb = N; g.ldc = N; g.out_f32 = true;
+  g.M = K; g.N = N; g.K = rows;
+  return g;
+}
+
+size_t act8_grad_ws(int32_t dtype, int32_t rows, int32_t K, int32_t N, void* base, Act8GradWs* w) {
+  Carver c(base);
+  Act8GradWs t{};
+  t.x = c.take<char>((size_t)rows * K * esz(dtype));
+  t.bias = c.take<float>(colsum_part_bytes(rows, N, false) / sizeof(float));
+  t.gws_bytes = gemm_workspace_bytes(act8_grad_gemm(dtype, rows, K, N));
+  t.gws = c.take<char>(t.gws_bytes);
+  if (w) *w = t;
+  return c.used();
+}
+
+orbit_status act8_grad_check(const char* fn, int32_t dtype, int32_t rows, int32_t K, int32_t N) {
+  ORBIT_TRY(check_dtype(fn, dtype));
+  REQ(rows > 0 && K > 0 && N > 0 && K % 8 == 0 && N % 8 == 0, ORBIT_E_ARG,
+      "%s: bad sizes rows=%d K=%d N=%d (K and N must be multiples of 8)", fn, rows, K, N);
+  return ORBIT_OK;
+}
+
+}  // namespace
+
+size_t orbit_act8_weight_grad_workspace_bytes(int32_t dtype, int32_t rows, int32_t K, int32_t N) {
+  if (act8_grad_check("orbit_act8_weight_grad_workspace_bytes", dtype, rows, K, N) != ORBIT_OK) return 0;
+  return act8_grad_ws(dtype, rows, K, N, nullptr, nullptr);
+}
+
+orbit_status orbit_act8_weight_grad(int32_t dtype, int32_t rows, int32_t K, int32_t N, const void* store,
+                                    size_t store_bytes, const void* dy, int64_t lddy, float* dw, float* db,
+                                    int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "orbit_act8_weight_grad";
+  clear_error();
+  ORBIT_TRY(act8_grad_check(fn, dtype, rows, K, N));
+  ORBIT_TRY(act8_check(fn, rows, K, store, store_bytes));
+  PTR(dy, "dy"); PTR(dw, "dw"); OPT_PTR(db, "db"); PTR(ws, "ws");
+  REQ(lddy >= N && lddy % 8 == 0, ORBIT_E_ARG, "%s: lddy must be >= N and a multiple of 8", fn);
+  REQ(accumulate == 0 || accumulate == 1, ORBIT_E_ARG, "%s: accumulate must be 0 or 1", fn);
+  Act8GradWs w;
+  const size_t need = act8_grad_ws(dtype, rows, K, N, ws, &w);
+  REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes,
+      need);
+  hipStream_t s = S(stream);
+  const orbit_dtype dt = (orbit_dtype)dtype;
+  ORBIT_TRY(act8_unpack(dt, store, rows, K, w.x, K, nullptr, 0, s));
+  Gemm g = act8_grad_gemm(dtype, rows, K, N);
+  g.A = w.x; g.B = dy; g.ldb = lddy; g.C = dw; g.accumulate = accumulate != 0;
+  // the bias gradient comes out of the product where its kernel forms it
+  g.bsum_max_parts = colsum_chunks(rows);
+  const int parts = db ? gemm_bsum_parts(g) : 0;
+  const bool fused = parts > 0 && parts <= colsum_chunks(rows);
+  if (fused) g.bsum = w.bias;
+  ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+  if (!db) return ORBIT_OK;
+  if (!fused) return colsum(dt, dy, lddy, rows, N, nullptr, 0, nullptr, nullptr, db, nullptr, accumulate, w.bias, s);
+  ColFinal fin;
+  fin.add(w.bias, N, parts, N, db);
+  return fin.run(accumulate, s);
+}
+
+// ---------------------------------------------------------------------------
+// gated norms
+// ---------------------------------------------------------------------------
+static orbit_status gnorm_check(const char* fn, const orbit_gated_norm_desc* desc, GnormDims* o) {
+  REQ(desc != nullptr, ORBIT_E_ARG, "%s: desc is NULL", fn);
+  const orbit_gated_norm_desc& d = *desc;
+  ORBIT_TRY(check_dtype(fn, d.dtype));
+  REQ(d.rows > 0 && d.n > 0 && d.n % 8 == 0, ORBIT_E_ARG, "%s: bad sizes rows=%d n=%d (n must be a multiple of 8)", fn,
+      d.rows, d.n);
+  REQ(d.n <= 16384, ORBIT_E_UNSUPPORTED, "%s: n=%d exceeds 16384", fn, d.n);
+  REQ((d.post_norm == 0 || d.post_norm == 1) && (d.pre_norm == 0 || d.pre_norm == 1), ORBIT_E_ARG,
+      "%s: post_norm and pre_norm must be 0 or 1", fn);
+  REQ(d.gate_rows >= 0 && (d.gate_rows == 0 || d.rows % d.gate_rows == 0), ORBIT_E_ARG,
+      "%s: gate_rows=%d must divide rows=%d", fn, d.gate_rows, d.rows);
+  REQ(d.eps > 0.f, ORBIT_E_ARG, "%s: eps must be positive", fn);
+  o->rows = d.rows; o->n = d.n; o->gates = d.gate_rows; o->post = d.post_norm != 0; o->pre = d.pre_norm != 0;
+  o->scale = d.scale; o->eps = d.eps; o->dt = (orbit_dtype)d.dtype;
+  return ORBIT_OK;
+}
+
+static orbit_status gnorm_params_check(const char* fn, const GnormDims& z, const orbit_gated_norm_params* p,
+                                       bool shifts) {
+  REQ(p != nullptr, ORBIT_E_ARG, "%s: params is NULL", fn);
+  if (z.gates) PTR(p->gate, "gate");
+  if (z.post) { PTR(p->post_g, "post_g"); PTR(p->post_b, "post_b"); }
+  if (z.pre) { PTR(p->pre_g, "pre_g"); if (shifts) PTR(p->pre_b, "pre_b"); }
+  return ORBIT_OK;
+}
+
+static GnormParams gnorm_params(const orbit_gated_norm_params* p) {
+  return GnormParams{p->gate, p->post_g, p->post_b, p->pre_g, p->pre_b};
+}
+
+orbit_status orbit_gated_norm_fwd(const orbit_gated_norm_desc* desc, const orbit_gated_norm_params* p, const void* x,
+                                  const void* f, void* store, size_t store_bytes, void* y, void* h, float* stats,
+                                  void* stream) {
+  const char* fn = "orbit_gated_norm_fwd";
+  clear_error();
+  GnormDims z;
+  ORBIT_TRY(gnorm_check(fn, desc, &z));
+  ORBIT_TRY(gnorm_params_check(fn, z, p, true));
+  PTR(x, "x"); OPT_PTR(f, "f"); PTR(y, "y"); PTR(stats, "stats");
+  REQ(f || store, ORBIT_E_ARG, "%s: f and its store are both NULL", fn);
+  if (store) ORBIT_TRY(act8_check(fn, z.rows, z.n, store, store_bytes));
+  if (z.pre) PTR(h, "h");
+  REQ(y != x && y != f && (!z.pre || (h != x && h != f && h != y)), ORBIT_E_ARG,
+      "%s: y and h must not alias x, f or each other", fn);
+  return gnorm_fwd(z, gnorm_params(p), x, f, store, y, h, stats, S(stream));
+}
+
+size_t orbit_gated_norm_bwd_workspace_bytes(const orbit_gated_norm_desc* desc) {
+  GnormDims z;
+  if (gnorm_check("orbit_gated_norm_bwd_workspace_bytes", desc, &z) != ORBIT_OK) return 0;
+  return gnorm_bwd_ws_bytes(z);
+}
+
+orbit_status orbit_gated_norm_bwd(const orbit_gated_norm_desc* desc, const orbit_gated_norm_params* p, const void* f,
+                                  const void* store, size_t store_bytes, const void* y, const float* stats,
+                                  const void* dh, const void* dy, void* dx, void* df, const orbit_gated_norm_grads* g,
+                                  int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "orbit_gated_norm_bwd";
+  clear_error();
+  GnormDims z;
+  ORBIT_TRY(gnorm_check(fn, desc, &z));
+  ORBIT_TRY(gnorm_params_check(fn, z, p, false));
+  REQ(g != nullptr, ORBIT_E_ARG, "%s: grads is NULL", fn);
+  OPT_PTR(f, "f"); PTR(stats, "stats"); OPT_PTR(dy, "dy"); OPT_PTR(dx, "dx"); PTR(df, "df"); PTR(ws, "ws");
+  if (z.post || z.gates) {
+    REQ(f || store, ORBIT_E_ARG, "%s: f and its store are both NULL", fn);
+    if (!f) ORBIT_TRY(act8_check(fn, z.rows, z.n, store, store_bytes));
+  }
+  if (z.pre) { PTR(y, "y"); PTR(dh, "dh"); PTR(g->pre_g, "grads.pre_g"); PTR(g->pre_b, "grads.pre_b"); }
+  REQ(z.pre || dy, ORBIT_E_ARG, "%s: dy is NULL without pre_norm", fn);
+  if (z.post) { PTR(g->post_g, "grads.post_g"); PTR(g->post_b, "grads.post_b"); }
+  if (z.gates) PTR(g->gate, "grads.gate");
+  REQ(dx != df && (!z.pre || (dx != y && df != y && dx != dh)) && df != dy, ORBIT_E_ARG,
+      "%s: dx may alias dy and df may alias dh or f, nothing else", fn);
+  REQ(!dx || dx != f, ORBIT_E_ARG, "%s: dx must not alias f", fn);
+  REQ(accumulate == 0 || accumulate == 1, ORBIT_E_ARG, "%s: accumulate must be 0 or 1", fn);
+  const size_t need = gnorm_bwd_ws_bytes(z);
+  REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes,
+      need);
+  const GnormGrads gg{g->gate, g->post_g, g->post_b, g->pre_g, g->pre_b};
+  return gnorm_bwd(z, gnorm_params(p), f, store, y, stats, z.pre ? dh : nullptr, dy, dx, df, gg, accumulate, ws,
+                   S(stream));
 }
 
 }  // extern "C"
