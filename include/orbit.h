@@ -122,6 +122,43 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
                                  const orbit_block_grads* g, int accumulate,
                                  void* ws, size_t ws_bytes, void* stream);
 
+/* The block with its residuals scaled, gated and normed, and / or with `saved`
+ * in 8 bits. With p_i = post_norm ? LN(f_i) post_i_g + post_i_b : f_i (eps as in
+ * desc) for the sub-layers' outputs f_1 = o W_proj + b_proj and
+ * f_2 = GELU(u) W_fc2 + b_fc2:
+ *   x1 = x + scale gate_1 p_1;   y = x1 + scale gate_2 p_2
+ * (gates as in orbit_gated_norm_desc below, over the B*L tokens; 0 gate rows:
+ * ones). The rest, shards included, is orbit_vit_block_fwd's, whose result this
+ * is, bit for bit, with act8 = post_norm = gate_rows = 0 and scale 1.
+ * act8 = 1: `saved` holds q, k, v, o, u and the sub-layers' outputs as 8-bit
+ * stores (see orbit_act8_bytes below) and the softmax normalisers in float32:
+ * about a fifth of the bytes in bf16. The forward's result does not depend on
+ * it; the backward reads the stores back into its workspace, forms x1 and the
+ * norms' and GELU's outputs from them, and runs as from stored tensors, so that
+ * its gradients carry the stores' rounding (at most half a step of a group of
+ * 32 values, below 2^-7 of its largest). saved == NULL is inference, and
+ * activation checkpointing without that rounding, as in the plain calls. */
+typedef struct {
+  int32_t act8, post_norm, gate_rows;
+  float scale;
+} orbit_block_ext;
+typedef struct {
+  const void *post1_g, *post1_b, *gate1; /* [d], [d], [gate_rows, d] (NULL if absent) */
+  const void *post2_g, *post2_b, *gate2;
+} orbit_block_ext_params; /* may be NULL without post_norm and gates */
+typedef struct { float *post1_g, *post1_b, *gate1, *post2_g, *post2_b, *gate2; } orbit_block_ext_grads;
+
+size_t orbit_vit_block_ext_saved_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext);
+size_t orbit_vit_block_ext_workspace_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext);
+orbit_status orbit_vit_block_ext_fwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_params* p, const orbit_block_ext_params* ep, const void* x,
+                                     void* y, void* saved, void* ws, size_t ws_bytes, void* stream);
+orbit_status orbit_vit_block_ext_bwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_params* p, const orbit_block_ext_params* ep, const void* x,
+                                     const void* saved, const void* dy, void* dx, const orbit_block_grads* g,
+                                     const orbit_block_ext_grads* eg, int accumulate, void* ws, size_t ws_bytes,
+                                     void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Per-variable patch tokenisation (Sec. II: every variable is tokenised     */
 /* independently)                                                            */

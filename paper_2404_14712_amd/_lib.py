@@ -22,6 +22,7 @@ ABI_VERSION = 2
 BLOCK_PARAMS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "qn_g", "qn_b", "kn_g", "kn_b",
                 "w_proj", "b_proj", "ln2_g", "ln2_b", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
 AGG_PARAMS = ("q0", "w_q", "b_q", "w_k", "b_k", "w_v", "b_v", "w_o", "b_o", "pos")
+BLOCK_EXT_PARAMS = ("post1_g", "post1_b", "gate1", "post2_g", "post2_b", "gate2")
 GATED_NORM_PARAMS = ("gate", "post_g", "post_b", "pre_g", "pre_b")
 HEAD_PARAMS = ("lnf_g", "lnf_b", "w_h", "b_h", "w_hid", "b_hid")
 
@@ -38,6 +39,18 @@ class BlockParams(ctypes.Structure):
 
 class BlockGrads(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in BLOCK_PARAMS]
+
+
+class BlockExt(ctypes.Structure):
+    _fields_ = [("act8", c_int32), ("post_norm", c_int32), ("gate_rows", c_int32), ("scale", c_float)]
+
+
+class BlockExtParams(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in BLOCK_EXT_PARAMS]
+
+
+class BlockExtGrads(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in BLOCK_EXT_PARAMS]
 
 
 class EmbedDesc(ctypes.Structure):
@@ -103,6 +116,13 @@ _PROTOS = {
     "orbit_vit_block_fwd": (c_int, [POINTER(BlockDesc), POINTER(BlockParams), P, P, P, P, c_size_t, P]),
     "orbit_vit_block_bwd": (c_int, [POINTER(BlockDesc), POINTER(BlockParams), P, P, P, P, POINTER(BlockGrads),
                                     c_int, P, c_size_t, P]),
+    "orbit_vit_block_ext_saved_bytes": (c_size_t, [POINTER(BlockDesc), POINTER(BlockExt)]),
+    "orbit_vit_block_ext_workspace_bytes": (c_size_t, [POINTER(BlockDesc), POINTER(BlockExt)]),
+    "orbit_vit_block_ext_fwd": (c_int, [POINTER(BlockDesc), POINTER(BlockExt), POINTER(BlockParams),
+                                        POINTER(BlockExtParams), P, P, P, P, c_size_t, P]),
+    "orbit_vit_block_ext_bwd": (c_int, [POINTER(BlockDesc), POINTER(BlockExt), POINTER(BlockParams),
+                                        POINTER(BlockExtParams), P, P, P, P, POINTER(BlockGrads),
+                                        POINTER(BlockExtGrads), c_int, P, c_size_t, P]),
     "orbit_patch_embed": (c_int, [POINTER(EmbedDesc), P, P, P, P, P, P]),
     "orbit_patch_embed_workspace_bytes": (c_size_t, [POINTER(EmbedDesc)]),
     "orbit_patch_embed_bwd": (c_int, [POINTER(EmbedDesc), P, P, P, P, P, c_int, P, c_size_t, P]),
@@ -226,6 +246,27 @@ class OrbitLib:
         self._check("orbit_vit_block_bwd", self.lib.orbit_vit_block_bwd(
             ctypes.byref(desc), ctypes.byref(p), _ptr(x), _ptr(saved), _ptr(dy), _ptr(dx), ctypes.byref(g),
             int(accumulate), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+    # -- block with gated norms and / or saved tensors in 8 bits ------------------
+    def orbit_vit_block_ext_saved_bytes(self, desc: BlockDesc, ext: BlockExt) -> int:
+        return self.lib.orbit_vit_block_ext_saved_bytes(ctypes.byref(desc), ctypes.byref(ext))
+
+    def orbit_vit_block_ext_workspace_bytes(self, desc: BlockDesc, ext: BlockExt) -> int:
+        return self.lib.orbit_vit_block_ext_workspace_bytes(ctypes.byref(desc), ctypes.byref(ext))
+
+    def orbit_vit_block_ext_fwd(self, desc, ext, params, x, y, saved, ws, stream=None):
+        """params: the block's and the extension's, by name."""
+        p, e = self._struct(BlockParams, params), self._struct(BlockExtParams, params)
+        self._check("orbit_vit_block_ext_fwd", self.lib.orbit_vit_block_ext_fwd(
+            ctypes.byref(desc), ctypes.byref(ext), ctypes.byref(p), ctypes.byref(e), _ptr(x), _ptr(y), _ptr(saved),
+            _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    def orbit_vit_block_ext_bwd(self, desc, ext, params, x, saved, dy, dx, grads, accumulate, ws, stream=None):
+        p, e = self._struct(BlockParams, params), self._struct(BlockExtParams, params)
+        g, eg = self._struct(BlockGrads, grads), self._struct(BlockExtGrads, grads)
+        self._check("orbit_vit_block_ext_bwd", self.lib.orbit_vit_block_ext_bwd(
+            ctypes.byref(desc), ctypes.byref(ext), ctypes.byref(p), ctypes.byref(e), _ptr(x), _ptr(saved), _ptr(dy),
+            _ptr(dx), ctypes.byref(g), ctypes.byref(eg), int(accumulate), _ptr(ws), _nbytes(ws), _stream(stream)))
 
     # -- patch embedding -------------------------------------------------------
     def orbit_patch_embed(self, desc, img, w_pe, b_pe, ve, tok, stream=None):

@@ -87,7 +87,18 @@ orbit_status block_dims(const char* fn, const orbit_block_desc* desc, BlockDims*
   return ORBIT_OK;
 }
 
+// The residual form of a block: a norm, gate and scale on each sub-layer's
+// output, and saved tensors in 8 bits. `on` is false for the plain block.
+struct BlockExt {
+  bool on = false, act8 = false, post = false;
+  int gates = 0;
+  float scale = 1.f;
+  bool branch() const { return post || gates; }  // the backward reads the sub-layers' outputs
+};
+
 struct BlockSaved {
+  void *f1, *f2;     // sub-layer outputs (ext.branch() only)
+  float *st1, *st2;  // statistics of the gated norms [T, 4] (ext only)
   float *mu1, *r1;
   void* h1;
   void* qkv;
@@ -103,10 +114,18 @@ struct BlockSaved {
   void* g;
 };
 
-BlockSaved carve_block_saved(const BlockDims& z, void* base, size_t* used) {
+BlockSaved carve_block_saved(const BlockDims& z, const BlockExt& x, void* base, size_t* used) {
   Carver c(base);
   const size_t e = esz(z.dt);
   BlockSaved s{};
+  if (x.on) {
+    s.st1 = c.take<float>(z.T * 4);
+    s.st2 = c.take<float>(z.T * 4);
+    if (x.branch()) {
+      s.f1 = c.take<char>(z.T * z.d * e);
+      s.f2 = c.take<char>(z.T * z.d * e);
+    }
+  }
   s.mu1 = c.take<float>(z.T);
   s.r1 = c.take<float>(z.T);
   s.h1 = c.take<char>(z.T * z.d * e);
@@ -117,7 +136,8 @@ BlockSaved carve_block_saved(const BlockDims& z, void* base, size_t* used) {
     s.qr = c.take<float>(z.T * 2 * z.H);
   }
   s.o = c.take<char>(z.T * z.A * e);
-  s.o32 = z.dt == ORBIT_BF16 ? c.take<float>(z.T * z.A) : nullptr;
+  // a stored 8-bit o is exact in bf16: no float32 copy to keep beside it
+  s.o32 = z.dt == ORBIT_BF16 && !x.act8 ? c.take<float>(z.T * z.A) : nullptr;
   s.lse = c.take<float>(z.T * z.H);
   s.x1 = c.take<char>(z.T * z.d * e);
   s.mu2 = c.take<float>(z.T);
@@ -129,10 +149,45 @@ BlockSaved carve_block_saved(const BlockDims& z, void* base, size_t* used) {
   return s;
 }
 
-size_t block_saved_bytes(const BlockDims& z) {
+// Saved tensors in 8 bits (act8.h). h1 and h2 are formed again by their norms,
+// g by the GELU, x1 from x and the store of f1; lse and f2's statistics stay
+// float32.
+struct BlockSaved8 {
+  void *qkv, *o, *f1, *u, *f2;  // f2: ext.branch() only
+  float *lse, *st2;
+};
+
+BlockSaved8 carve_block_saved8(const BlockDims& z, const BlockExt& x, void* base, size_t* used) {
+  Carver c(base);
+  BlockSaved8 s{};
+  s.qkv = c.take<char>(act8_store_bytes(z.T, 3 * z.A));
+  s.o = c.take<char>(act8_store_bytes(z.T, z.A));
+  s.f1 = c.take<char>(act8_store_bytes(z.T, z.d));
+  s.u = c.take<char>(act8_store_bytes(z.T, z.F));
+  if (x.branch()) s.f2 = c.take<char>(act8_store_bytes(z.T, z.d));
+  s.lse = c.take<float>(z.T * z.H);
+  s.st2 = c.take<float>(z.T * 4);
+  if (used) *used = c.used();
+  return s;
+}
+
+// bytes of the tensors the backward reads, in full types
+size_t block_full_bytes(const BlockDims& z, BlockExt x) {
   size_t u = 0;
-  carve_block_saved(z, nullptr, &u);
+  x.act8 = false;
+  carve_block_saved(z, x, nullptr, &u);
   return u;
+}
+
+size_t block_saved_bytes(const BlockDims& z, const BlockExt& x) {
+  if (!x.act8) return block_full_bytes(z, x);
+  size_t u = 0;
+  carve_block_saved8(z, x, nullptr, &u);
+  return u;
+}
+
+GnormDims block_gnorm(const BlockDims& z, const BlockExt& x, bool pre) {
+  return GnormDims{(int)z.T, z.d, x.gates, x.post, pre, x.scale, z.eps, z.dt};
 }
 
 struct BlockWs {
@@ -143,6 +198,11 @@ struct BlockWs {
   void* dqkv;  // [T, 3A]
   float* D;    // attention backward workspace
   float *p_fc1, *p_fc2, *p_ln2, *p_qkv, *p_ln1;  // column-sum partials
+  // ext only: gradient of a sub-layer's output [T, d], the projection's bias
+  // partials, the gated norms' workspaces
+  void* df;
+  float* p_proj;
+  void *gn1, *gn2;
   void* qws;
   void* gws;
   size_t gws_bytes;
@@ -166,10 +226,11 @@ size_t block_gemm_ws(const BlockDims& z) {
   return m;
 }
 
-size_t block_ws_layout(const BlockDims& z, void* base, size_t bytes, BlockWs* w, bool inference_saved) {
+size_t block_ws_layout(const BlockDims& z, const BlockExt& x, void* base, size_t bytes, BlockWs* w) {
   Carver c(base);
   const size_t e = esz(z.dt);
-  if (inference_saved) c.take<char>(block_saved_bytes(z));
+  // the tensors the backward reads, where no stored ones are passed
+  c.take<char>(block_full_bytes(z, x));
   BlockWs t{};
   t.du = c.take<char>(z.T * z.F * e);
   t.dx1 = c.take<char>(z.T * z.d * e);
@@ -184,6 +245,12 @@ size_t block_ws_layout(const BlockDims& z, void* base, size_t bytes, BlockWs* w,
   t.p_ln2 = c.take<float>(ln_bwd_cols_part_bytes(T, z.d, true) / sizeof(float));
   t.p_qkv = c.take<float>(colsum_part_bytes(T, 3 * z.A, false) / sizeof(float));
   t.p_ln1 = c.take<float>(ln_bwd_cols_part_bytes(T, z.d, false) / sizeof(float));
+  if (x.on) {
+    t.df = c.take<char>(z.T * z.d * e);
+    t.p_proj = c.take<float>(colsum_part_bytes(T, z.d, false) / sizeof(float));
+    t.gn1 = c.take<char>(gnorm_bwd_ws_bytes(block_gnorm(z, x, true)));
+    t.gn2 = c.take<char>(gnorm_bwd_ws_bytes(block_gnorm(z, x, false)));
+  }
   t.qws = c.take<char>(qk_norm_bwd_workspace_bytes(z.dh));
   const size_t g = block_gemm_ws(z);
   t.gws = c.take<char>(g);
@@ -193,19 +260,30 @@ size_t block_ws_layout(const BlockDims& z, void* base, size_t bytes, BlockWs* w,
   return used;
 }
 
-size_t block_ws_bytes(const BlockDims& z) {
+size_t block_ws_bytes(const BlockDims& z, const BlockExt& x) {
   // the backward layout; the forward needs only the GEMM part (plus the
   // saved-tensor region when called without `saved`)
-  return block_ws_layout(z, nullptr, 0, nullptr, true);
+  return block_ws_layout(z, x, nullptr, 0, nullptr);
+}
+
+GnormParams block_gnorm_params(const orbit_block_params* p, const orbit_block_ext_params* ep, int sub) {
+  GnormParams g{};
+  if (ep && sub == 1) { g.gate = ep->gate1; g.post_g = ep->post1_g; g.post_b = ep->post1_b; }
+  if (ep && sub == 2) { g.gate = ep->gate2; g.post_g = ep->post2_g; g.post_b = ep->post2_b; }
+  if (sub == 1) { g.pre_g = p->ln2_g; g.pre_b = p->ln2_b; }
+  return g;
 }
 
 // The forward's kernel sequence, writing the tensors the backward reads into
-// `sv`. With y == NULL the last product (fc2, whose output the backward does
-// not read) is skipped: the recompute of the activation-checkpoint backward.
-orbit_status block_forward_steps(const BlockDims& z, const orbit_block_params* p, const void* x, void* y,
-                                 const BlockSaved& sv, const BlockWs& w, hipStream_t s) {
+// `sv`. With y == NULL the last product (fc2) is skipped where the backward
+// does not read its output: the recompute of the activation-checkpoint
+// backward. s8 (may be null): the 8-bit stores, written as the tensors appear.
+orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const orbit_block_params* p,
+                                 const orbit_block_ext_params* ep, const void* x, void* y, const BlockSaved& sv,
+                                 const BlockSaved8* s8, const BlockWs& w, hipStream_t s) {
   const int T = (int)z.T;
   const orbit_dtype dt = z.dt;
+  float* lse = s8 ? s8->lse : sv.lse;
   ORBIT_TRY(layernorm_fwd(dt, x, z.d, p->ln1_g, p->ln1_b, sv.h1, z.d, sv.mu1, sv.r1, T, z.d, z.eps, s));
   {
     Gemm g; g.dtype = dt; g.tag = "qkv";
@@ -228,51 +306,69 @@ orbit_status block_forward_steps(const BlockDims& z, const orbit_block_params* p
   }
   // the attention backward's workspace is idle during the forward and holds
   // the forward's split partials
-  ORBIT_TRY(attn_fwd(dt, io, sv.o, z.A, sv.lse, sv.o32, z.A, w.D, attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh), s));
+  ORBIT_TRY(attn_fwd(dt, io, sv.o, z.A, lse, sv.o32, z.A, w.D, attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh), s));
+  if (s8) {
+    ORBIT_TRY(act8_pack(dt, sv.qkv, 3 * z.A, T, 3 * z.A, s8->qkv, s));
+    ORBIT_TRY(act8_pack(dt, sv.o, z.A, T, z.A, s8->o, s));
+  }
+  // where the backward does not read a sub-layer's output, it passes through a
+  // buffer of the backward that is idle here
+  void* f1 = ext.branch() ? sv.f1 : w.dx1;
+  void* f2 = ext.branch() ? sv.f2 : w.dh;
   {
     Gemm g; g.dtype = dt; g.tag = "proj";
-    g.A = sv.o; g.lda = z.A; g.B = p->w_proj; g.ldb = z.d; g.C = sv.x1; g.ldc = z.d;
-    g.M = T; g.N = z.d; g.K = z.A; g.bias = p->b_proj; g.res = x; g.ldr = z.d;
+    g.A = sv.o; g.lda = z.A; g.B = p->w_proj; g.ldb = z.d; g.C = ext.on ? f1 : sv.x1; g.ldc = z.d;
+    g.M = T; g.N = z.d; g.K = z.A; g.bias = p->b_proj;
+    if (!ext.on) { g.res = x; g.ldr = z.d; }
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
-  ORBIT_TRY(layernorm_fwd(dt, sv.x1, z.d, p->ln2_g, p->ln2_b, sv.h2, z.d, sv.mu2, sv.r2, T, z.d, z.eps, s));
+  if (ext.on) {
+    ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), x, f1, s8 ? s8->f1 : nullptr, sv.x1,
+                        sv.h2, sv.st1, s));
+  } else {
+    ORBIT_TRY(layernorm_fwd(dt, sv.x1, z.d, p->ln2_g, p->ln2_b, sv.h2, z.d, sv.mu2, sv.r2, T, z.d, z.eps, s));
+  }
   {
     Gemm g; g.dtype = dt; g.tag = "fc1";
     g.A = sv.h2; g.lda = z.d; g.B = p->w_fc1; g.ldb = z.F; g.C = sv.g; g.ldc = z.F;
     g.M = T; g.N = z.F; g.K = z.d; g.bias = p->b_fc1; g.gelu_out = sv.u; g.ldgo = z.F;
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
-  if (y) {
+  if (s8) ORBIT_TRY(act8_pack(dt, sv.u, z.F, T, z.F, s8->u, s));
+  if (y || ext.branch()) {
     Gemm g; g.dtype = dt; g.tag = "fc2";
-    g.A = sv.g; g.lda = z.F; g.B = p->w_fc2; g.ldb = z.d; g.C = y; g.ldc = z.d;
-    g.M = T; g.N = z.d; g.K = z.F; g.bias = p->b_fc2; g.res = sv.x1; g.ldr = z.d;
+    g.A = sv.g; g.lda = z.F; g.B = p->w_fc2; g.ldb = z.d; g.C = ext.on ? f2 : y; g.ldc = z.d;
+    g.M = T; g.N = z.d; g.K = z.F; g.bias = p->b_fc2;
+    if (!ext.on) { g.res = sv.x1; g.ldr = z.d; }
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
+  // the recompute runs this norm too where the backward reads its statistics;
+  // its output then goes to an idle buffer
+  if (ext.on && (y || ext.post))
+    ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, false), block_gnorm_params(p, ep, 2), sv.x1, f2, s8 ? s8->f2 : nullptr,
+                        y ? y : w.dh, nullptr, s8 ? s8->st2 : sv.st2, s));
   return ORBIT_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t orbit_vit_block_saved_bytes(const orbit_block_desc* desc) {
-  BlockDims z;
-  if (block_dims("orbit_vit_block_saved_bytes", desc, &z) != ORBIT_OK) return 0;
-  return block_saved_bytes(z);
+// The tensors the backward reads, from the 8-bit stores.
+orbit_status block_restore(const BlockDims& z, const BlockExt& ext, const orbit_block_params* p,
+                           const orbit_block_ext_params* ep, const void* x, const BlockSaved8& s8,
+                           const BlockSaved& sv, hipStream_t s) {
+  const int T = (int)z.T;
+  ORBIT_TRY(layernorm_fwd(z.dt, x, z.d, p->ln1_g, p->ln1_b, sv.h1, z.d, sv.mu1, sv.r1, T, z.d, z.eps, s));
+  ORBIT_TRY(act8_unpack(z.dt, s8.qkv, T, 3 * z.A, sv.qkv, 3 * z.A, nullptr, 0, s));
+  if (z.qk)
+    ORBIT_TRY(qk_norm_fwd(z.dt, sv.qkv, 3 * z.A, sv.qkn, 2 * z.A, p->qn_g, p->qn_b, p->kn_g, p->kn_b, sv.qmu, sv.qr,
+                          T, z.H, z.dh, z.eps, s));
+  ORBIT_TRY(act8_unpack(z.dt, s8.o, T, z.A, sv.o, z.A, nullptr, 0, s));
+  ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), x, nullptr, s8.f1, sv.x1, sv.h2, sv.st1,
+                      s));
+  return act8_unpack(z.dt, s8.u, T, z.F, sv.u, z.F, sv.g, z.F, s);
 }
 
-size_t orbit_vit_block_workspace_bytes(const orbit_block_desc* desc) {
-  BlockDims z;
-  if (block_dims("orbit_vit_block_workspace_bytes", desc, &z) != ORBIT_OK) return 0;
-  return block_ws_bytes(z);
-}
-
-orbit_status orbit_vit_block_fwd(const orbit_block_desc* desc, const orbit_block_params* p, const void* x, void* y,
-                                 void* saved, void* ws, size_t ws_bytes, void* stream) {
-  const char* fn = "orbit_vit_block_fwd";
-  clear_error();
-  BlockDims z;
-  ORBIT_TRY(block_dims(fn, desc, &z));
+// Arguments shared by the plain and the extended entry points.
+orbit_status block_fwd_check(const char* fn, const BlockDims& z, const BlockExt& ext, const orbit_block_params* p,
+                             const void* x, const void* y, const void* saved, const void* ws, size_t ws_bytes) {
   REQ(p != nullptr, ORBIT_E_ARG, "%s: params is NULL", fn);
   PTR(x, "x");
   PTR(y, "y");
@@ -283,15 +379,54 @@ orbit_status orbit_vit_block_fwd(const orbit_block_desc* desc, const orbit_block
   if (z.qk) { PTR(p->qn_g, "qn_g"); PTR(p->qn_b, "qn_b"); PTR(p->kn_g, "kn_g"); PTR(p->kn_b, "kn_b"); }
   OPT_PTR(saved, "saved");
   PTR(ws, "ws");
-  const size_t need = block_ws_bytes(z);
+  const size_t need = block_ws_bytes(z, ext);
   REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes,
       need);
-  hipStream_t s = S(stream);
-  const bool inference = saved == nullptr;
+  return ORBIT_OK;
+}
+
+orbit_status block_forward(const BlockDims& z, BlockExt ext, const orbit_block_params* p,
+                           const orbit_block_ext_params* ep, const void* x, void* y, void* saved, void* ws,
+                           size_t ws_bytes, hipStream_t s) {
   BlockWs w;
-  block_ws_layout(z, ws, ws_bytes, &w, true);
-  const BlockSaved sv = carve_block_saved(z, inference ? ws : saved, nullptr);
-  return block_forward_steps(z, p, x, y, sv, w, s);
+  block_ws_layout(z, ext, ws, ws_bytes, &w);
+  if (!saved) ext.act8 = false;
+  const BlockSaved sv = carve_block_saved(z, ext, saved == nullptr || ext.act8 ? ws : saved, nullptr);
+  BlockSaved8 s8{};
+  if (ext.act8) s8 = carve_block_saved8(z, ext, saved, nullptr);
+  return block_forward_steps(z, ext, p, ep, x, y, sv, ext.act8 ? &s8 : nullptr, w, s);
+}
+
+orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, const orbit_block_params* p,
+                            const orbit_block_ext_params* ep, const void* x, const void* saved, const void* dy,
+                            void* dx, const orbit_block_grads* gr, const orbit_block_ext_grads* eg, int accumulate,
+                            void* ws, size_t ws_bytes, hipStream_t s);
+
+}  // namespace
+
+extern "C" {
+
+size_t orbit_vit_block_saved_bytes(const orbit_block_desc* desc) {
+  BlockDims z;
+  if (block_dims("orbit_vit_block_saved_bytes", desc, &z) != ORBIT_OK) return 0;
+  return block_saved_bytes(z, BlockExt{});
+}
+
+size_t orbit_vit_block_workspace_bytes(const orbit_block_desc* desc) {
+  BlockDims z;
+  if (block_dims("orbit_vit_block_workspace_bytes", desc, &z) != ORBIT_OK) return 0;
+  return block_ws_bytes(z, BlockExt{});
+}
+
+orbit_status orbit_vit_block_fwd(const orbit_block_desc* desc, const orbit_block_params* p, const void* x, void* y,
+                                 void* saved, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "orbit_vit_block_fwd";
+  clear_error();
+  BlockDims z;
+  const BlockExt plain{};
+  ORBIT_TRY(block_dims(fn, desc, &z));
+  ORBIT_TRY(block_fwd_check(fn, z, plain, p, x, y, saved, ws, ws_bytes));
+  return block_forward(z, plain, p, nullptr, x, y, saved, ws, ws_bytes, S(stream));
 }
 
 orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block_params* p, const void* x,
@@ -301,15 +436,105 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   clear_error();
   BlockDims z;
   ORBIT_TRY(block_dims(fn, desc, &z));
+  return block_backward(fn, z, BlockExt{}, p, nullptr, x, saved, dy, dx, gr, nullptr, accumulate, ws, ws_bytes,
+                        S(stream));
+}
+
+// ---------------------------------------------------------------------------
+// block with gated norms and / or saved tensors in 8 bits
+// ---------------------------------------------------------------------------
+static orbit_status block_ext(const char* fn, const BlockDims& z, const orbit_block_ext* e, BlockExt* o) {
+  REQ(e != nullptr, ORBIT_E_ARG, "%s: ext is NULL", fn);
+  REQ((e->act8 == 0 || e->act8 == 1) && (e->post_norm == 0 || e->post_norm == 1), ORBIT_E_ARG,
+      "%s: act8 and post_norm must be 0 or 1", fn);
+  REQ(e->gate_rows >= 0 && (e->gate_rows == 0 || z.T % e->gate_rows == 0), ORBIT_E_ARG,
+      "%s: gate_rows=%d must divide the %lld tokens", fn, e->gate_rows, (long long)z.T);
+  o->act8 = e->act8 != 0; o->post = e->post_norm != 0; o->gates = e->gate_rows; o->scale = e->scale;
+  // with nothing asked for this is the plain block
+  o->on = o->act8 || o->branch() || o->scale != 1.f;
+  return ORBIT_OK;
+}
+
+static orbit_status block_ext_params_check(const char* fn, const BlockExt& x, const orbit_block_ext_params* ep) {
+  if (!x.branch()) return ORBIT_OK;
+  REQ(ep != nullptr, ORBIT_E_ARG, "%s: ext params is NULL", fn);
+  if (x.gates) { PTR(ep->gate1, "gate1"); PTR(ep->gate2, "gate2"); }
+  if (x.post) {
+    PTR(ep->post1_g, "post1_g"); PTR(ep->post1_b, "post1_b"); PTR(ep->post2_g, "post2_g"); PTR(ep->post2_b, "post2_b");
+  }
+  return ORBIT_OK;
+}
+
+size_t orbit_vit_block_ext_saved_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext) {
+  const char* fn = "orbit_vit_block_ext_saved_bytes";
+  BlockDims z;
+  BlockExt x;
+  if (block_dims(fn, desc, &z) != ORBIT_OK || block_ext(fn, z, ext, &x) != ORBIT_OK) return 0;
+  return block_saved_bytes(z, x);
+}
+
+size_t orbit_vit_block_ext_workspace_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext) {
+  const char* fn = "orbit_vit_block_ext_workspace_bytes";
+  BlockDims z;
+  BlockExt x;
+  if (block_dims(fn, desc, &z) != ORBIT_OK || block_ext(fn, z, ext, &x) != ORBIT_OK) return 0;
+  return block_ws_bytes(z, x);
+}
+
+orbit_status orbit_vit_block_ext_fwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_params* p, const orbit_block_ext_params* ep, const void* x,
+                                     void* y, void* saved, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "orbit_vit_block_ext_fwd";
+  clear_error();
+  BlockDims z;
+  BlockExt e;
+  ORBIT_TRY(block_dims(fn, desc, &z));
+  ORBIT_TRY(block_ext(fn, z, ext, &e));
+  ORBIT_TRY(block_fwd_check(fn, z, e, p, x, y, saved, ws, ws_bytes));
+  ORBIT_TRY(block_ext_params_check(fn, e, ep));
+  return block_forward(z, e, p, ep, x, y, saved, ws, ws_bytes, S(stream));
+}
+
+orbit_status orbit_vit_block_ext_bwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_params* p, const orbit_block_ext_params* ep, const void* x,
+                                     const void* saved, const void* dy, void* dx, const orbit_block_grads* gr,
+                                     const orbit_block_ext_grads* eg, int accumulate, void* ws, size_t ws_bytes,
+                                     void* stream) {
+  const char* fn = "orbit_vit_block_ext_bwd";
+  clear_error();
+  BlockDims z;
+  BlockExt e;
+  ORBIT_TRY(block_dims(fn, desc, &z));
+  ORBIT_TRY(block_ext(fn, z, ext, &e));
+  ORBIT_TRY(block_ext_params_check(fn, e, ep));
+  if (e.branch()) {
+    REQ(eg != nullptr, ORBIT_E_ARG, "%s: ext grads is NULL", fn);
+    if (e.gates) { PTR(eg->gate1, "grads.gate1"); PTR(eg->gate2, "grads.gate2"); }
+    if (e.post) {
+      PTR(eg->post1_g, "grads.post1_g"); PTR(eg->post1_b, "grads.post1_b");
+      PTR(eg->post2_g, "grads.post2_g"); PTR(eg->post2_b, "grads.post2_b");
+    }
+  }
+  return block_backward(fn, z, e, p, ep, x, saved, dy, dx, gr, eg, accumulate, ws, ws_bytes, S(stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, const orbit_block_params* p,
+                            const orbit_block_ext_params* ep, const void* x, const void* saved, const void* dy,
+                            void* dx, const orbit_block_grads* gr, const orbit_block_ext_grads* eg, int accumulate,
+                            void* ws, size_t ws_bytes, hipStream_t s) {
   REQ(p != nullptr && gr != nullptr, ORBIT_E_ARG, "%s: params or grads is NULL", fn);
   PTR(x, "x"); OPT_PTR(saved, "saved"); PTR(dy, "dy"); PTR(dx, "dx"); PTR(ws, "ws");
   PTR(p->ln1_g, "ln1_g"); PTR(p->w_qkv, "w_qkv"); PTR(p->w_proj, "w_proj"); PTR(p->ln2_g, "ln2_g");
   PTR(p->w_fc1, "w_fc1"); PTR(p->w_fc2, "w_fc2");
   if (z.qk) { PTR(p->qn_g, "qn_g"); PTR(p->kn_g, "kn_g"); }
   REQ(dx != x, ORBIT_E_ARG, "%s: dx must not alias x", fn);
-  const bool recompute = saved == nullptr;
-  if (recompute) {
-    // the forward's other parameters are read again by the recompute
+  const bool recompute = saved == nullptr, restore = !recompute && ext.act8;
+  if (recompute || restore) {
+    // the forward's parameters that are read again
     PTR(p->ln1_b, "ln1_b"); PTR(p->b_qkv, "b_qkv"); PTR(p->b_proj, "b_proj"); PTR(p->ln2_b, "ln2_b");
     PTR(p->b_fc1, "b_fc1");
     if (z.qk) { PTR(p->qn_b, "qn_b"); PTR(p->kn_b, "kn_b"); }
@@ -321,16 +546,21 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   PTR(gr->w_fc1, "grads.w_fc1"); PTR(gr->b_fc1, "grads.b_fc1"); PTR(gr->w_fc2, "grads.w_fc2");
   PTR(gr->b_fc2, "grads.b_fc2");
   REQ(accumulate == 0 || accumulate == 1, ORBIT_E_ARG, "%s: accumulate must be 0 or 1", fn);
-  const size_t need = block_ws_bytes(z);
+  const size_t need = block_ws_bytes(z, ext);
   REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes,
       need);
-  hipStream_t s = S(stream);
   BlockWs w;
-  block_ws_layout(z, ws, ws_bytes, &w, true);
-  // activation checkpointing: the saved tensors are recomputed from x into the
-  // workspace's saved-tensor region (the region the inference forward uses)
-  const BlockSaved sv = carve_block_saved(z, recompute ? ws : const_cast<void*>(saved), nullptr);
-  if (recompute) ORBIT_TRY(block_forward_steps(z, p, x, nullptr, sv, w, s));
+  block_ws_layout(z, ext, ws, ws_bytes, &w);
+  if (recompute) ext.act8 = false;
+  // activation checkpointing: the saved tensors are recomputed from x, or read
+  // back from their 8-bit stores, into the workspace's saved-tensor region (the
+  // region the inference forward uses)
+  const BlockSaved sv = carve_block_saved(z, ext, recompute || restore ? ws : const_cast<void*>(saved), nullptr);
+  BlockSaved8 s8{};
+  if (restore) s8 = carve_block_saved8(z, ext, const_cast<void*>(saved), nullptr);
+  if (recompute) ORBIT_TRY(block_forward_steps(z, ext, p, ep, x, nullptr, sv, nullptr, w, s));
+  if (restore) ORBIT_TRY(block_restore(z, ext, p, ep, x, s8, sv, s));
+  const float* lse = restore ? s8.lse : sv.lse;
   const int T = (int)z.T;
   const orbit_dtype dt = z.dt;
   const size_t e = esz(dt);
@@ -351,11 +581,21 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   auto bias_job = [](ColJob& j, const void* src, int64_t n, float* part, float* out) {
     j.src = src; j.ld = n; j.n = (int)n; j.part = part; j.out_sum = out;
   };
+  // the feed-forward sub-layer's output gradient: dy, or through its gated norm
+  const void* dff = dy;
+  if (ext.on && (ext.branch() || ext.scale != 1.f)) {
+    GnormGrads gg{};
+    if (ext.gates) gg.gate = eg->gate2;
+    if (ext.post) { gg.post_g = eg->post2_g; gg.post_b = eg->post2_b; }
+    ORBIT_TRY(gnorm_bwd(block_gnorm(z, ext, false), block_gnorm_params(p, ep, 2), restore ? nullptr : sv.f2, s8.f2,
+                        nullptr, restore ? s8.st2 : sv.st2, nullptr, dy, nullptr, w.df, gg, accumulate, w.gn2, fin, s));
+    dff = w.df;
+  }
   // feed-forward sub-layer
   bool fused_fc2, fused_fc1;
   {
     Gemm g; g.dtype = dt; g.tag = "fc2_dw";
-    g.A = sv.g; g.lda = z.F; g.a_kmajor = false; g.B = dy; g.ldb = z.d; g.b_kmajor = false;
+    g.A = sv.g; g.lda = z.F; g.a_kmajor = false; g.B = dff; g.ldb = z.d; g.b_kmajor = false;
     g.C = gr->w_fc2; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
     g.M = z.F; g.N = z.d; g.K = T;
     fused_fc2 = dw_bias(g, w.p_fc2, gr->b_fc2);
@@ -363,7 +603,7 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   }
   {
     Gemm g; g.dtype = dt; g.tag = "fc2_dx";
-    g.A = dy; g.lda = z.d; g.B = p->w_fc2; g.ldb = z.d; g.b_kmajor = true;
+    g.A = dff; g.lda = z.d; g.B = p->w_fc2; g.ldb = z.d; g.b_kmajor = true;
     g.C = w.du; g.ldc = z.F; g.M = T; g.N = z.F; g.K = z.d; g.gelu_in = sv.u; g.ldgi = z.F;
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
@@ -379,7 +619,7 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
     ColJob j[2];
     int nj = 0;
     if (!fused_fc1) bias_job(j[nj++], w.du, z.F, w.p_fc1, gr->b_fc1);
-    if (!fused_fc2) bias_job(j[nj++], dy, z.d, w.p_fc2, gr->b_fc2);
+    if (!fused_fc2) bias_job(j[nj++], dff, z.d, w.p_fc2, gr->b_fc2);
     if (nj) ORBIT_TRY(colsum_partials(dt, j, nj, T, s));
     for (int i = 0; i < nj; ++i) fin.add_job(j[i], T);
   }
@@ -391,19 +631,40 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   }
   // LN2 backward; the chunk sums of its rows give the LN2 parameter gradients
   // and, summed over its output dx1, the projection's bias gradient
-  ORBIT_TRY(layernorm_bwd_cols(dt, w.dh, z.d, sv.x1, z.d, sv.mu2, sv.r2, p->ln2_g, dy, w.dx1, z.d, T, z.d, w.p_ln2,
-                               gr->ln2_b, gr->ln2_g, gr->b_proj, fin, s));
+  const void* df1 = w.dx1;  // gradient of the projection's output
+  if (!ext.on) {
+    ORBIT_TRY(layernorm_bwd_cols(dt, w.dh, z.d, sv.x1, z.d, sv.mu2, sv.r2, p->ln2_g, dy, w.dx1, z.d, T, z.d, w.p_ln2,
+                                 gr->ln2_b, gr->ln2_g, gr->b_proj, fin, s));
+  } else {
+    // dx1 is the residual's gradient; the projection's is the same tensor
+    // where nothing scales it
+    GnormGrads gg{};
+    gg.pre_g = gr->ln2_g; gg.pre_b = gr->ln2_b;
+    if (ext.gates) gg.gate = eg->gate1;
+    if (ext.post) { gg.post_g = eg->post1_g; gg.post_b = eg->post1_b; }
+    const bool same = !ext.branch() && ext.scale == 1.f;
+    if (!same) df1 = w.df;
+    ORBIT_TRY(gnorm_bwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), restore ? nullptr : sv.f1, s8.f1,
+                        sv.x1, sv.st1, w.dh, dy, w.dx1, same ? nullptr : w.df, gg, accumulate, w.gn1, fin, s));
+  }
   {
     Gemm g; g.dtype = dt; g.tag = "proj_dw";
-    g.A = sv.o; g.lda = z.A; g.a_kmajor = false; g.B = w.dx1; g.ldb = z.d; g.b_kmajor = false;
+    g.A = sv.o; g.lda = z.A; g.a_kmajor = false; g.B = df1; g.ldb = z.d; g.b_kmajor = false;
     g.C = gr->w_proj; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
     g.M = z.A; g.N = z.d; g.K = T;
+    const bool fused = ext.on && dw_bias(g, w.p_proj, gr->b_proj);
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    if (ext.on && !fused) {
+      ColJob j[1];
+      bias_job(j[0], df1, z.d, w.p_proj, gr->b_proj);
+      ORBIT_TRY(colsum_partials(dt, j, 1, T, s));
+      fin.add_job(j[0], T);
+    }
   }
   // attention sub-layer
   {
     Gemm g; g.dtype = dt; g.tag = "proj_dx";
-    g.A = w.dx1; g.lda = z.d; g.B = p->w_proj; g.ldb = z.d; g.b_kmajor = true;
+    g.A = df1; g.lda = z.d; g.B = p->w_proj; g.ldb = z.d; g.b_kmajor = true;
     g.C = w.dO; g.ldc = z.A; g.M = T; g.N = z.A; g.K = z.d;
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
@@ -417,9 +678,9 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   }
   char* dq = static_cast<char*>(w.dqkv);
   if (sv.o32)
-    ORBIT_TRY(attn_bwd(dt, io, sv.o32, z.A, 1, sv.lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
+    ORBIT_TRY(attn_bwd(dt, io, sv.o32, z.A, 1, lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
   else
-    ORBIT_TRY(attn_bwd(dt, io, sv.o, z.A, 0, sv.lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
+    ORBIT_TRY(attn_bwd(dt, io, sv.o, z.A, 0, lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
   if (z.qk) {
     ORBIT_TRY(qk_norm_bwd(dt, w.dqkv, 3 * z.A, sv.qkv, 3 * z.A, sv.qmu, sv.qr, p->qn_g, p->kn_g, gr->qn_g, gr->qn_b,
                           gr->kn_g, gr->kn_b, accumulate, T, z.H, z.dh, w.qws, &fin, s));
@@ -454,6 +715,10 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
   }
   return fin.run(accumulate, s);
 }
+
+}  // namespace
+
+extern "C" {
 
 // ---------------------------------------------------------------------------
 // patch embedding
@@ -1147,8 +1412,10 @@ orbit_status orbit_gated_norm_bwd(const orbit_gated_norm_desc* desc, const orbit
   REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes,
       need);
   const GnormGrads gg{g->gate, g->post_g, g->post_b, g->pre_g, g->pre_b};
-  return gnorm_bwd(z, gnorm_params(p), f, store, y, stats, z.pre ? dh : nullptr, dy, dx, df, gg, accumulate, ws,
-                   S(stream));
+  ColFinal fin;
+  ORBIT_TRY(gnorm_bwd(z, gnorm_params(p), f, store, y, stats, z.pre ? dh : nullptr, dy, dx, df, gg, accumulate, ws, fin,
+                      S(stream)));
+  return fin.run(accumulate, S(stream));
 }
 
 }  // extern "C"

@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     }
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
-      if (rv && on[c]) store8(static_cast<T*>(a.df) + base + col[c], wv[c]);
+      if (a.df && rv && on[c]) store8(static_cast<T*>(a.df) + base + col[c], wv[c]);
   }
   // the groups' sums, added in group order through LDS, then a partial row each
   __shared__ float comb[NCH == 2 ? 512 * 16 : 1];
@@ -432,7 +432,7 @@ size_t gnorm_bwd_ws_bytes(const GnormDims& z) {
 
 orbit_status gnorm_bwd(const GnormDims& z, const GnormParams& p, const void* f, const void* store, const void* y,
                        const float* stats, const void* dh, const void* dy, void* dx, void* df, const GnormGrads& g,
-                       int accumulate, void* ws, hipStream_t s) {
+                       int accumulate, void* ws, ColFinal& fin, hipStream_t s) {
   const int gates = std::max(1, z.gates);
   GnBwd a{};
   a.f = f; a.y = y; a.dh = dh; a.dy = dy; a.gate = z.gates ? p.gate : nullptr;
@@ -464,10 +464,8 @@ orbit_status gnorm_bwd(const GnormDims& z, const GnormParams& p, const void* f, 
     else ORBIT_TRY(launch(ki, gnorm_bwd_kernel<float, 2>, grid, block, 0, s, a));
   }
   if (z.pre) {
-    ColFinal fin;
     fin.add(a.part, z.n, chunks, z.n, g.pre_b);
     fin.add(a.part + (int64_t)chunks * z.n, z.n, chunks, z.n, g.pre_g);
-    ORBIT_TRY(fin.run(accumulate, s));
   }
   if (!rf) return ORBIT_OK;
   GnFinal b{};

@@ -4,11 +4,14 @@
 workspace, float32 gradients) that a pass needs, allocated with torch, and
 enqueues the entry points in order on the current stream:
 
-    full model : orbit_patch_embed -> orbit_var_aggregate -> orbit_vit_block_fwd x n
+    full model : orbit_patch_embed -> orbit_var_aggregate -> orbit_vit_block_ext_fwd x n
                  -> orbit_head_fwd -> orbit_mse_loss -> orbit_head_bwd
-                 -> orbit_vit_block_bwd x n -> orbit_var_aggregate_bwd -> orbit_patch_embed_bwd
-    block stack: orbit_vit_block_fwd x n -> orbit_vit_block_bwd x n (upstream gradient given)
+                 -> orbit_vit_block_ext_bwd x n -> orbit_var_aggregate_bwd -> orbit_patch_embed_bwd
+    block stack: orbit_vit_block_ext_fwd x n -> orbit_vit_block_ext_bwd x n (upstream gradient given)
     agg + stack: orbit_var_aggregate -> blocks -> blocks backward -> orbit_var_aggregate_bwd
+
+(the _ext calls are the plain block's, bit for bit, unless the dims ask for
+gates, norms or a scale of the residuals, or checkpoint is "act8")
 
 Only marshalling happens here; every step runs in the HIP library.
 """
@@ -19,7 +22,7 @@ from typing import Dict, List, Optional
 
 import torch
 
-from ._lib import (AggDesc, BlockDesc, EmbedDesc, HeadDesc, ORBIT_BF16, ORBIT_F32, OrbitLib, WmseDesc)
+from ._lib import (AggDesc, BlockDesc, BlockExt, EmbedDesc, HeadDesc, ORBIT_BF16, ORBIT_F32, OrbitLib, WmseDesc)
 
 
 @dataclasses.dataclass
@@ -43,6 +46,11 @@ class PassDims:
     patch: int = 4
     head_hidden: int = 0  # GELU layers of width d in the prediction head before its last linear map
     loss: str = "mse"     # "mse" or "wmse" (latitude-weighted, Sec. IV)
+    # residuals of the blocks: x + res_scale * gate * (LayerNorm of) the sub-layer's output, the gate a
+    # parameter [gate_rows, d] (0: none, 1: for every token, B: one row per sample)
+    post_norm: int = 0
+    gate_rows: int = 0
+    res_scale: float = 1.0
 
     @property
     def T(self):
@@ -65,10 +73,14 @@ class ViTPass:
     """Device state of one forward+backward pass (see module docstring)."""
 
     def __init__(self, lib: OrbitLib, dims: PassDims, params: Dict[str, object], device="cuda",
-                 checkpoint: bool = False):
-        """checkpoint: activation checkpointing of the blocks (Sec. III-B): the
-        forward keeps only each block's input and the backward recomputes the
-        rest (orbit_vit_block_bwd with saved = NULL)."""
+                 checkpoint=False):
+        """checkpoint: True for activation checkpointing of the blocks
+        (Sec. III-B): the forward keeps only each block's input and the backward
+        recomputes the rest (orbit_vit_block_bwd with saved = NULL). "act8": the
+        forward keeps the blocks' activations in 8 bits
+        (orbit_vit_block_ext_fwd with act8)."""
+        if checkpoint not in (False, True, "act8"):
+            raise ValueError(f"checkpoint must be False, True or 'act8', not {checkpoint!r}")
         self.lib, self.z, self.dev = lib, dims, torch.device(device)
         self.checkpoint = checkpoint
         z = dims
@@ -77,14 +89,15 @@ class ViTPass:
         code = _code(z.dtype)
         self.params = params
         self.bdesc = BlockDesc(z.B, z.L, z.d, z.heads, z.head_dim, z.mlp, z.qk_norm, z.eps, code)
-        ws = lib.orbit_vit_block_workspace_bytes(self.bdesc)
+        self.bext = BlockExt(int(checkpoint == "act8"), z.post_norm, z.gate_rows, z.res_scale)
+        ws = lib.orbit_vit_block_ext_workspace_bytes(self.bdesc, self.bext)
         if ws == 0:
             raise ValueError(f"invalid block description: {lib.last_error()}")
-        sb = lib.orbit_vit_block_saved_bytes(self.bdesc)
+        sb = lib.orbit_vit_block_ext_saved_bytes(self.bdesc, self.bext)
         E = lambda *shape, dt=tdt: torch.empty(*shape, dtype=dt, device=self.dev)
         F32 = lambda *shape: torch.zeros(*shape, dtype=torch.float32, device=self.dev)
         self.xs = [E(z.B, z.L, z.d) for _ in range(z.blocks + 1)]
-        self.saved = [None if checkpoint else torch.empty(sb, dtype=torch.uint8, device=self.dev)
+        self.saved = [None if checkpoint is True else torch.empty(sb, dtype=torch.uint8, device=self.dev)
                       for _ in range(z.blocks)]
         self.dxa = E(z.B, z.L, z.d)
         self.dxb = E(z.B, z.L, z.d)
@@ -147,7 +160,8 @@ class ViTPass:
             self.xs[0] = inputs["x"]
         mark("blocks_fwd")
         for i in range(z.blocks):
-            lib.orbit_vit_block_fwd(self.bdesc, P["blocks"][i], self.xs[i], self.xs[i + 1], self.saved[i], self.ws)
+            lib.orbit_vit_block_ext_fwd(self.bdesc, self.bext, P["blocks"][i], self.xs[i], self.xs[i + 1],
+                                        self.saved[i], self.ws)
         mark("blocks_fwd_end")
         if z.mode == "full":
             lib.orbit_head_fwd(self.hdesc, self.xs[-1], P["head"], self.pred, self.hsaved, self.ws)
@@ -164,8 +178,8 @@ class ViTPass:
         mark("blocks_bwd")
         for i in range(z.blocks - 1, -1, -1):
             dx = bufs[i % 2] if dy is not bufs[i % 2] else bufs[(i + 1) % 2]
-            lib.orbit_vit_block_bwd(self.bdesc, P["blocks"][i], self.xs[i], self.saved[i], dy, dx, G["blocks"][i],
-                                    accumulate, self.ws)
+            lib.orbit_vit_block_ext_bwd(self.bdesc, self.bext, P["blocks"][i], self.xs[i], self.saved[i], dy, dx,
+                                        G["blocks"][i], accumulate, self.ws)
             dy = dx
         mark("blocks_bwd_end")
         self.dx = dy

@@ -145,3 +145,122 @@ def gated_norm_grad_tol(z, p, f, y, dh, dy, half):
     elif z["gate_rows"]:
         tol["gate"] = abs(z["scale"]) * S * per_gate(size_t * f.abs())
     return half * t.abs() + K * size_t, half * df.abs() + K * w, tol
+
+
+# ---------------------------------------------------------------------------
+# transformer block with gated norms, and with saved tensors in 8 bits
+# ---------------------------------------------------------------------------
+def act8_values(t):
+    """The values a store of t (float64, last axis the columns) reads back as."""
+    return torch.from_numpy(act8_ref(t.reshape(-1, t.shape[-1]).numpy())[2]).reshape(t.shape)
+
+
+def _heads(t, H):
+    B, L, A = t.shape
+    return t.reshape(B, L, H, A // H).permute(0, 2, 1, 3)
+
+
+def _merge(t):
+    B, H, L, dh = t.shape
+    return t.permute(0, 2, 1, 3).reshape(B, L, H * dh)
+
+
+def block_ext_forward(x, p, H, z, qk=True, eps=1e-5):
+    """x [B, L, d] float64 -> y and what the backward reads (z as in gated_norm_ref)."""
+    B, L, d = x.shape
+    gn = lambda sub, pre, res, f: gated_norm_ref(
+        dict(z, rows=B * L, pre_norm=pre, eps=eps),
+        {"gate": p.get(f"gate{sub}"), "post_g": p.get(f"post{sub}_g"), "post_b": p.get(f"post{sub}_b"),
+         "pre_g": p["ln2_g"], "pre_b": p["ln2_b"]}, res.reshape(B * L, d), f.reshape(B * L, d))
+    c = {"h1": ln_ref(x, p["ln1_g"], p["ln1_b"], eps)}
+    c["qkv"] = c["h1"] @ p["w_qkv"] + p["b_qkv"]
+    q, k, v = (_heads(t, H) for t in c["qkv"].chunk(3, -1))
+    if qk:
+        q, k = ln_ref(q, p["qn_g"], p["qn_b"], eps), ln_ref(k, p["kn_g"], p["kn_b"], eps)
+    sc = q @ k.transpose(-1, -2).contiguous() / q.shape[-1] ** 0.5
+    c["lse"] = torch.logsumexp(sc, -1, keepdim=True)
+    c["o"] = _merge(torch.exp(sc - c["lse"]) @ v)
+    c["f1"] = c["o"] @ p["w_proj"] + p["b_proj"]
+    x1, h2 = gn(1, 1, x, c["f1"])
+    c["x1"], c["h2"] = x1.reshape(x.shape), h2.reshape(x.shape)
+    c["u"] = c["h2"] @ p["w_fc1"] + p["b_fc1"]
+    c["f2"] = gelu_ref(c["u"]) @ p["w_fc2"] + p["b_fc2"]
+    return gn(2, 0, c["x1"], c["f2"])[0].reshape(x.shape), c
+
+
+def block_ext_backward(x, p, H, z, c, dy, keep, qk=True, eps=1e-5):
+    """Gradients from the tensors `keep(t)` makes of the forward's (identity: the exact gradients;
+    act8_values: those of 8-bit stores). The softmax normalisers and f2's statistics are the forward's."""
+    B, L, d = x.shape
+    T = B * L
+    flat = lambda t: t.reshape(T, -1)
+    g = {}
+
+    def ln_back(t, gain, dh):
+        mu = t.mean(-1, keepdim=True)
+        r = 1.0 / torch.sqrt(((t - mu) ** 2).mean(-1, keepdim=True) + eps)
+        th, w = (t - mu) * r, dh * gain
+        n = t.shape[-1]
+        return (r * (w - w.mean(-1, keepdim=True) - th * (w * th).mean(-1, keepdim=True)),
+                (dh * th).reshape(-1, n).sum(0), dh.reshape(-1, n).sum(0))
+
+    def branch_back(sub, f, t, stats_of):
+        """gradient of f through scale gate (LN f): statistics taken from stats_of."""
+        gate = torch.ones(1, d, dtype=torch.float64)
+        if z["gate_rows"]:
+            gate = p[f"gate{sub}"]
+        G = gate.shape[0]
+        rows = gate.repeat_interleave(T // G, 0)
+        w = z["scale"] * rows * t
+        if not z["post_norm"]:
+            if z["gate_rows"]:
+                g[f"gate{sub}"] = z["scale"] * (t * f).reshape(G, -1, d).sum(1)
+            return w
+        mu = stats_of.mean(-1, keepdim=True)
+        r = 1.0 / torch.sqrt(((stats_of - mu) ** 2).mean(-1, keepdim=True) + eps)
+        fh = (f - mu) * r
+        g[f"post{sub}_g"], g[f"post{sub}_b"] = (w * fh).sum(0), w.sum(0)
+        if z["gate_rows"]:
+            g[f"gate{sub}"] = z["scale"] * (t * (fh * p[f"post{sub}_g"] + p[f"post{sub}_b"])).reshape(G, -1, d).sum(1)
+        w = w * p[f"post{sub}_g"]
+        return r * (w - w.mean(-1, keepdim=True) - fh * (w * fh).mean(-1, keepdim=True))
+
+    qkv, o, f1, u, f2 = (keep(c[k]) for k in ("qkv", "o", "f1", "u", "f2"))
+    # x1 and h2 as formed again from x and the kept f1
+    t1 = flat(f1)
+    if z["post_norm"]:
+        t1 = ln_ref(t1, p["post1_g"], p["post1_b"], eps)
+    if z["gate_rows"]:
+        t1 = t1 * p["gate1"].repeat_interleave(T // z["gate_rows"], 0)
+    x1 = flat(x) + z["scale"] * t1
+    h2 = ln_ref(x1, p["ln2_g"], p["ln2_b"], eps)
+    dyf = flat(dy)
+    df2 = branch_back(2, flat(f2), dyf, flat(c["f2"]))
+    ge, uf = gelu_ref(flat(u)), flat(u)
+    g["w_fc2"], g["b_fc2"] = ge.t() @ df2, df2.sum(0)
+    phi = torch.exp(-uf * uf / 2) / (2 * np.pi) ** 0.5
+    du = (df2 @ p["w_fc2"].t()) * (0.5 * torch.erfc(-uf / 2 ** 0.5) + uf * phi)
+    g["w_fc1"], g["b_fc1"] = h2.t() @ du, du.sum(0)
+    dx1, g["ln2_g"], g["ln2_b"] = ln_back(x1, p["ln2_g"], du @ p["w_fc1"].t())
+    dx1 = dx1 + dyf
+    df1 = branch_back(1, flat(f1), dx1, flat(f1))
+    g["w_proj"], g["b_proj"] = flat(o).t() @ df1, df1.sum(0)
+    dO = (df1 @ p["w_proj"].t()).reshape(B, L, -1)
+    q0, k0, v = (_heads(t, H) for t in qkv.chunk(3, -1))
+    q, k = q0, k0
+    if qk:
+        q, k = ln_ref(q0, p["qn_g"], p["qn_b"], eps), ln_ref(k0, p["kn_g"], p["kn_b"], eps)
+    dh = q.shape[-1]
+    P = torch.exp(q @ k.transpose(-1, -2).contiguous() / dh ** 0.5 - c["lse"])
+    dOh, oh = _heads(dO, H), _heads(o, H)
+    dS = P * (dOh @ v.transpose(-1, -2).contiguous() - (dOh * oh).sum(-1, keepdim=True)) / dh ** 0.5
+    dq, dk, dv = dS @ k, dS.transpose(-1, -2).contiguous() @ q, P.transpose(-1, -2).contiguous() @ dOh
+    for name in ("qn_g", "qn_b", "kn_g", "kn_b"):
+        g[name] = torch.zeros(dh, dtype=torch.float64)
+    if qk:
+        dq, g["qn_g"], g["qn_b"] = ln_back(q0, p["qn_g"], dq)
+        dk, g["kn_g"], g["kn_b"] = ln_back(k0, p["kn_g"], dk)
+    dqkv = flat(torch.cat([_merge(dq), _merge(dk), _merge(dv)], -1))
+    g["w_qkv"], g["b_qkv"] = flat(c["h1"]).t() @ dqkv, dqkv.sum(0)
+    dx, g["ln1_g"], g["ln1_b"] = ln_back(flat(x), p["ln1_g"], dqkv @ p["w_qkv"].t())
+    return (dx + dx1).reshape(x.shape), g

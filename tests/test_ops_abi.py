@@ -141,3 +141,89 @@ def test_gated_norm_reference_by_differences():
                           f + s * e * v if name == "f" else f)
         num = (value(*args(1)) - value(*args(-1))) / (2 * e)
         assert abs(num - float((grad * v).sum())) <= 1e-6 * max(1.0, abs(num)), name
+
+
+def _bdesc(**kw):
+    v = dict(B=2, L=20, d=64, heads=2, head_dim=32, mlp=128, qk_norm=1, eps=1e-5, dtype=1)
+    v.update(kw)
+    return L.BlockDesc(*[v[k] for k, _ in L.BlockDesc._fields_])
+
+
+def test_block_ext_sizes(lib):
+    """The plain form asks for what the plain calls ask for; 8-bit stores take under a quarter of the
+    bytes at the workloads' sizes."""
+    import synth
+    for c in synth.CONFIGS.values():
+        d = L.BlockDesc(c.B, c.L, c.d, c.heads, c.head_dim, c.mlp, c.qk_norm, c.eps, 1 if c.dtype == "bf16" else 0)
+        plain = L.BlockExt(0, 0, 0, 1.0)
+        full = lib.orbit_vit_block_saved_bytes(d)
+        assert lib.orbit_vit_block_ext_saved_bytes(d, plain) == full
+        assert lib.orbit_vit_block_ext_workspace_bytes(d, plain) == lib.orbit_vit_block_workspace_bytes(d)
+        small = lib.orbit_vit_block_ext_saved_bytes(d, L.BlockExt(1, 0, 0, 1.0))
+        assert 0 < small < full / 4, c.name
+        gated = L.BlockExt(1, 1, c.B, 0.5)
+        assert small < lib.orbit_vit_block_ext_saved_bytes(d, gated) < full / 3
+        assert lib.orbit_vit_block_ext_saved_bytes(d, L.BlockExt(0, 1, c.B, 0.5)) > full
+
+
+def test_block_ext_refusals(lib):
+    d = _bdesc()
+    for ext, what in (((2, 0, 0, 1.0), "act8"), ((0, 3, 0, 1.0), "post_norm"), ((0, 0, 3, 1.0), "gate_rows"),
+                      ((0, 0, -1, 1.0), "gate_rows")):
+        e = L.BlockExt(*ext)
+        assert lib.orbit_vit_block_ext_saved_bytes(d, e) == 0 and what in lib.last_error()
+        assert lib.orbit_vit_block_ext_workspace_bytes(d, e) == 0
+    assert lib.orbit_vit_block_ext_saved_bytes(_bdesc(d=60), L.BlockExt(1, 0, 0, 1.0)) == 0
+
+    def fwd(e, drop=(), ws_bytes=1 << 40, y=0x200):
+        p = L.BlockParams(*[0x1000 + 0x100 * i for i in range(16)])
+        ep = L.BlockExtParams(*[None if n in drop else 0x4000 + 0x100 * i for i, n in enumerate(L.BLOCK_EXT_PARAMS)])
+        return lib.lib.orbit_vit_block_ext_fwd(ctypes.byref(d), ctypes.byref(e) if e else None, ctypes.byref(p),
+                                               ctypes.byref(ep), 0x100, y, None, 0x300, ws_bytes, None)
+
+    def bwd(e, drop=(), ws_bytes=1 << 40):
+        p = L.BlockParams(*[0x1000 + 0x100 * i for i in range(16)])
+        ep = L.BlockExtParams(*[0x4000 + 0x100 * i for i in range(6)])
+        g = L.BlockGrads(*[0x5000 + 0x100 * i for i in range(16)])
+        eg = L.BlockExtGrads(*[None if n in drop else 0x7000 + 0x100 * i for i, n in enumerate(L.BLOCK_EXT_PARAMS)])
+        return lib.lib.orbit_vit_block_ext_bwd(ctypes.byref(d), ctypes.byref(e), ctypes.byref(p), ctypes.byref(ep), 0x100,
+                                               None, 0x200, 0x300, ctypes.byref(g), ctypes.byref(eg), 0, 0x400, ws_bytes,
+                                               None)
+
+    full = L.BlockExt(1, 1, 2, 0.5)
+    assert fwd(None) == L.ORBIT_E_ARG and "ext is NULL" in lib.last_error()
+    assert fwd(full, y=0x100) == L.ORBIT_E_ARG and "alias" in lib.last_error()
+    assert fwd(full, ws_bytes=64) == L.ORBIT_E_ARG and "workspace" in lib.last_error()
+    assert bwd(full, ws_bytes=64) == L.ORBIT_E_ARG and "workspace" in lib.last_error()
+    # the plain call's workspace is too small for the extended one
+    assert fwd(full, ws_bytes=lib.orbit_vit_block_workspace_bytes(d)) == L.ORBIT_E_ARG
+    for n in L.BLOCK_EXT_PARAMS:
+        assert fwd(full, drop=(n,)) == L.ORBIT_E_ARG and n in lib.last_error()
+        assert bwd(full, drop=(n,)) == L.ORBIT_E_ARG and f"grads.{n}" in lib.last_error()
+
+
+@pytest.mark.parametrize("post,gates", [(1, 2), (0, 1), (1, 0), (0, 0)])
+def test_block_ext_reference_by_autograd(post, gates):
+    """The written-out gradients equal autograd's of the forward when nothing is rounded."""
+    g = torch.Generator().manual_seed(6)
+    B, Lq, d, H, F = 2, 5, 16, 2, 24
+    rnd = lambda *s: 0.4 * torch.randn(*s, generator=g, dtype=torch.float64)
+    p = {"w_qkv": rnd(d, 3 * d), "b_qkv": rnd(3 * d), "w_proj": rnd(d, d), "b_proj": rnd(d), "w_fc1": rnd(d, F),
+         "b_fc1": rnd(F), "w_fc2": rnd(F, d), "b_fc2": rnd(d)}
+    for n, w in (("ln1", d), ("ln2", d), ("qn", d // H), ("kn", d // H), ("post1", d), ("post2", d)):
+        if post or not n.startswith("post"):
+            p.update({n + "_g": 1 + rnd(w), n + "_b": rnd(w)})
+    if gates:
+        p.update(gate1=rnd(gates, d), gate2=rnd(gates, d))
+    z = dict(n=d, gate_rows=gates, post_norm=post, scale=0.7)
+    x, dy = rnd(B, Lq, d), rnd(B, Lq, d)
+    leaf = {k: v.clone().requires_grad_(True) for k, v in p.items()}
+    xl = x.clone().requires_grad_(True)
+    y, _ = R.block_ext_forward(xl, leaf, H, z)
+    y.backward(dy)
+    _, c = R.block_ext_forward(x, p, H, z)
+    dx, gr = R.block_ext_backward(x, p, H, z, c, dy, lambda t: t)
+    assert torch.allclose(dx, xl.grad, rtol=1e-9, atol=1e-11)
+    assert set(gr) == set(p)
+    for k in p:
+        assert torch.allclose(gr[k], leaf[k].grad, rtol=1e-9, atol=1e-11), k
