@@ -588,7 +588,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     if (ext.gates) gg.gate = eg->gate2;
     if (ext.post) { gg.post_g = eg->post2_g; gg.post_b = eg->post2_b; }
     ORBIT_TRY(gnorm_bwd(block_gnorm(z, ext, false), block_gnorm_params(p, ep, 2), restore ? nullptr : sv.f2, s8.f2,
-                        nullptr, restore ? s8.st2 : sv.st2, nullptr, dy, nullptr, w.df, gg, accumulate, w.gn2, fin, s));
+                        nullptr, restore ? s8.st2 : sv.st2, nullptr, dy, nullptr, w.df, gg, accumulate, w.gn2, s));
     dff = w.df;
   }
   // feed-forward sub-layer
@@ -645,7 +645,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     const bool same = !ext.branch() && ext.scale == 1.f;
     if (!same) df1 = w.df;
     ORBIT_TRY(gnorm_bwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), restore ? nullptr : sv.f1, s8.f1,
-                        sv.x1, sv.st1, w.dh, dy, w.dx1, same ? nullptr : w.df, gg, accumulate, w.gn1, fin, s));
+                        sv.x1, sv.st1, w.dh, dy, w.dx1, same ? nullptr : w.df, gg, accumulate, w.gn1, s));
   }
   {
     Gemm g; g.dtype = dt; g.tag = "proj_dw";
@@ -1412,10 +1412,8 @@ orbit_status orbit_gated_norm_bwd(const orbit_gated_norm_desc* desc, const orbit
   REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes,
       need);
   const GnormGrads gg{g->gate, g->post_g, g->post_b, g->pre_g, g->pre_b};
-  ColFinal fin;
-  ORBIT_TRY(gnorm_bwd(z, gnorm_params(p), f, store, y, stats, z.pre ? dh : nullptr, dy, dx, df, gg, accumulate, ws, fin,
-                      S(stream)));
-  return fin.run(accumulate, S(stream));
+  return gnorm_bwd(z, gnorm_params(p), f, store, y, stats, z.pre ? dh : nullptr, dy, dx, df, gg, accumulate, ws,
+                   S(stream));
 }
 
 }  // extern "C"

@@ -26,8 +26,7 @@ orbit_status gnorm_fwd(const GnormDims& z, const GnormParams& p, const void* x, 
 
 // dh (null without the pre norm) and dy (null: zero) -> dx (may be null; the
 // gradient of x and of y's other readers together) and df (may be null without
-// the post norm and a gate), and the float32 parameter gradients, those of the
-// pre norm queued on `fin`. f == nullptr: from the store; neither is read without
+// the post norm and a gate), and the float32 parameter gradients. f == nullptr: from the store; neither is read without
 // the post norm and a gate. ws: gnorm_bwd_ws_bytes.
 size_t gnorm_bwd_ws_bytes(const GnormDims& z);
 struct GnormGrads {
@@ -35,6 +34,6 @@ struct GnormGrads {
 };
 orbit_status gnorm_bwd(const GnormDims& z, const GnormParams& p, const void* f, const void* store, const void* y,
                        const float* stats, const void* dh, const void* dy, void* dx, void* df, const GnormGrads& g,
-                       int accumulate, void* ws, ColFinal& fin, hipStream_t s);
+                       int accumulate, void* ws, hipStream_t s);
 
 }  // namespace orbit

@@ -2,9 +2,11 @@
 // in registers between the passes over it, so every tensor is read and written
 // once; statistics and parameter gradients are float32.
 #include <algorithm>
+#include <type_traits>
 
 #include "act8.h"
 #include "gnorm.h"
+#include "rowbuf.h"
 
 namespace orbit {
 namespace {
@@ -170,32 +172,70 @@ struct GnBwd {
   float scale;
 };
 
-template <typename T, int NCH>
-__global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
-  __shared__ float red[2][8][2];
-  const int tpr = a.tpr, G = (int)blockDim.x / tpr, wpg = tpr >> 6;
-  const int q = (int)threadIdx.x / tpr, t = (int)threadIdx.x % tpr;
+// 8 codes of a store and their group's E
+struct Raw8Q {
+  u32v2 q;
+  uint32_t e;
+  ORBIT_DEV void renew() { asm volatile("" : "+v"(q)); }
+  ORBIT_DEV void get4(int h, float* f) const { act8_decode4(q[h], e, f); }
+};
+
+// a thread's part of one row, as loaded
+template <typename T, int NCH, bool F8>
+struct GnRow {
+  int64_t r;
+  bool rv;
+  float4 st;
+  Raw8<T> dh[NCH], y[NCH], dy[NCH];
+  std::conditional_t<F8, Raw8Q, Raw8<T>> f[NCH];
+};
+
+// The block's G = blockDim / tpr groups of tpr threads take the chunk's rows in
+// turn (above 512 threads there is one group); thread t of a group owns the NCH
+// 8-column pieces t + c tpr. Every group runs the same number of rows, so the
+// barriers line up. The four column sums of a thread's pieces would take half of
+// the register file at full width; the two of the pre norm live in LDS, which
+// leaves 128 registers per thread enough (16 waves per CU). The next row's
+// loads are issued into the registers of the current one as soon as these are
+// used up: dh, y and dy before the second row reduction, f after it. KEEP:
+// values stay in registers from their one load; float32 rows of 1024 threads
+// are loaded again where they are used instead.
+template <typename T, int NCH, int NT, bool F8, bool KEEP, int WPE>
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) gnorm_bwd_kernel(GnBwd a) {
+  using Row = GnRow<T, NCH, F8>;
+  constexpr bool ONE = NT > 512;
+  constexpr int PIECES = NT * NCH;
+  __shared__ float red[2][NT / 64][2];
+  // column sums: half h of piece p of sum k at (2 k + h) PIECES + p, so that
+  // consecutive lanes touch consecutive 16 bytes
+  extern __shared__ __attribute__((aligned(16))) f32x4 sums[];
+  const int tpr = ONE ? (int)blockDim.x : a.tpr, G = ONE ? 1 : (int)blockDim.x / tpr, wpg = tpr >> 6;
+  // a group is whole waves: its number, and with it the row and its statistics,
+  // are scalars
+  const int q = ONE ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / tpr);
+  const int t = (int)threadIdx.x - q * tpr;
   const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
-  const int n = a.n, chunks = (int)gridDim.x;
+  const int n = a.n, chunks = (int)gridDim.x, row_bytes = n * (int)sizeof(T);
   const int gi = (int)blockIdx.x / a.cpg, ci = (int)blockIdx.x % a.cpg;
   const int r0 = gi * a.rpg + ci * a.rpb, r1 = min((gi + 1) * a.rpg, r0 + a.rpb);
-  const T* gate = static_cast<const T*>(a.gate);
-  if (gate) gate += (int64_t)gi * n;
-  const bool rf_ = a.post || gate;  // f is read
-  int col[NCH];
-  bool on[NCH];
+  const bool post = a.post, pre = a.pre, rf = post || a.gate;  // rf: f is read
+  // an absent gain or gate is 1: its zeros or-ed with the bits of 1
+  const RowBuf pre_g(a.pre_g, 0, pre ? row_bytes : 0), post_g(a.post_g, 0, post ? row_bytes : 0);
+  const RowBuf gate(a.gate, a.gate ? (int64_t)gi * row_bytes : 0, a.gate ? row_bytes : 0);
+  const uint32_t gate_or = a.gate ? 0u : one_bits<T>(), post_or = post ? 0u : one_bits<T>();
+  uint32_t col[NCH];
+  f32x4* const mine = sums + q * tpr * NCH + t;
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
-    col[c] = 8 * (t + c * tpr);
-    on[c] = col[c] < n;
+    col[c] = 8u * (uint32_t)(t + c * tpr);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mine[k * PIECES + c * tpr] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  float s[4][NCH][8];
+  f32x4 s2[NCH][2], s3[NCH][2];  // column sums of t and t fh
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int c = 0; c < NCH; ++c)
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[k][c][i] = 0.f;
+    for (int h = 0; h < 2; ++h) s2[c][h] = s3[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float inv_n = 1.f / (float)n;
   // sums of two values over the row's threads; every thread of the block calls
   auto row_sum2 = [&](int k, float& u, float& v) {
@@ -214,178 +254,291 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
       }
     }
   };
+  // Lanes past the row and rows past the chunk read zeros, an absent pre norm a
+  // zero dh, an absent post norm f itself (mean 0, 1 / deviation 1): the
+  // arithmetic has no branches on these.
   const int steps = (a.rpb + G - 1) / G;
-  for (int it = 0; it < steps; ++it) {
-    const int64_t r = r0 + q + (int64_t)it * G;
-    const bool rv = r < r1;
-    const int64_t base = r * n;
-    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (rv) st = *reinterpret_cast<const float4*>(a.stats + 4 * r);
-    float tv[NCH][8], fv[NCH][8], wv[NCH][8];
-    float s1 = 0.f, s2 = 0.f;
+  auto fetch_row = [&](int it, Row& R) {
+    R.r = r0 + q + (int64_t)it * G;
+    R.rv = it < steps && R.r < r1;
+    R.st = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (R.rv) R.st = *reinterpret_cast<const float4*>(a.stats + 4 * R.r);
+    if (!post) R.st.x = 0.f, R.st.y = 1.f;
+    if (!pre) R.st.z = R.st.w = 0.f;
+  };
+  auto row = [&](const void* v, const Row& R, bool on) {
+    return RowBuf(v, R.r * row_bytes, on && R.rv ? row_bytes : 0);
+  };
+  auto fetch_h = [&](Row& R) {  // what the pre norm needs
+    const RowBuf bh = row(a.dh, R, pre), by = row(a.y, R, pre);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) tv[c][i] = fv[c][i] = wv[c][i] = 0.f;
-      if (!(rv && on[c])) continue;
-      if (a.dy) load8(static_cast<const T*>(a.dy) + base + col[c], tv[c]);
-      if (rf_) {
-        if (a.f) load8(static_cast<const T*>(a.f) + base + col[c], fv[c]);
-        else act8_decode(*reinterpret_cast<const uint2*>(a.fc + base + col[c]),
-                         a.fe[r * a.groups + (col[c] >> 5)], fv[c]);
-      }
-      if (a.pre) {
-        float yv[8], g8[8];
-        load8(static_cast<const T*>(a.dh) + base + col[c], wv[c]);
-        load8(static_cast<const T*>(a.y) + base + col[c], yv);
-        load8(static_cast<const T*>(a.pre_g) + col[c], g8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float yh = (yv[i] - st.z) * st.w;
-          s[0][c][i] += wv[c][i];
-          s[1][c][i] += wv[c][i] * yh;
-          wv[c][i] *= g8[i];
-          s1 += wv[c][i];
-          s2 += wv[c][i] * yh;
-        }
-      }
+      R.dh[c].load(bh, col[c] * (uint32_t)sizeof(T));
+      R.y[c].load(by, col[c] * (uint32_t)sizeof(T));
     }
-    if (a.pre) {
-      row_sum2(0, s1, s2);
-      const float m1 = s1 * inv_n, m2 = s2 * inv_n;
+  };
+  auto fetch_d = [&](Row& R) {
+    const RowBuf b = row(a.dy, R, a.dy != nullptr);
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) R.dy[c].load(b, col[c] * (uint32_t)sizeof(T));
+  };
+  auto fetch_f = [&](Row& R) {
+    if constexpr (F8) {
+      const bool v = rf && R.rv;
+      const RowBuf bq(a.fc, R.r * n, v ? n : 0), be(a.fe, R.r * a.groups, v ? a.groups : 0);
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
-        if (!(rv && on[c])) continue;
-        float yv[8];
-        load8(static_cast<const T*>(a.y) + base + col[c], yv);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) tv[c][i] += st.w * (wv[c][i] - m1 - (yv[i] - st.z) * st.w * m2);
+        R.f[c].q = __builtin_amdgcn_raw_buffer_load_b64(bq.r, col[c], 0, 0);
+        // where nothing is read: any E but 0, which stands for NaN
+        R.f[c].e = __builtin_amdgcn_raw_buffer_load_b8(be.r, col[c] >> 5, 0, 0) | (v && col[c] < (uint32_t)n ? 0u : 7u);
       }
+    } else {
+      const RowBuf b = row(a.f, R, rf);
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) R.f[c].load(b, col[c] * (uint32_t)sizeof(T));
     }
-    float s3 = 0.f, s4 = 0.f;
+  };
+  Row cur;
+  fetch_row(0, cur);
+  if (KEEP) {
+    fetch_h(cur);
+    fetch_d(cur);
+    fetch_f(cur);
+  }
+  for (int it = 0; it < steps; ++it) {
+    // yh = y ry - my ry, fh = f rf - mf rf
+    const float ry = cur.st.w, oy = -cur.st.z * ry, rr = cur.st.y, of = -cur.st.x * rr;
+    float m1 = 0.f, m2 = 0.f;
+    if (pre) {
+      if (!KEEP) fetch_h(cur);
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      if (!(rv && on[c])) continue;
-      if (a.dx) store8(static_cast<T*>(a.dx) + base + col[c], tv[c]);
-      float w[8];
+      for (int c = 0; c < NCH; ++c) {
+        Raw8<T> g;
+        g.load(pre_g, col[c] * (uint32_t)sizeof(T));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (a.post) fv[c][i] = (fv[c][i] - st.x) * st.y;
-        s[2][c][i] += tv[c][i];
-        s[3][c][i] += tv[c][i] * fv[c][i];
-        wv[c][i] = a.scale * tv[c][i];
-      }
-      if (gate) {
-        load8(gate + col[c], w);
+        for (int h = 0; h < 2; ++h) {
+          float d4[4], y4[4], g4[4];
+          cur.dh[c].get4(h, d4);
+          cur.y[c].get4(h, y4);
+          g.get4(h, g4);
+          f32x4 u = mine[h * PIECES + c * tpr], v = mine[(2 + h) * PIECES + c * tpr];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) wv[c][i] *= w[i];
-      }
-      if (a.post) {
-        load8(static_cast<const T*>(a.post_g) + col[c], w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          wv[c][i] *= w[i];
-          s3 += wv[c][i];
-          s4 += wv[c][i] * fv[c][i];
+          for (int i = 0; i < 4; ++i) {
+            const float yh = fmaf(y4[i], ry, oy), w = d4[i] * g4[i];
+            u[i] += d4[i];
+            v[i] = fmaf(d4[i], yh, v[i]);
+            m1 += w;
+            m2 = fmaf(w, yh, m2);
+          }
+          mine[h * PIECES + c * tpr] = u;
+          mine[(2 + h) * PIECES + c * tpr] = v;
+        }
+        if (KEEP) {
+          cur.dh[c].renew();
+          cur.y[c].renew();
         }
       }
+      row_sum2(0, m1, m2);
+      m1 *= inv_n;
+      m2 *= inv_n;
     }
-    if (a.post) {
-      row_sum2(1, s3, s4);
-      const float m3 = s3 * inv_n, m4 = s4 * inv_n;
+    if (!KEEP) {
+      fetch_h(cur);
+      fetch_d(cur);
+      fetch_f(cur);
+    }
+    float w[NCH][8];
+    float m3 = 0.f, m4 = 0.f;
+    const RowBuf bx = row(a.dx, cur, a.dx != nullptr), bf = row(a.df, cur, a.df != nullptr);
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
+    for (int c = 0; c < NCH; ++c) {
+      Raw8<T> g, gg, pg, o;
+      g.load(pre_g, col[c] * (uint32_t)sizeof(T));
+      gg.load(gate, col[c] * (uint32_t)sizeof(T));
+      pg.load(post_g, col[c] * (uint32_t)sizeof(T));
+      gg.or_bits(gate_or);
+      pg.or_bits(post_or);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) wv[c][i] = st.y * (wv[c][i] - m3 - fv[c][i] * m4);
+      for (int h = 0; h < 2; ++h) {
+        float t4[4], d4[4], v4[4], f4[4];
+        cur.dy[c].get4(h, t4);
+        cur.dh[c].get4(h, d4);
+        cur.y[c].get4(h, f4);
+        g.get4(h, v4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          t4[i] = fmaf(ry, fmaf(-m2, fmaf(f4[i], ry, oy), fmaf(d4[i], v4[i], -m1)), t4[i]);
+        o.put4(h, t4);
+        cur.f[c].get4(h, f4);
+        gg.get4(h, v4);
+        pg.get4(h, d4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f4[i] = fmaf(f4[i], rr, of);
+          s2[c][h][i] += t4[i];
+          s3[c][h][i] = fmaf(t4[i], f4[i], s3[c][h][i]);
+          t4[i] *= a.scale * v4[i] * d4[i];
+          m3 += t4[i];
+          m4 = fmaf(t4[i], f4[i], m4);
+          w[c][4 * h + i] = t4[i];
+        }
+      }
+      o.store(bx, col[c] * (uint32_t)sizeof(T));
+    }
+    Row nxt;
+    fetch_row(it + 1, nxt);
+    if (KEEP) {
+      fetch_h(nxt);
+      fetch_d(nxt);
+    }
+    if (post) {
+      row_sum2(1, m3, m4);
+      m3 *= inv_n;
+      m4 *= inv_n;
+      if (!KEEP) fetch_f(cur);
     }
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
-      if (a.df && rv && on[c]) store8(static_cast<T*>(a.df) + base + col[c], wv[c]);
+    for (int c = 0; c < NCH; ++c) {
+      Raw8<T> o;
+      if (KEEP) cur.f[c].renew();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float t4[4], f4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t4[i] = w[c][4 * h + i];
+        if (post) {
+          cur.f[c].get4(h, f4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t4[i] = rr * fmaf(-m4, fmaf(f4[i], rr, of), t4[i] - m3);
+        }
+        o.put4(h, t4);
+      }
+      o.store(bf, col[c] * (uint32_t)sizeof(T));
+    }
+    if (KEEP) fetch_f(nxt);
+    cur = nxt;
   }
-  // the groups' sums, added in group order through LDS, then a partial row each
-  __shared__ float comb[NCH == 2 ? 512 * 16 : 1];
+  // the groups' sums of a column, added in group order by all threads, then a
+  // partial row each: the pre norm's, already in LDS, then the others
+  auto put = [&](int k) {  // sums k and k + 1
+    __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (k < 2 ? !a.pre : !rf_) continue;
-    if (NCH == 2 && G > 1) {
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < NCH; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) comb[threadIdx.x * 16 + c * 8 + i] = s[k][c][i];
-      __syncthreads();
-      if (q == 0)
-        for (int gq = 1; gq < G; ++gq)
-#pragma unroll
-          for (int c = 0; c < NCH; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[k][c][i] += comb[(gq * tpr + t) * 16 + c * 8 + i];
+    for (int j = 0; j < 2; ++j) {
+      float* out = a.part + ((int64_t)(k + j) * chunks + blockIdx.x) * n;
+      const f32x4* src = sums + 2 * j * PIECES;
+      for (int e = (int)threadIdx.x; 4 * e < n; e += (int)blockDim.x) {
+        const int p = e >> 1, h = e & 1;
+        f32x4 v = src[h * PIECES + p];
+        for (int gq = 1; gq < G; ++gq) v += src[h * PIECES + gq * tpr * NCH + p];
+        *reinterpret_cast<f32x4*>(out + 4 * e) = v;
+      }
     }
-    if (q != 0) continue;
+  };
+  if (pre) put(0);
+  if (!rf) return;
+  __syncthreads();
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
-      if (on[c]) store8(a.part + ((int64_t)k * chunks + blockIdx.x) * n + col[c], s[k][c]);
-  }
+  for (int c = 0; c < NCH; ++c)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      mine[h * PIECES + c * tpr] = s2[c][h];
+      mine[(2 + h) * PIECES + c * tpr] = s3[c][h];
+    }
+  put(2);
 }
 
 struct GnFinal {
-  const float *p1, *p2;  // partials of S1 and S2 [gates * cpg][n]
+  const float* part;  // as GnBwd's
   const void *gate, *post_g, *post_b;
-  float *dgate, *dpost_g, *dpost_b;
-  int n, gates, cpg, post, accumulate;
+  float *dgate, *dpost_g, *dpost_b, *dpre_g, *dpre_b;
+  int n, gates, cpg, pre, post, lanes, accumulate;
   float scale;
 };
 
-// 16 columns x 16 chunk lanes per block; the lanes' sums are added in order
+// Sums of the partial rows: 32 columns x 32 chunk lanes per block, a lane
+// adding every 32nd chunk, the lanes' sums added in order. blockIdx.y 0 and 1:
+// the pre norm's shift and gain; 2 and 3: the post norm's, each chunk weighted
+// by its gate; from 4 on the gate, `lanes` lanes to a gate row.
 template <typename T>
-__global__ void __launch_bounds__(256) gnorm_final_kernel(GnFinal a) {
-  __shared__ float red[2][16][17];
-  const int e = threadIdx.x % 16, q = threadIdx.x / 16;
-  const int64_t c = (int64_t)blockIdx.x * 16 + e;
+__global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
+  __shared__ float red[2][32][33];
+  const int e = threadIdx.x % 32, q = threadIdx.x / 32;
+  const int64_t c = (int64_t)blockIdx.x * 32 + e;
+  const int job = (int)blockIdx.y;
   const bool on = c < a.n;
-  const float pg = on && a.post ? to_f(static_cast<const T*>(a.post_g)[c]) : 1.f;
-  const float pb = on && a.post ? to_f(static_cast<const T*>(a.post_b)[c]) : 0.f;
-  float dg = 0.f, db = 0.f;
-  for (int g = 0; g < a.gates; ++g) {
-    float s1 = 0.f, s2 = 0.f;
+  const int chunks = a.gates * a.cpg;
+  const T* gate = static_cast<const T*>(a.gate);
+  if (job < 2 ? !a.pre : job < 4 && !a.post) return;
+  if (job < 4) {
+    const float* p = a.part + (int64_t)job * chunks * a.n + c;
+    float s = 0.f;
     if (on) {
-      for (int k = q; k < a.cpg; k += 16) {
-        const int64_t at = ((int64_t)g * a.cpg + k) * a.n + c;
-        if (a.post) s1 += a.p1[at];
-        s2 += a.p2[at];
+      if (job < 2 || !gate) {
+#pragma unroll 8
+        for (int k = q; k < chunks; k += 32) s += p[(int64_t)k * a.n];
+      } else {
+#pragma unroll 8
+        for (int k = q; k < chunks; k += 32) s = fmaf(to_f(gate[(int64_t)(k / a.cpg) * a.n + c]), p[(int64_t)k * a.n], s);
       }
     }
+    red[0][q][e] = s;
     __syncthreads();
-    red[0][q][e] = s1;
-    red[1][q][e] = s2;
-    __syncthreads();
-    if (q == 0 && on) {
-      s1 = s2 = 0.f;
+    if (q != 0 || !on) return;
+    s = 0.f;
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        s1 += red[0][k][e];
-        s2 += red[1][k][e];
-      }
-      const float gt = a.gate ? to_f(static_cast<const T*>(a.gate)[(int64_t)g * a.n + c]) : 1.f;
-      dg += gt * s2;
-      db += gt * s1;
-      if (a.gate) {
-        const float v = a.scale * (pg * s2 + pb * s1);
-        float* o = a.dgate + (int64_t)g * a.n + c;
-        *o = a.accumulate ? *o + v : v;
-      }
+    for (int k = 0; k < 32; ++k) s += red[0][k][e];
+    if (job >= 2) s *= a.scale;
+    float* o = (job == 0 ? a.dpre_b : job == 1 ? a.dpre_g : job == 2 ? a.dpost_b : a.dpost_g) + c;
+    *o = a.accumulate ? *o + s : s;
+    return;
+  }
+  const int per = 32 / a.lanes, ql = q % a.lanes;
+  const int64_t g = (int64_t)(job - 4) * per + q / a.lanes;
+  float s1 = 0.f, s2 = 0.f;
+  if (on && g < a.gates) {
+    const float* p2 = a.part + ((int64_t)3 * chunks + g * a.cpg) * a.n + c;
+    const float* p1 = p2 - (int64_t)chunks * a.n;
+#pragma unroll 4
+    for (int k = ql; k < a.cpg; k += a.lanes) {
+      s2 += p2[(int64_t)k * a.n];
+      if (a.post) s1 += p1[(int64_t)k * a.n];
     }
   }
-  if (q == 0 && on && a.post) {
-    a.dpost_g[c] = a.accumulate ? a.dpost_g[c] + a.scale * dg : a.scale * dg;
-    a.dpost_b[c] = a.accumulate ? a.dpost_b[c] + a.scale * db : a.scale * db;
+  red[0][q][e] = s1;
+  red[1][q][e] = s2;
+  __syncthreads();
+  if (ql != 0 || !on || g >= a.gates) return;
+  for (int k = 1; k < a.lanes; ++k) {
+    s1 += red[0][q + k][e];
+    s2 += red[1][q + k][e];
   }
+  float v = s2;
+  if (a.post)
+    v = to_f(static_cast<const T*>(a.post_g)[c]) * s2 + to_f(static_cast<const T*>(a.post_b)[c]) * s1;
+  v *= a.scale;
+  float* o = a.dgate + g * a.n + c;
+  *o = a.accumulate ? *o + v : v;
 }
 
-// rows per chunk of the backward: 16, or 8 where 16-row chunks leave CUs idle
-int gn_rpb(const GnormDims& z) { return cdiv(z.rows, 16) >= 256 ? 16 : 8; }
-int gn_rpg(const GnormDims& z) { return z.rows / std::max(1, z.gates); }
-int gn_cpg(const GnormDims& z) { return (int)cdiv(gn_rpg(z), gn_rpb(z)); }
+// The backward's launch shape. A thread owns one or two pieces (two from 513
+// columns on, where a row then fills a wave), a block 512 threads, 1024 above
+// 8192 columns. Chunks: about one per CU, whole turns of the block's groups.
+struct GnShape {
+  int nch, nt, tpr, G, rpg, rpb, cpg;
+};
+GnShape gn_shape(const GnormDims& z) {
+  GnShape h{};
+  h.nch = z.n <= 512 ? 1 : 2;
+  h.nt = z.n <= 8192 ? 512 : 1024;
+  h.tpr = (int)(cdiv(cdiv(z.n, 8 * h.nch), 64) * 64);
+  h.G = h.nt / h.tpr;
+  h.rpg = z.rows / std::max(1, z.gates);
+  const int turns = std::max<int>({1, (8 + h.G - 1) / h.G, (z.rows + 128 * h.G) / (256 * h.G)});
+  h.rpb = std::min(h.rpg, turns * h.G);
+  h.G = std::min(h.G, h.rpb);
+  h.cpg = (int)cdiv(h.rpg, h.rpb);
+  return h;
+}
 
 template <typename T>
 orbit_status gnorm_fwd_t(const GnFwd& a, const KernelInfo& ki, hipStream_t s) {
@@ -416,7 +569,7 @@ orbit_status gnorm_fwd(const GnormDims& z, const GnormParams& p, const void* x, 
     if (f) { a.qc = codes; a.qe = exps; }
     else { a.fc = codes; a.fe = exps; }
   }
-  a.rows = z.rows; a.n = z.n; a.groups = act8_groups(z.n); a.rpg = gn_rpg(z);
+  a.rows = z.rows; a.n = z.n; a.groups = act8_groups(z.n); a.rpg = z.rows / std::max(1, z.gates);
   a.post = z.post; a.pre = z.pre; a.scale = z.scale; a.eps = z.eps;
   const double e = z.dt == ORBIT_BF16 ? 2.0 : 4.0, q = 1.0 + 1.0 / kAct8Group;
   const double rn = (double)z.rows * z.n;
@@ -427,57 +580,80 @@ orbit_status gnorm_fwd(const GnormDims& z, const GnormParams& p, const void* x, 
 }
 
 size_t gnorm_bwd_ws_bytes(const GnormDims& z) {
-  return align_up((size_t)4 * std::max(1, z.gates) * gn_cpg(z) * (size_t)z.n * sizeof(float));
+  return align_up((size_t)4 * std::max(1, z.gates) * gn_shape(z).cpg * (size_t)z.n * sizeof(float));
 }
+
+namespace {
+
+template <typename T, int NCH, int NT, bool F8>
+orbit_status gnorm_bwd_run(const GnBwd& a, const KernelInfo& ki, int chunks, int threads, hipStream_t s) {
+  // bf16: 16 waves per CU; float32 values take twice the registers
+  constexpr bool KEEP = sizeof(T) == 2 || NT == 512;
+  constexpr int WPE = sizeof(T) == 2 || NT == 1024 ? 4 : 2;
+  const auto kern = gnorm_bwd_kernel<T, NCH, NT, F8, KEEP, WPE>;
+  static const bool once = [&] {
+    // lift the default dynamic-LDS cap (a failure surfaces as a launch error)
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                              NT * NCH * 64);
+    (void)hipGetLastError();
+    return true;
+  }();
+  (void)once;
+  return launch(ki, kern, dim3((unsigned)chunks), dim3((unsigned)threads), (size_t)NT * NCH * 64, s, a);
+}
+
+template <typename T, bool F8>
+orbit_status gnorm_bwd_t(const GnBwd& a, const GnShape& h, const KernelInfo& ki, int chunks, hipStream_t s) {
+  const int threads = h.G * h.tpr;
+  if (h.nt == 1024) return gnorm_bwd_run<T, 2, 1024, F8>(a, ki, chunks, threads, s);
+  if (h.nch == 2) return gnorm_bwd_run<T, 2, 512, F8>(a, ki, chunks, threads, s);
+  return gnorm_bwd_run<T, 1, 512, F8>(a, ki, chunks, threads, s);
+}
+
+}  // namespace
 
 orbit_status gnorm_bwd(const GnormDims& z, const GnormParams& p, const void* f, const void* store, const void* y,
                        const float* stats, const void* dh, const void* dy, void* dx, void* df, const GnormGrads& g,
-                       int accumulate, void* ws, ColFinal& fin, hipStream_t s) {
+                       int accumulate, void* ws, hipStream_t s) {
   const int gates = std::max(1, z.gates);
+  const GnShape h = gn_shape(z);
   GnBwd a{};
   a.f = f; a.y = y; a.dh = dh; a.dy = dy; a.gate = z.gates ? p.gate : nullptr;
-  a.post_g = p.post_g; a.pre_g = p.pre_g; a.dx = dx; a.df = df; a.stats = stats;
+  a.post_g = z.post ? p.post_g : nullptr; a.pre_g = z.pre ? p.pre_g : nullptr; a.dx = dx; a.df = df; a.stats = stats;
   if (!f && store) {
     a.fc = static_cast<const uint8_t*>(store);
     a.fe = a.fc + act8_exp_offset(z.rows, z.n);
   }
   a.part = static_cast<float*>(ws);
   a.rows = z.rows; a.n = z.n; a.groups = act8_groups(z.n);
-  a.rpg = gn_rpg(z); a.rpb = gn_rpb(z); a.cpg = gn_cpg(z);
+  a.rpg = h.rpg; a.rpb = h.rpb; a.cpg = h.cpg; a.tpr = h.tpr;
   a.post = z.post; a.pre = z.pre; a.scale = z.scale;
-  const int nch = z.n <= 8192 ? 2 : 4;
-  a.tpr = (int)(cdiv(cdiv(z.n, 8 * nch), 64) * 64);
-  const int chunks = gates * a.cpg;
-  const dim3 grid((unsigned)chunks), block((unsigned)(512 / a.tpr * a.tpr));
+  const int chunks = gates * h.cpg;
   const bool rf = z.post || z.gates;
   const double e = z.dt == ORBIT_BF16 ? 2.0 : 4.0, rn = (double)z.rows * z.n;
   KernelInfo ki{z.dt == ORBIT_BF16 ? "gnorm_bwd<bf16>" : "gnorm_bwd<f32>", 30.0 * rn,
-                rn * (e * (1 + 2 * z.pre + (dy ? 1 : 0) + (dx ? 1 : 0) + (rf && f ? 1 : 0)) +
+                rn * (e * (2 * z.pre + (df ? 1 : 0) + (dy ? 1 : 0) + (dx ? 1 : 0) + (rf && f ? 1 : 0)) +
                       (rf && !f ? 1.0 + 1.0 / kAct8Group : 0.0)) +
                     4.0 * chunks * z.n * (2 * z.pre + 2 * rf)};
-  const bool wide = nch == 4;
   if (z.dt == ORBIT_BF16) {
-    if (wide) ORBIT_TRY(launch(ki, gnorm_bwd_kernel<bf16, 4>, grid, block, 0, s, a));
-    else ORBIT_TRY(launch(ki, gnorm_bwd_kernel<bf16, 2>, grid, block, 0, s, a));
+    if (a.fc) ORBIT_TRY((gnorm_bwd_t<bf16, true>(a, h, ki, chunks, s)));
+    else ORBIT_TRY((gnorm_bwd_t<bf16, false>(a, h, ki, chunks, s)));
   } else {
-    if (wide) ORBIT_TRY(launch(ki, gnorm_bwd_kernel<float, 4>, grid, block, 0, s, a));
-    else ORBIT_TRY(launch(ki, gnorm_bwd_kernel<float, 2>, grid, block, 0, s, a));
+    if (a.fc) ORBIT_TRY((gnorm_bwd_t<float, true>(a, h, ki, chunks, s)));
+    else ORBIT_TRY((gnorm_bwd_t<float, false>(a, h, ki, chunks, s)));
   }
-  if (z.pre) {
-    fin.add(a.part, z.n, chunks, z.n, g.pre_b);
-    fin.add(a.part + (int64_t)chunks * z.n, z.n, chunks, z.n, g.pre_g);
-  }
-  if (!rf) return ORBIT_OK;
+  if (!z.pre && !rf) return ORBIT_OK;
   GnFinal b{};
-  b.p1 = a.part + (int64_t)2 * chunks * z.n;
-  b.p2 = a.part + (int64_t)3 * chunks * z.n;
+  b.part = a.part;
   b.gate = a.gate; b.post_g = p.post_g; b.post_b = p.post_b;
-  b.dgate = g.gate; b.dpost_g = g.post_g; b.dpost_b = g.post_b;
-  b.n = z.n; b.gates = gates; b.cpg = a.cpg; b.post = z.post; b.accumulate = accumulate; b.scale = z.scale;
-  KernelInfo kf{"gnorm_final", 0.0, 8.0 * chunks * z.n};
-  const dim3 fgrid((unsigned)cdiv(z.n, 16));
-  if (z.dt == ORBIT_BF16) return launch(kf, gnorm_final_kernel<bf16>, fgrid, dim3(256), 0, s, b);
-  return launch(kf, gnorm_final_kernel<float>, fgrid, dim3(256), 0, s, b);
+  b.dgate = g.gate; b.dpost_g = g.post_g; b.dpost_b = g.post_b; b.dpre_g = g.pre_g; b.dpre_b = g.pre_b;
+  b.n = z.n; b.gates = gates; b.cpg = h.cpg; b.pre = z.pre; b.post = z.post;
+  b.accumulate = accumulate; b.scale = z.scale;
+  b.lanes = std::min(32, pow2_ceil(h.cpg));
+  KernelInfo kf{"gnorm_final", 0.0, 4.0 * chunks * z.n * (2 * z.pre + 2 * rf)};
+  const dim3 fgrid((unsigned)cdiv(z.n, 32), (unsigned)(z.gates ? 4 + cdiv(z.gates, 32 / b.lanes) : z.post ? 4 : 2));
+  if (z.dt == ORBIT_BF16) return launch(kf, gnorm_final_kernel<bf16>, fgrid, dim3(1024), 0, s, b);
+  return launch(kf, gnorm_final_kernel<float>, fgrid, dim3(1024), 0, s, b);
 }
 
 }  // namespace orbit
