@@ -190,29 +190,30 @@ struct GnRow {
   std::conditional_t<F8, Raw8Q, Raw8<T>> f[NCH];
 };
 
-// The block's G = blockDim / tpr groups of tpr threads take the chunk's rows in
-// turn (above 512 threads there is one group); thread t of a group owns the NCH
-// 8-column pieces t + c tpr. Every group runs the same number of rows, so the
-// barriers line up. The four column sums of a thread's pieces would take half of
-// the register file at full width; the two of the pre norm live in LDS, which
-// leaves 128 registers per thread enough (16 waves per CU). The next row's
-// loads are issued into the registers of the current one as soon as these are
-// used up: dh, y and dy before the second row reduction, f after it. KEEP:
-// values stay in registers from their one load; float32 rows of 1024 threads
-// are loaded again where they are used instead.
-template <typename T, int NCH, int NT, bool F8, bool KEEP, int WPE>
-__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) gnorm_bwd_kernel(GnBwd a) {
+// A block of 512 threads (one per CU, 256 registers each) whose G = blockDim /
+// tpr groups of tpr threads take the chunk's rows in turn; thread t of a group
+// owns the NCH 8-column pieces t + c tpr. Every group runs the same number of
+// rows, so the barriers line up. The four column sums would take half of the
+// register file at full width; the two of the pre norm live in LDS. That leaves
+// room for the next row's dh and y (PF, bf16), so that loads are in flight all
+// the time; its dy and f follow into the registers of the current row's once
+// these are used up. KEEP:
+// values stay in registers from their one load; the widest float32 rows are
+// loaded again where they are used instead.
+template <typename T, int NCH, bool F8, bool KEEP, bool PF>
+__global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   using Row = GnRow<T, NCH, F8>;
-  constexpr bool ONE = NT > 512;
+  constexpr int NT = 512;
   constexpr int PIECES = NT * NCH;
   __shared__ float red[2][NT / 64][2];
-  // column sums: half h of piece p of sum k at (2 k + h) PIECES + p, so that
-  // consecutive lanes touch consecutive 16 bytes
+  // column sums: half h of a thread's piece c of sum k at (2 k + h) PIECES +
+  // c NT + thread, so that consecutive lanes touch consecutive 16 bytes and the
+  // offsets are constants
   extern __shared__ __attribute__((aligned(16))) f32x4 sums[];
-  const int tpr = ONE ? (int)blockDim.x : a.tpr, G = ONE ? 1 : (int)blockDim.x / tpr, wpg = tpr >> 6;
+  const int tpr = a.tpr, G = (int)blockDim.x / tpr, wpg = tpr >> 6;
   // a group is whole waves: its number, and with it the row and its statistics,
   // are scalars
-  const int q = ONE ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / tpr);
+  const int q = __builtin_amdgcn_readfirstlane((int)threadIdx.x / tpr);
   const int t = (int)threadIdx.x - q * tpr;
   const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
   const int n = a.n, chunks = (int)gridDim.x, row_bytes = n * (int)sizeof(T);
@@ -224,12 +225,12 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
   const RowBuf gate(a.gate, a.gate ? (int64_t)gi * row_bytes : 0, a.gate ? row_bytes : 0);
   const uint32_t gate_or = a.gate ? 0u : one_bits<T>(), post_or = post ? 0u : one_bits<T>();
   uint32_t col[NCH];
-  f32x4* const mine = sums + q * tpr * NCH + t;
+  f32x4* const mine = sums + threadIdx.x;
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
     col[c] = 8u * (uint32_t)(t + c * tpr);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mine[k * PIECES + c * tpr] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < 4; ++k) mine[k * PIECES + c * NT] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   f32x4 s2[NCH][2], s3[NCH][2];  // column sums of t and t fh
 #pragma unroll
@@ -306,6 +307,9 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
     fetch_f(cur);
   }
   for (int it = 0; it < steps; ++it) {
+    Row nxt;
+    fetch_row(it + 1, nxt);
+    if (PF) fetch_h(nxt);
     // yh = y ry - my ry, fh = f rf - mf rf
     const float ry = cur.st.w, oy = -cur.st.z * ry, rr = cur.st.y, of = -cur.st.x * rr;
     float m1 = 0.f, m2 = 0.f;
@@ -321,7 +325,7 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
           cur.dh[c].get4(h, d4);
           cur.y[c].get4(h, y4);
           g.get4(h, g4);
-          f32x4 u = mine[h * PIECES + c * tpr], v = mine[(2 + h) * PIECES + c * tpr];
+          f32x4 u = mine[h * PIECES + c * NT], v = mine[(2 + h) * PIECES + c * NT];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float yh = fmaf(y4[i], ry, oy), w = d4[i] * g4[i];
@@ -330,13 +334,14 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
             m1 += w;
             m2 = fmaf(w, yh, m2);
           }
-          mine[h * PIECES + c * tpr] = u;
-          mine[(2 + h) * PIECES + c * tpr] = v;
+          mine[h * PIECES + c * NT] = u;
+          mine[(2 + h) * PIECES + c * NT] = v;
         }
         if (KEEP) {
           cur.dh[c].renew();
           cur.y[c].renew();
         }
+        if (NCH == 4) __builtin_amdgcn_sched_barrier(0);  // one piece's temporaries at a time
       }
       row_sum2(0, m1, m2);
       m1 *= inv_n;
@@ -384,13 +389,10 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
         }
       }
       o.store(bx, col[c] * (uint32_t)sizeof(T));
+      if (NCH == 4) __builtin_amdgcn_sched_barrier(0);
     }
-    Row nxt;
-    fetch_row(it + 1, nxt);
-    if (KEEP) {
-      fetch_h(nxt);
-      fetch_d(nxt);
-    }
+    if (KEEP && !PF) fetch_h(nxt);
+    if (KEEP) fetch_d(nxt);
     if (post) {
       row_sum2(1, m3, m4);
       m3 *= inv_n;
@@ -427,9 +429,10 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
       float* out = a.part + ((int64_t)(k + j) * chunks + blockIdx.x) * n;
       const f32x4* src = sums + 2 * j * PIECES;
       for (int e = (int)threadIdx.x; 4 * e < n; e += (int)blockDim.x) {
-        const int p = e >> 1, h = e & 1;
-        f32x4 v = src[h * PIECES + p];
-        for (int gq = 1; gq < G; ++gq) v += src[h * PIECES + gq * tpr * NCH + p];
+        const int p = e >> 1, h = e & 1, c = p / tpr;
+        const f32x4* at = src + h * PIECES + c * NT + (p - c * tpr);
+        f32x4 v = at[0];
+        for (int gq = 1; gq < G; ++gq) v += at[gq * tpr];
         *reinterpret_cast<f32x4*>(out + 4 * e) = v;
       }
     }
@@ -441,8 +444,8 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) 
   for (int c = 0; c < NCH; ++c)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      mine[h * PIECES + c * tpr] = s2[c][h];
-      mine[(2 + h) * PIECES + c * tpr] = s3[c][h];
+      mine[h * PIECES + c * NT] = s2[c][h];
+      mine[(2 + h) * PIECES + c * NT] = s3[c][h];
     }
   put(2);
 }
@@ -455,53 +458,68 @@ struct GnFinal {
   float scale;
 };
 
-// Sums of the partial rows: 32 columns x 32 chunk lanes per block, a lane
-// adding every 32nd chunk, the lanes' sums added in order. blockIdx.y 0 and 1:
-// the pre norm's shift and gain; 2 and 3: the post norm's, each chunk weighted
-// by its gate; from 4 on the gate, `lanes` lanes to a gate row.
+// Sums of the partial rows: 64 columns (4 per thread) x 64 chunk lanes per
+// block, a lane adding every 64th chunk, the lanes' sums added in order.
+// Jobs 0 and 1: the pre norm's shift and gain; 2 and 3: the post norm's, each
+// chunk weighted by its gate; from 4 on the gate, `lanes` lanes to a gate row.
+// With one gate row (or none) job 4 forms the post norm's sums as well, so that
+// the partials of t and t fh are read once (16384 columns, 256 chunks: 100 MB
+// down to 67).
 template <typename T>
 __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
-  __shared__ float red[2][32][33];
-  const int e = threadIdx.x % 32, q = threadIdx.x / 32;
-  const int64_t c = (int64_t)blockIdx.x * 32 + e;
-  const int job = (int)blockIdx.y;
+  __shared__ f32x4 red[2][64][16];
+  const int e = threadIdx.x % 16, q = threadIdx.x / 16;
+  const int tiles = (a.n + 63) / 64, job = (int)blockIdx.x / tiles;
+  const int c = ((int)blockIdx.x % tiles) * 64 + 4 * e;
   const bool on = c < a.n;
   const int chunks = a.gates * a.cpg;
   const T* gate = static_cast<const T*>(a.gate);
-  if (job < 2 ? !a.pre : job < 4 && !a.post) return;
+  const bool one = a.gates == 1;
+  if (job < 2 ? !a.pre : job < 4 && (one || !a.post)) return;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  auto get = [&](const float* p) { return *reinterpret_cast<const f32x4*>(p); };
+  auto vec = [&](const void* p, int64_t at) {
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = to_f(static_cast<const T*>(p)[at + i]);
+    return v;
+  };
+  auto put = [&](float* o, f32x4 v) {
+    if (a.accumulate) v += get(o);
+    *reinterpret_cast<f32x4*>(o) = v;
+  };
   if (job < 4) {
     const float* p = a.part + (int64_t)job * chunks * a.n + c;
-    float s = 0.f;
+    f32x4 s = zero;
     if (on) {
-      if (job < 2 || !gate) {
+      if (job < 2) {
 #pragma unroll 8
-        for (int k = q; k < chunks; k += 32) s += p[(int64_t)k * a.n];
+        for (int k = q; k < chunks; k += 64) s += get(p + (int64_t)k * a.n);
       } else {
 #pragma unroll 8
-        for (int k = q; k < chunks; k += 32) s = fmaf(to_f(gate[(int64_t)(k / a.cpg) * a.n + c]), p[(int64_t)k * a.n], s);
+        for (int k = q; k < chunks; k += 64) s += vec(gate, (int64_t)(k / a.cpg) * a.n + c) * get(p + (int64_t)k * a.n);
       }
     }
     red[0][q][e] = s;
     __syncthreads();
     if (q != 0 || !on) return;
-    s = 0.f;
-#pragma unroll
-    for (int k = 0; k < 32; ++k) s += red[0][k][e];
+    s = zero;
+#pragma unroll 8
+    for (int k = 0; k < 64; ++k) s += red[0][k][e];
     if (job >= 2) s *= a.scale;
-    float* o = (job == 0 ? a.dpre_b : job == 1 ? a.dpre_g : job == 2 ? a.dpost_b : a.dpost_g) + c;
-    *o = a.accumulate ? *o + s : s;
+    put((job == 0 ? a.dpre_b : job == 1 ? a.dpre_g : job == 2 ? a.dpost_b : a.dpost_g) + c, s);
     return;
   }
-  const int per = 32 / a.lanes, ql = q % a.lanes;
+  const int per = 64 / a.lanes, ql = q % a.lanes;
   const int64_t g = (int64_t)(job - 4) * per + q / a.lanes;
-  float s1 = 0.f, s2 = 0.f;
+  f32x4 s1 = zero, s2 = zero;
   if (on && g < a.gates) {
     const float* p2 = a.part + ((int64_t)3 * chunks + g * a.cpg) * a.n + c;
     const float* p1 = p2 - (int64_t)chunks * a.n;
-#pragma unroll 4
+#pragma unroll 8
     for (int k = ql; k < a.cpg; k += a.lanes) {
-      s2 += p2[(int64_t)k * a.n];
-      if (a.post) s1 += p1[(int64_t)k * a.n];
+      s2 += get(p2 + (int64_t)k * a.n);
+      if (a.post) s1 += get(p1 + (int64_t)k * a.n);
     }
   }
   red[0][q][e] = s1;
@@ -512,26 +530,28 @@ __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
     s1 += red[0][q + k][e];
     s2 += red[1][q + k][e];
   }
-  float v = s2;
-  if (a.post)
-    v = to_f(static_cast<const T*>(a.post_g)[c]) * s2 + to_f(static_cast<const T*>(a.post_b)[c]) * s1;
-  v *= a.scale;
-  float* o = a.dgate + g * a.n + c;
-  *o = a.accumulate ? *o + v : v;
+  if (one && a.post) {
+    const f32x4 w = gate ? vec(gate, c) * a.scale : f32x4{a.scale, a.scale, a.scale, a.scale};
+    put(a.dpost_g + c, w * s2);
+    put(a.dpost_b + c, w * s1);
+  }
+  if (!gate) return;
+  f32x4 v = s2;
+  if (a.post) v = vec(a.post_g, c) * s2 + vec(a.post_b, c) * s1;
+  put(a.dgate + g * a.n + c, v * a.scale);
 }
 
-// The backward's launch shape. A thread owns one or two pieces (two from 513
-// columns on, where a row then fills a wave), a block 512 threads, 1024 above
-// 8192 columns. Chunks: about one per CU, whole turns of the block's groups.
+// The backward's launch shape. A thread owns one, two or four pieces (a row of up
+// to 1024 columns is a wave's), a block as many rows at once as 512 threads
+// hold. Chunks: about one per CU, whole turns of the block's groups.
 struct GnShape {
-  int nch, nt, tpr, G, rpg, rpb, cpg;
+  int nch, tpr, G, rpg, rpb, cpg;
 };
 GnShape gn_shape(const GnormDims& z) {
   GnShape h{};
-  h.nch = z.n <= 512 ? 1 : 2;
-  h.nt = z.n <= 8192 ? 512 : 1024;
+  h.nch = z.n <= 512 ? 1 : z.n <= 1024 ? 2 : 4;
   h.tpr = (int)(cdiv(cdiv(z.n, 8 * h.nch), 64) * 64);
-  h.G = h.nt / h.tpr;
+  h.G = 512 / h.tpr;
   h.rpg = z.rows / std::max(1, z.gates);
   const int turns = std::max<int>({1, (8 + h.G - 1) / h.G, (z.rows + 128 * h.G) / (256 * h.G)});
   h.rpb = std::min(h.rpg, turns * h.G);
@@ -585,29 +605,27 @@ size_t gnorm_bwd_ws_bytes(const GnormDims& z) {
 
 namespace {
 
-template <typename T, int NCH, int NT, bool F8>
+template <typename T, int NCH, bool F8>
 orbit_status gnorm_bwd_run(const GnBwd& a, const KernelInfo& ki, int chunks, int threads, hipStream_t s) {
-  // bf16: 16 waves per CU; float32 values take twice the registers
-  constexpr bool KEEP = sizeof(T) == 2 || NT == 512;
-  constexpr int WPE = sizeof(T) == 2 || NT == 1024 ? 4 : 2;
-  const auto kern = gnorm_bwd_kernel<T, NCH, NT, F8, KEEP, WPE>;
+  constexpr bool KEEP = sizeof(T) == 2 || NCH < 4, PF = sizeof(T) == 2;
+  constexpr int LDS = 512 * NCH * 64;
+  const auto kern = gnorm_bwd_kernel<T, NCH, F8, KEEP, PF>;
   static const bool once = [&] {
     // lift the default dynamic-LDS cap (a failure surfaces as a launch error)
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                              NT * NCH * 64);
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     (void)hipGetLastError();
     return true;
   }();
   (void)once;
-  return launch(ki, kern, dim3((unsigned)chunks), dim3((unsigned)threads), (size_t)NT * NCH * 64, s, a);
+  return launch(ki, kern, dim3((unsigned)chunks), dim3((unsigned)threads), (size_t)LDS, s, a);
 }
 
 template <typename T, bool F8>
 orbit_status gnorm_bwd_t(const GnBwd& a, const GnShape& h, const KernelInfo& ki, int chunks, hipStream_t s) {
   const int threads = h.G * h.tpr;
-  if (h.nt == 1024) return gnorm_bwd_run<T, 2, 1024, F8>(a, ki, chunks, threads, s);
-  if (h.nch == 2) return gnorm_bwd_run<T, 2, 512, F8>(a, ki, chunks, threads, s);
-  return gnorm_bwd_run<T, 1, 512, F8>(a, ki, chunks, threads, s);
+  if (h.nch == 4) return gnorm_bwd_run<T, 4, F8>(a, ki, chunks, threads, s);
+  if (h.nch == 2) return gnorm_bwd_run<T, 2, F8>(a, ki, chunks, threads, s);
+  return gnorm_bwd_run<T, 1, F8>(a, ki, chunks, threads, s);
 }
 
 }  // namespace
@@ -649,9 +667,10 @@ orbit_status gnorm_bwd(const GnormDims& z, const GnormParams& p, const void* f, 
   b.dgate = g.gate; b.dpost_g = g.post_g; b.dpost_b = g.post_b; b.dpre_g = g.pre_g; b.dpre_b = g.pre_b;
   b.n = z.n; b.gates = gates; b.cpg = h.cpg; b.pre = z.pre; b.post = z.post;
   b.accumulate = accumulate; b.scale = z.scale;
-  b.lanes = std::min(32, pow2_ceil(h.cpg));
+  b.lanes = std::min(64, pow2_ceil(h.cpg));
   KernelInfo kf{"gnorm_final", 0.0, 4.0 * chunks * z.n * (2 * z.pre + 2 * rf)};
-  const dim3 fgrid((unsigned)cdiv(z.n, 32), (unsigned)(z.gates ? 4 + cdiv(z.gates, 32 / b.lanes) : z.post ? 4 : 2));
+  const int64_t jobs = rf ? 4 + cdiv(gates, 64 / b.lanes) : 2;
+  const dim3 fgrid((unsigned)(cdiv(z.n, 64) * jobs));
   if (z.dt == ORBIT_BF16) return launch(kf, gnorm_final_kernel<bf16>, fgrid, dim3(1024), 0, s, b);
   return launch(kf, gnorm_final_kernel<float>, fgrid, dim3(1024), 0, s, b);
 }
