@@ -6,36 +6,11 @@
 
 #include "act8.h"
 #include "gnorm.h"
+#include "lanes.h"
 #include "rowbuf.h"
 
 namespace orbit {
 namespace {
-
-template <typename T> ORBIT_DEV void load8(const T* p, float* f);
-template <> ORBIT_DEV void load8<bf16>(const bf16* p, float* f) { unpack(ld128(p), f, (bf16*)nullptr); }
-template <> ORBIT_DEV void load8<float>(const float* p, float* f) {
-  unpack(ld128(p), f, (float*)nullptr);
-  unpack(ld128(p + 4), f + 4, (float*)nullptr);
-}
-template <typename T> ORBIT_DEV void store8(T* p, const float* f);
-template <> ORBIT_DEV void store8<bf16>(bf16* p, const float* f) { st128(p, pack(f, (bf16*)nullptr)); }
-template <> ORBIT_DEV void store8<float>(float* p, const float* f) {
-  st128(p, pack(f, (float*)nullptr));
-  st128(p + 4, pack(f + 4, (float*)nullptr));
-}
-
-// sum over the TPR threads of a row: a wave, or the whole 256-thread block
-// (then `red` is 4 floats of LDS and the call ends with a barrier)
-template <int TPR> ORBIT_DEV float row_sum(float v, float* red) {
-  v = wave_sum(v);
-  if constexpr (TPR > 64) {
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = (red[0] + red[1]) + (red[2] + red[3]);
-    __syncthreads();
-  }
-  return v;
-}
 
 struct GnFwd {
   const void *x, *f, *gate, *post_g, *post_b, *pre_g, *pre_b;
@@ -43,109 +18,182 @@ struct GnFwd {
   const uint8_t *fc, *fe;  // the store that f is read from (f null)
   uint8_t *qc, *qe;        // the store that receives f (may be null)
   float* stats;
-  int rows, n, groups, rpg;  // rpg: rows per gate row
+  int rows, n, groups, rpg, tpr;  // rpg: rows per gate row
   int post, pre;
   float scale, eps;
 };
 
-// mean and 1 / sqrt(variance + eps) of a row held as v[NCH][8]
-template <int NCH, int TPR>
-ORBIT_DEV void row_stats(const float (*v)[8], const bool* on, int n, float eps, float* red, float& mu, float& r) {
-  float s = 0.f;
-#pragma unroll
-  for (int c = 0; c < NCH; ++c)
-    if (on[c])
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += v[c][i];
-  mu = row_sum<TPR>(s, red) / (float)n;
-  float q = 0.f;
-#pragma unroll
-  for (int c = 0; c < NCH; ++c)
-    if (on[c])
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float t = v[c][i] - mu;
-        q += t * t;
-      }
-  r = rsqrtf(row_sum<TPR>(q, red) / (float)n + eps);
-}
+// 8 codes of a store and their group's E
+struct Raw8Q {
+  u32v2 q;
+  uint32_t e;
+  ORBIT_DEV void renew() { asm volatile("" : "+v"(q)); }
+  ORBIT_DEV void get4(int h, float* f) const { act8_decode4(q[h], e, f); }
+  // piece at column col of row r; `on`: a row of n columns is there
+  ORBIT_DEV void load(const uint8_t* codes, const uint8_t* exps, int64_t r, int n, int groups, uint32_t col, bool on) {
+    const RowBuf bq(codes, r * n, on ? n : 0), be(exps, r * groups, on ? groups : 0);
+    q = __builtin_amdgcn_raw_buffer_load_b64(bq.r, col, 0, 0);
+    // where nothing is read: any E but 0, which stands for NaN
+    e = __builtin_amdgcn_raw_buffer_load_b8(be.r, col >> 5, 0, 0) | (on && col < (uint32_t)n ? 0u : 7u);
+  }
+};
 
-// TPR threads per row, thread t of a row owning the 8-column pieces t + c TPR,
-// so that a quad holds the 32 columns of a group of the store. y is written
-// rounded to the storage type, h and the statistics come from its float32
-// value: h then carries one rounding instead of two, and the backward's
-// (rounded y - mean) differs from the exact one by y's rounding alone.
-template <typename T, int NCH, int TPR>
-__global__ void __launch_bounds__(256) gnorm_fwd_kernel(GnFwd a) {
-  __shared__ float red[4];
-  const int t = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  if (row >= a.rows) return;  // whole waves (TPR 64); never with TPR 256
-  const int64_t base = row * a.n;
-  int col[NCH];
+// A block's G = blockDim / tpr groups of tpr threads take a row each; thread t
+// of a group owns the NCH 8-column pieces t + c tpr, so that a quad holds the 32
+// columns of a group of the store. Statistics: each thread's own mean and
+// squared deviations, merged pairwise over the wave, then over the row's waves
+// through LDS with one barrier. y is written rounded to the storage type, h and
+// the statistics come from its float32 value: h then carries one rounding
+// instead of two, and the backward's (rounded y - mean) differs from the exact
+// one by y's rounding alone.
+//
+// Many independent rows per CU (16 waves: at most 128 registers) hide the two
+// reductions of a row; 4096 x 8192 in bf16 moves 268 MB in 58 us (4.6 TB/s; a
+// copy of that size 5.3). One block per CU that kept the parameter vectors in
+// registers and loaded its next row ahead took 85 us, 20 waves with their
+// spills 76. STREAM: x and f are loaded non-temporally.
+template <typename T, int NCH, bool F8, bool STREAM>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) gnorm_fwd_kernel(GnFwd a) {
+  constexpr int AUX = STREAM ? 2 : 0;
+  __shared__ float2 red[2][8];  // [norm][wave]
+  __shared__ float counts[8];
+  const int tpr = a.tpr, G = (int)blockDim.x / tpr, wpg = tpr >> 6;
+  const int q = __builtin_amdgcn_readfirstlane((int)threadIdx.x / tpr);
+  const int t = (int)threadIdx.x - q * tpr, wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+  const int n = a.n, row_bytes = n * (int)sizeof(T);
+  const int64_t r = (int64_t)blockIdx.x * G + q;
+  const bool rv = r < a.rows, post = a.post, pre = a.pre;
+  uint32_t col[NCH];
   bool on[NCH];
-  float v[NCH][8], x[NCH][8];
+  int own = 0;  // values of this thread
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
-    col[c] = 8 * (t + c * TPR);
-    on[c] = col[c] < a.n;
+    col[c] = 8u * (uint32_t)(t + c * tpr);
+    on[c] = col[c] < (uint32_t)n;
+    own += on[c] ? 8 : 0;
+  }
+  auto row = [&](const void* p, int64_t at, bool there) { return RowBuf(p, at * row_bytes, there ? row_bytes : 0); };
+  // an absent gain or gate is 1: its zeros or-ed with the bits of 1
+  auto vec = [&](const RowBuf& b, int c, uint32_t bits) {
+    Raw8<T> v;
+    v.load(b, col[c] * (uint32_t)sizeof(T));
+    v.or_bits(bits);
+    return v;
+  };
+  Raw8<T> x[NCH];
+  float v[NCH][8];
+  {
+    std::conditional_t<F8, Raw8Q, Raw8<T>> f[NCH];
+    const RowBuf bx = row(a.x, r, rv), bf = row(a.f, F8 ? 0 : r, !F8 && rv);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] = x[c][i] = 0.f;
-    if (on[c]) {
-      if (a.f) load8(static_cast<const T*>(a.f) + base + col[c], v[c]);
-      else act8_decode(*reinterpret_cast<const uint2*>(a.fc + base + col[c]),
-                       a.fe[row * a.groups + (col[c] >> 5)], v[c]);
-      load8(static_cast<const T*>(a.x) + base + col[c], x[c]);
+    for (int c = 0; c < NCH; ++c) {
+      x[c].template load<AUX>(bx, col[c] * (uint32_t)sizeof(T));
+      if constexpr (F8) f[c].load(a.fc, a.fe, r, n, a.groups, col[c], rv);
+      else f[c].template load<AUX>(bf, col[c] * (uint32_t)sizeof(T));
     }
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) f[c].get4(h, v[c] + 4 * h);
+  }
+  const float inv_own = own ? 1.f / (float)own : 0.f;
+  WaveMoments wm;
+  wm.init((float)own);
+  if (wpg > 1) {
+    if (lane == 0) counts[wave] = wm.count;
+    __syncthreads();
   }
   if (a.qc) {
+    const RowBuf bq(a.qc, r * n, rv ? n : 0), be(a.qe, r * a.groups, rv ? a.groups : 0);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-      uint2 q;
-      const uint32_t e = act8_encode(v[c], q);
-      if (on[c]) {
-        *reinterpret_cast<uint2*>(a.qc + base + col[c]) = q;
-        if ((t & 3) == 0) a.qe[row * a.groups + (col[c] >> 5)] = (uint8_t)e;
+      uint2 codes;
+      const uint32_t e = act8_encode(v[c], codes);
+      __builtin_amdgcn_raw_buffer_store_b64(u32v2{codes.x, codes.y}, bq.r, col[c], 0, 0);
+      // a quad's first lane stores its E; the others' stores fall past the end
+      __builtin_amdgcn_raw_buffer_store_b8((uint8_t)e, be.r, (t & 3) == 0 ? col[c] >> 5 : 0x7fffffffu, 0, 0);
+    }
+  }
+  // mean and 1 / sqrt(variance + eps) of the row held as v; k: which norm
+  auto moments = [&](int k, float& mu, float& rs) {
+    float s = 0.f, d = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[c][i];
+    float m = s * inv_own;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+      if (on[c])
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float e = v[c][i] - m;
+          d = fmaf(e, e, d);
+        }
+    wm.merge(m, d);
+    if (wpg > 1) {
+      if (lane == 0) red[k][wave] = make_float2(m, d);
+      __syncthreads();
+      float sum = 0.f;
+      for (int w = q * wpg; w < (q + 1) * wpg; ++w) sum = fmaf(counts[w], red[k][w].x, sum);
+      m = sum / (float)n;
+      d = 0.f;
+      for (int w = q * wpg; w < (q + 1) * wpg; ++w) {
+        const float2 e = red[k][w];
+        d += fmaf(counts[w] * (e.x - m), e.x - m, e.y);
       }
     }
-  }
-  float mf = 0.f, rf = 0.f, my = 0.f, ry = 0.f;
-  if (a.post) row_stats<NCH, TPR>(v, on, a.n, a.eps, red, mf, rf);
-  const T* gate = static_cast<const T*>(a.gate);
-  if (gate) gate += (row / a.rpg) * a.n;
+    mu = m;
+    rs = rsqrtf(d / (float)n + a.eps);
+  };
+  float mf = 0.f, rf = 1.f, my = 0.f, ry = 0.f;
+  if (post) moments(0, mf, rf);
+  const float of = -mf * rf;
+  const RowBuf by = row(a.y, r, rv);
+  const RowBuf bpg = row(a.post_g, 0, post), bpb = row(a.post_b, 0, post);
+  const RowBuf bgt = row(a.gate, a.gate && rv ? (int)r / a.rpg : 0, a.gate != nullptr);
+  const uint32_t gate_or = a.gate ? 0u : one_bits<T>(), post_or = post ? 0u : one_bits<T>();
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
-    if (!on[c]) continue;
-    float w[8], b[8];
-    if (a.post) {
-      load8(static_cast<const T*>(a.post_g) + col[c], w);
-      load8(static_cast<const T*>(a.post_b) + col[c], b);
+    const Raw8<T> pg = vec(bpg, c, post_or), pb = vec(bpb, c, 0u), gt = vec(bgt, c, gate_or);
+    Raw8<T> o;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] = (v[c][i] - mf) * rf * w[i] + b[i];
+    for (int h = 0; h < 2; ++h) {
+      float x4[4], g4[4], b4[4], t4[4];
+      x[c].get4(h, x4);
+      pg.get4(h, g4);
+      pb.get4(h, b4);
+      gt.get4(h, t4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = fmaf(fmaf(v[c][4 * h + i], rf, of), g4[i], b4[i]);
+        v[c][4 * h + i] = fmaf(a.scale * t4[i], p, x4[i]);
+      }
+      o.put4(h, v[c] + 4 * h);
     }
-    if (gate) {
-      load8(gate + col[c], w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] *= w[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] = x[c][i] + a.scale * v[c][i];
-    store8(static_cast<T*>(a.y) + base + col[c], v[c]);
+    o.store(by, col[c] * (uint32_t)sizeof(T));
   }
-  if (a.pre) {
-    row_stats<NCH, TPR>(v, on, a.n, a.eps, red, my, ry);
+  if (pre) {
+    moments(1, my, ry);
+    const float oy = -my * ry;
+    const RowBuf bh = row(a.h, r, rv), bhg = row(a.pre_g, 0, true), bhb = row(a.pre_b, 0, true);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-      if (!on[c]) continue;
-      float w[8], b[8];
-      load8(static_cast<const T*>(a.pre_g) + col[c], w);
-      load8(static_cast<const T*>(a.pre_b) + col[c], b);
+      const Raw8<T> hg = vec(bhg, c, 0u), hb = vec(bhb, c, 0u);
+      Raw8<T> o;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = (v[c][i] - my) * ry * w[i] + b[i];
-      store8(static_cast<T*>(a.h) + base + col[c], w);
+      for (int h = 0; h < 2; ++h) {
+        float g4[4], b4[4];
+        hg.get4(h, g4);
+        hb.get4(h, b4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b4[i] = fmaf(fmaf(v[c][4 * h + i], ry, oy), g4[i], b4[i]);
+        o.put4(h, b4);
+      }
+      o.store(bh, col[c] * (uint32_t)sizeof(T));
     }
   }
-  if (t == 0) *reinterpret_cast<float4*>(a.stats + 4 * row) = make_float4(mf, rf, my, ry);
+  if (rv && t == 0) *reinterpret_cast<float4*>(a.stats + 4 * r) = make_float4(mf, post ? rf : 0.f, my, ry);
 }
 
 // ---- backward ---------------------------------------------------------------
@@ -170,14 +218,6 @@ struct GnBwd {
   int rows, n, groups, rpg, rpb, cpg, tpr;
   int post, pre;
   float scale;
-};
-
-// 8 codes of a store and their group's E
-struct Raw8Q {
-  u32v2 q;
-  uint32_t e;
-  ORBIT_DEV void renew() { asm volatile("" : "+v"(q)); }
-  ORBIT_DEV void get4(int h, float* f) const { act8_decode4(q[h], e, f); }
 };
 
 // a thread's part of one row, as loaded
@@ -240,8 +280,8 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   const float inv_n = 1.f / (float)n;
   // sums of two values over the row's threads; every thread of the block calls
   auto row_sum2 = [&](int k, float& u, float& v) {
-    u = wave_sum(u);
-    v = wave_sum(v);
+    u = wave_add(u);
+    v = wave_add(v);
     if (wpg > 1) {
       if (lane == 0) {
         red[k][wave][0] = u;
@@ -285,14 +325,8 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   };
   auto fetch_f = [&](Row& R) {
     if constexpr (F8) {
-      const bool v = rf && R.rv;
-      const RowBuf bq(a.fc, R.r * n, v ? n : 0), be(a.fe, R.r * a.groups, v ? a.groups : 0);
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        R.f[c].q = __builtin_amdgcn_raw_buffer_load_b64(bq.r, col[c], 0, 0);
-        // where nothing is read: any E but 0, which stands for NaN
-        R.f[c].e = __builtin_amdgcn_raw_buffer_load_b8(be.r, col[c] >> 5, 0, 0) | (v && col[c] < (uint32_t)n ? 0u : 7u);
-      }
+      for (int c = 0; c < NCH; ++c) R.f[c].load(a.fc, a.fe, R.r, n, a.groups, col[c], rf && R.rv);
     } else {
       const RowBuf b = row(a.f, R, rf);
 #pragma unroll
@@ -560,19 +594,29 @@ GnShape gn_shape(const GnormDims& z) {
   return h;
 }
 
-template <typename T>
-orbit_status gnorm_fwd_t(const GnFwd& a, const KernelInfo& ki, hipStream_t s) {
-  const dim3 block(256);
-  if (a.n <= 2048) {
-    const dim3 grid((unsigned)cdiv(a.rows, 4));
-    if (a.n <= 512) return launch(ki, gnorm_fwd_kernel<T, 1, 64>, grid, block, 0, s, a);
-    if (a.n <= 1024) return launch(ki, gnorm_fwd_kernel<T, 2, 64>, grid, block, 0, s, a);
-    return launch(ki, gnorm_fwd_kernel<T, 4, 64>, grid, block, 0, s, a);
+// A row of up to 2048 columns is a wave's (one, two or four pieces a thread);
+// wider ones take up to 512 threads with four pieces, or three from 8193 to 12288
+// columns (2048 x 12288: 50 us, with four pieces on 384 threads 57). Narrow
+// rows share blocks of 256 threads. Non-temporal loads from 96 MB of x, f, y
+// and h on, which the caches would not hold (bf16, 134 MB: 31.1 -> 29.1 us,
+// 67 MB: 15.2 -> 16.4).
+template <typename T, bool F8>
+orbit_status gnorm_fwd_t(GnFwd& a, const KernelInfo& ki, hipStream_t s) {
+  const int nch = a.n <= 512 ? 1 : a.n <= 1024 ? 2 : a.n > 8192 && a.n <= 12288 ? 3 : 4;
+  a.tpr = (int)(cdiv(cdiv(a.n, 8 * nch), 64) * 64);
+  const int G = std::min(std::max(1, 256 / a.tpr), a.rows);
+  const bool stream = 4.0 * a.rows * a.n * sizeof(T) >= 96e6;
+  const dim3 grid((unsigned)cdiv(a.rows, G)), block((unsigned)(G * a.tpr));
+#define GNF(C)                                                                              \
+  return stream ? launch(ki, gnorm_fwd_kernel<T, C, F8, true>, grid, block, 0, s, a)        \
+                : launch(ki, gnorm_fwd_kernel<T, C, F8, false>, grid, block, 0, s, a)
+  switch (nch) {
+    case 1: GNF(1);
+    case 2: GNF(2);
+    case 3: GNF(3);
+    default: GNF(4);
   }
-  const dim3 grid((unsigned)a.rows);
-  if (a.n <= 4096) return launch(ki, gnorm_fwd_kernel<T, 2, 256>, grid, block, 0, s, a);
-  if (a.n <= 8192) return launch(ki, gnorm_fwd_kernel<T, 4, 256>, grid, block, 0, s, a);
-  return launch(ki, gnorm_fwd_kernel<T, 8, 256>, grid, block, 0, s, a);
+#undef GNF
 }
 
 }  // namespace
@@ -595,8 +639,8 @@ orbit_status gnorm_fwd(const GnormDims& z, const GnormParams& p, const void* x, 
   const double rn = (double)z.rows * z.n;
   KernelInfo ki{z.dt == ORBIT_BF16 ? "gnorm_fwd<bf16>" : "gnorm_fwd<f32>", 16.0 * rn,
                 rn * (e * (2 + (f ? 1 : 0) + z.pre) + (store ? q : 0.0))};
-  if (z.dt == ORBIT_BF16) return gnorm_fwd_t<bf16>(a, ki, s);
-  return gnorm_fwd_t<float>(a, ki, s);
+  if (z.dt == ORBIT_BF16) return a.fc ? gnorm_fwd_t<bf16, true>(a, ki, s) : gnorm_fwd_t<bf16, false>(a, ki, s);
+  return a.fc ? gnorm_fwd_t<float, true>(a, ki, s) : gnorm_fwd_t<float, false>(a, ki, s);
 }
 
 size_t gnorm_bwd_ws_bytes(const GnormDims& z) {

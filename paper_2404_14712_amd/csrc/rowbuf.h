@@ -25,9 +25,9 @@ template <typename T>
 struct Raw8 {
   static constexpr int NV = sizeof(T) / 2;
   u32v4 v[NV];
-  ORBIT_DEV void load(const RowBuf& b, uint32_t off) {
+  template <int AUX = 0> ORBIT_DEV void load(const RowBuf& b, uint32_t off) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(b.r, off + 16 * i, 0, 0);
+    for (int i = 0; i < NV; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(b.r, off + 16 * i, 0, AUX);
   }
   ORBIT_DEV void store(const RowBuf& b, uint32_t off) const {
 #pragma unroll
