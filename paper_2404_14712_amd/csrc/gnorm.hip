@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
       const uint32_t e = act8_encode(v[c], codes);
       __builtin_amdgcn_raw_buffer_store_b64(u32v2{codes.x, codes.y}, bq.r, col[c], 0, 0);
       // a quad's first lane stores its E; the others' stores fall past the end
-      __builtin_amdgcn_raw_buffer_store_b8((uint8_t)e, be.r, (t & 3) == 0 ? col[c] >> 5 : 0x7fffffffu, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b8((uint8_t)e, be.r, (t & 3) == 0 ? col[c] >> 5 : kNoOffset, 0, 0);
     }
   }
   // mean and 1 / sqrt(variance + eps) of the row held as v; k: which norm

@@ -11,6 +11,9 @@ namespace orbit {
 typedef uint32_t u32v4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32v2 __attribute__((ext_vector_type(2)));
 
+// an offset past every descriptor: nothing is read (zeros) or written there
+constexpr uint32_t kNoOffset = 0x7fffffffu;
+
 struct RowBuf {
   __amdgpu_buffer_rsrc_t r;
   // bytes of the tensor p from byte `off` on (both wave-uniform)

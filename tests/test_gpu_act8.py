@@ -144,6 +144,23 @@ def test_far_offsets(lib):
     assert bool((out[0] == 1.0).all()) and not bool(out[1:-3].any())
 
 
+def test_rows_far_apart(lib):
+    """Rows of a few columns 2^30 bytes apart: offsets of a block's rows pass 31 bits."""
+    rows, n, ld = 4, 40, 1 << 29
+    x = torch.zeros((rows - 1) * ld + n, dtype=torch.bfloat16, device="cuda")
+    v = torch.randn(rows, n, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    for r in range(rows):
+        x[r * ld:r * ld + n] = v[r].cuda()
+    store = torch.empty(lib.orbit_act8_bytes(rows, n), dtype=torch.uint8, device="cuda")
+    lib.orbit_act8_pack(1, rows, n, x, ld, store)
+    _, _, val = R.act8_ref(v.double().numpy())
+    x.zero_()
+    lib.orbit_act8_unpack(1, rows, n, store, x, ld)
+    for r in range(rows):
+        np.testing.assert_array_equal(x[r * ld:r * ld + n].cpu().double().numpy(), val[r])
+        assert r + 1 == rows or not bool(x[r * ld + n:(r + 1) * ld].any())
+
+
 def test_side_stream_and_graph(lib):
     """Pack, read back and the weight gradient on another stream and captured into a graph,
     replayed with eager work in between: every replay gives the eager result for its inputs."""
