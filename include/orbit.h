@@ -133,7 +133,7 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
  * act8 = 1: `saved` holds q, k, v, o, u and the sub-layers' outputs as 8-bit
  * stores (see orbit_act8_bytes below) and the softmax normalisers in float32:
  * about a fifth of the bytes in bf16. The forward's result does not depend on
- * it; the backward reads the stores back into its workspace, forms x1 and the
+ * it, bit for bit; the backward reads the stores back into its workspace, forms x1 and the
  * norms' and GELU's outputs from them, and runs as from stored tensors, so that
  * its gradients carry the stores' rounding (at most half a step of a group of
  * 32 values, below 2^-7 of its largest). saved == NULL is inference, and

@@ -93,7 +93,8 @@ struct BlockExt {
   bool on = false, act8 = false, post = false;
   int gates = 0;
   float scale = 1.f;
-  bool branch() const { return post || gates; }  // the backward reads the sub-layers' outputs
+  bool branch() const { return post || gates; }            // the backward reads the sub-layers' outputs
+  bool normed() const { return branch() || scale != 1.f; }  // the residuals go through the gated norms
 };
 
 struct BlockSaved {
@@ -308,8 +309,8 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
   // the forward's split partials
   ORBIT_TRY(attn_fwd(dt, io, sv.o, z.A, lse, sv.o32, z.A, w.D, attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh), s));
   if (s8) {
-    ORBIT_TRY(act8_pack(dt, sv.qkv, 3 * z.A, T, 3 * z.A, s8->qkv, s));
-    ORBIT_TRY(act8_pack(dt, sv.o, z.A, T, z.A, s8->o, s));
+    ORBIT_TRY(act8_pack(dt, sv.qkv, nullptr, 3 * z.A, T, 3 * z.A, s8->qkv, s));
+    ORBIT_TRY(act8_pack(dt, sv.o, nullptr, z.A, T, z.A, s8->o, s));
   }
   // where the backward does not read a sub-layer's output, it passes through a
   // buffer of the backward that is idle here
@@ -317,16 +318,19 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
   void* f2 = ext.branch() ? sv.f2 : w.dh;
   {
     Gemm g; g.dtype = dt; g.tag = "proj";
-    g.A = sv.o; g.lda = z.A; g.B = p->w_proj; g.ldb = z.d; g.C = ext.on ? f1 : sv.x1; g.ldc = z.d;
+    g.A = sv.o; g.lda = z.A; g.B = p->w_proj; g.ldb = z.d; g.C = ext.normed() ? f1 : sv.x1; g.ldc = z.d;
     g.M = T; g.N = z.d; g.K = z.A; g.bias = p->b_proj;
-    if (!ext.on) { g.res = x; g.ldr = z.d; }
+    if (!ext.normed()) { g.res = x; g.ldr = z.d; }
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
-  if (ext.on) {
+  if (ext.normed()) {
     ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), x, f1, s8 ? s8->f1 : nullptr, sv.x1,
                         sv.h2, sv.st1, s));
   } else {
     ORBIT_TRY(layernorm_fwd(dt, sv.x1, z.d, p->ln2_g, p->ln2_b, sv.h2, z.d, sv.mu2, sv.r2, T, z.d, z.eps, s));
+    // what the sub-layer added, from which the backward forms x1 again: far
+    // smaller than the residual stream, and stored with a step to match
+    if (s8) ORBIT_TRY(act8_pack(dt, sv.x1, x, z.d, T, z.d, s8->f1, s));
   }
   {
     Gemm g; g.dtype = dt; g.tag = "fc1";
@@ -334,17 +338,17 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
     g.M = T; g.N = z.F; g.K = z.d; g.bias = p->b_fc1; g.gelu_out = sv.u; g.ldgo = z.F;
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
-  if (s8) ORBIT_TRY(act8_pack(dt, sv.u, z.F, T, z.F, s8->u, s));
+  if (s8) ORBIT_TRY(act8_pack(dt, sv.u, nullptr, z.F, T, z.F, s8->u, s));
   if (y || ext.branch()) {
     Gemm g; g.dtype = dt; g.tag = "fc2";
-    g.A = sv.g; g.lda = z.F; g.B = p->w_fc2; g.ldb = z.d; g.C = ext.on ? f2 : y; g.ldc = z.d;
+    g.A = sv.g; g.lda = z.F; g.B = p->w_fc2; g.ldb = z.d; g.C = ext.normed() ? f2 : y; g.ldc = z.d;
     g.M = T; g.N = z.d; g.K = z.F; g.bias = p->b_fc2;
-    if (!ext.on) { g.res = sv.x1; g.ldr = z.d; }
+    if (!ext.normed()) { g.res = sv.x1; g.ldr = z.d; }
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
   // the recompute runs this norm too where the backward reads its statistics;
   // its output then goes to an idle buffer
-  if (ext.on && (y || ext.post))
+  if (ext.normed() && (y || ext.post))
     ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, false), block_gnorm_params(p, ep, 2), sv.x1, f2, s8 ? s8->f2 : nullptr,
                         y ? y : w.dh, nullptr, s8 ? s8->st2 : sv.st2, s));
   return ORBIT_OK;
@@ -583,7 +587,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   };
   // the feed-forward sub-layer's output gradient: dy, or through its gated norm
   const void* dff = dy;
-  if (ext.on && (ext.branch() || ext.scale != 1.f)) {
+  if (ext.normed()) {
     GnormGrads gg{};
     if (ext.gates) gg.gate = eg->gate2;
     if (ext.post) { gg.post_g = eg->post2_g; gg.post_b = eg->post2_b; }
@@ -632,7 +636,8 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   // LN2 backward; the chunk sums of its rows give the LN2 parameter gradients
   // and, summed over its output dx1, the projection's bias gradient
   const void* df1 = w.dx1;  // gradient of the projection's output
-  if (!ext.on) {
+  const bool plain_ln2 = !ext.normed() && !restore;
+  if (plain_ln2) {
     ORBIT_TRY(layernorm_bwd_cols(dt, w.dh, z.d, sv.x1, z.d, sv.mu2, sv.r2, p->ln2_g, dy, w.dx1, z.d, T, z.d, w.p_ln2,
                                  gr->ln2_b, gr->ln2_g, gr->b_proj, fin, s));
   } else {
@@ -642,7 +647,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     gg.pre_g = gr->ln2_g; gg.pre_b = gr->ln2_b;
     if (ext.gates) gg.gate = eg->gate1;
     if (ext.post) { gg.post_g = eg->post1_g; gg.post_b = eg->post1_b; }
-    const bool same = !ext.branch() && ext.scale == 1.f;
+    const bool same = !ext.normed();
     if (!same) df1 = w.df;
     ORBIT_TRY(gnorm_bwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), restore ? nullptr : sv.f1, s8.f1,
                         sv.x1, sv.st1, w.dh, dy, w.dx1, same ? nullptr : w.df, gg, accumulate, w.gn1, s));
@@ -652,9 +657,9 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     g.A = sv.o; g.lda = z.A; g.a_kmajor = false; g.B = df1; g.ldb = z.d; g.b_kmajor = false;
     g.C = gr->w_proj; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
     g.M = z.A; g.N = z.d; g.K = T;
-    const bool fused = ext.on && dw_bias(g, w.p_proj, gr->b_proj);
+    const bool fused = !plain_ln2 && dw_bias(g, w.p_proj, gr->b_proj);
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-    if (ext.on && !fused) {
+    if (!plain_ln2 && !fused) {
       ColJob j[1];
       bias_job(j[0], df1, z.d, w.p_proj, gr->b_proj);
       ORBIT_TRY(colsum_partials(dt, j, 1, T, s));
@@ -1236,7 +1241,7 @@ orbit_status orbit_act8_pack(int32_t dtype, int64_t rows, int32_t n, const void*
   ORBIT_TRY(act8_check(fn, rows, n, store, store_bytes));
   PTR(x, "x");
   REQ(ldx >= n && ldx % 8 == 0, ORBIT_E_ARG, "%s: ldx must be >= n and a multiple of 8", fn);
-  return act8_pack((orbit_dtype)dtype, x, ldx, rows, n, store, S(stream));
+  return act8_pack((orbit_dtype)dtype, x, nullptr, ldx, rows, n, store, S(stream));
 }
 
 orbit_status orbit_act8_unpack(int32_t dtype, int64_t rows, int32_t n, const void* store, size_t store_bytes, void* x,

@@ -67,8 +67,9 @@ ORBIT_DEV void act8_decode(uint2 q, uint32_t e, float* f) {
   act8_decode4(q.y, e, f + 4);
 }
 
-// x[rows, n] (leading dimension ldx) -> store
-orbit_status act8_pack(orbit_dtype dt, const void* x, int64_t ldx, int64_t rows, int n, void* store, hipStream_t s);
+// x[rows, n], or x - sub (sub may be null), both of leading dimension ldx -> store
+orbit_status act8_pack(orbit_dtype dt, const void* x, const void* sub, int64_t ldx, int64_t rows, int n, void* store,
+                       hipStream_t s);
 // store -> x and / or gelu(x) (either may be null)
 orbit_status act8_unpack(orbit_dtype dt, const void* store, int64_t rows, int n, void* x, int64_t ldx, void* gelu,
                          int64_t ldg, hipStream_t s);

@@ -36,7 +36,7 @@ Act8Shape act8_shape(int64_t rows, int n, bool flat, int u, int64_t span) {
 }
 
 struct Act8Args {
-  const void* x;
+  const void *x, *sub;  // sub (may be null; leading dimension ldx): x - sub is packed
   void *out, *gelu;
   const uint8_t *fc, *fe;
   uint8_t *qc, *qe;
@@ -58,15 +58,19 @@ __global__ void __launch_bounds__(256) act8_pack_kernel(Act8Args a) {
     const int rows = (int)std::min<int64_t>(a.rows - rb, ty);
     const bool rv = lr < rows;
     const RowBuf bx(a.x, (rb * a.ldx + c0) * (int)sizeof(T), (int)(((rows - 1) * a.ldx + cols) * (int)sizeof(T)));
+    const RowBuf bs(a.sub, (rb * a.ldx + c0) * (int)sizeof(T),
+                    a.sub ? (int)(((rows - 1) * a.ldx + cols) * (int)sizeof(T)) : 0);
     const RowBuf bq(a.qc, rb * a.n + c0, (int)((rows - 1) * a.n + cols));
     const RowBuf be(a.qe, rb * a.groups + (c0 >> 5), (int)((rows - 1) * a.groups + ((cols + 31) >> 5)));
-    Raw8<T> v[U];
+    Raw8<T> v[U], w[U];
     uint32_t col[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       col[u] = (uint32_t)(u * tx + lx) * 8u;
       const bool on = rv && col[u] < (uint32_t)cols;
-      v[u].template load<AUX>(bx, on ? ((uint32_t)lr * (uint32_t)a.ldx + col[u]) * (uint32_t)sizeof(T) : kNoOffset);
+      const uint32_t at = on ? ((uint32_t)lr * (uint32_t)a.ldx + col[u]) * (uint32_t)sizeof(T) : kNoOffset;
+      v[u].template load<AUX>(bx, at);
+      if (a.sub) w[u].template load<AUX>(bs, at);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -74,6 +78,13 @@ __global__ void __launch_bounds__(256) act8_pack_kernel(Act8Args a) {
       float f[8];
       v[u].get4(0, f);
       v[u].get4(1, f + 4);
+      if (a.sub) {
+        float g[8];
+        w[u].get4(0, g);
+        w[u].get4(1, g + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] -= g[i];
+      }
       uint2 q;
       const uint32_t e = act8_encode(f, q);
       __builtin_amdgcn_raw_buffer_store_b64(u32v2{q.x, q.y}, bq.r, on ? (uint32_t)lr * (uint32_t)a.n + col[u] : kNoOffset, 0, 0);
@@ -135,33 +146,36 @@ __global__ void __launch_bounds__(256) act8_unpack_kernel(Act8Args a) {
 // Two pieces per thread keep enough loads in flight (bf16 8192 x 4096: pack 20.3
 // -> 18.5 us, unpack 22.9 -> 19.5); float32 with the GELU's second output is
 // better off with one where rows are whole groups (4096 x 4096: 32.5 us, two
-// 39.1). From 96 MB on, more than the caches hold, loads are non-temporal
-// (17.6 and 17.8 us; at 50 MB 9.1 -> 9.8).
+// 39.1). From 96 MB on, more than the caches hold, bf16 loads are non-temporal
+// (17.6 and 17.8 us; at 50 MB 9.1 -> 9.8; float32's two 16-byte loads a piece
+// share their cache lines and lose by it, 84 MB: 13.4 -> 16.8).
 template <typename T>
 orbit_status act8_run(const KernelInfo& ki, Act8Args a, int64_t rows, int n, bool flat, bool pack, hipStream_t s) {
   const int u = sizeof(T) == 4 && a.gelu && flat ? 1 : 2;
-  const bool stream = ki.bytes >= 96e6;
+  const bool stream = sizeof(T) == 2 && ki.bytes >= 96e6;
   const Act8Shape z = act8_shape(rows, n, flat, u, std::max(a.ldx, a.ldg) * (int64_t)sizeof(T));
   a.rows = z.rows; a.n = z.n; a.groups = z.groups; a.tx_log2 = z.tx_log2;
   const dim3 block(256);
+  constexpr int NT = sizeof(T) == 2 ? 2 : 0;
   if (pack)
-    return stream ? launch(ki, act8_pack_kernel<T, 2, 2>, z.grid, block, 0, s, a)
+    return stream ? launch(ki, act8_pack_kernel<T, 2, NT>, z.grid, block, 0, s, a)
                   : launch(ki, act8_pack_kernel<T, 2, 0>, z.grid, block, 0, s, a);
   if (sizeof(T) == 4 && u == 1) return launch(ki, act8_unpack_kernel<T, sizeof(T) == 4 ? 1 : 2, 0>, z.grid, block, 0, s, a);
-  return stream ? launch(ki, act8_unpack_kernel<T, 2, 2>, z.grid, block, 0, s, a)
+  return stream ? launch(ki, act8_unpack_kernel<T, 2, NT>, z.grid, block, 0, s, a)
                 : launch(ki, act8_unpack_kernel<T, 2, 0>, z.grid, block, 0, s, a);
 }
 
 }  // namespace
 
-orbit_status act8_pack(orbit_dtype dt, const void* x, int64_t ldx, int64_t rows, int n, void* store, hipStream_t s) {
+orbit_status act8_pack(orbit_dtype dt, const void* x, const void* sub, int64_t ldx, int64_t rows, int n, void* store,
+                       hipStream_t s) {
   Act8Args a{};
-  a.x = x; a.ldx = ldx;
+  a.x = x; a.sub = sub; a.ldx = ldx;
   a.qc = static_cast<uint8_t*>(store);
   a.qe = a.qc + act8_exp_offset(rows, n);
   const double e = dt == ORBIT_BF16 ? 2.0 : 4.0;
   KernelInfo ki{dt == ORBIT_BF16 ? "act8_pack<bf16>" : "act8_pack<f32>", 4.0 * rows * n,
-                (e + 1.0 + 1.0 / kAct8Group) * rows * n};
+                ((sub ? 2.0 : 1.0) * e + 1.0 + 1.0 / kAct8Group) * rows * n};
   const bool flat = n % kAct8Group == 0 && ldx == n;
   if (dt == ORBIT_BF16) return act8_run<bf16>(ki, a, rows, n, flat, true, s);
   return act8_run<float>(ki, a, rows, n, flat, true, s);

@@ -244,6 +244,10 @@ template <typename T, int NCH, bool F8, bool KEEP, bool PF>
 __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   using Row = GnRow<T, NCH, F8>;
   constexpr int NT = 512;
+  // non-temporal loads: bf16 rows only, as a float32 piece's two 16-byte loads
+  // share each cache line with those of the neighbours (2048 x 16384 bf16: 136 ->
+  // 126 us, float32 1024 x 16384: 167 -> 231)
+  constexpr int AUX = sizeof(T) == 2 ? 2 : 0;
   constexpr int PIECES = NT * NCH;
   __shared__ float red[2][NT / 64][2];
   // column sums: half h of a thread's piece c of sum k at (2 k + h) PIECES +
@@ -314,14 +318,14 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     const RowBuf bh = row(a.dh, R, pre), by = row(a.y, R, pre);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-      R.dh[c].load(bh, col[c] * (uint32_t)sizeof(T));
-      R.y[c].load(by, col[c] * (uint32_t)sizeof(T));
+      R.dh[c].template load<AUX>(bh, col[c] * (uint32_t)sizeof(T));
+      R.y[c].template load<AUX>(by, col[c] * (uint32_t)sizeof(T));
     }
   };
   auto fetch_d = [&](Row& R) {
     const RowBuf b = row(a.dy, R, a.dy != nullptr);
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) R.dy[c].load(b, col[c] * (uint32_t)sizeof(T));
+    for (int c = 0; c < NCH; ++c) R.dy[c].template load<AUX>(b, col[c] * (uint32_t)sizeof(T));
   };
   auto fetch_f = [&](Row& R) {
     if constexpr (F8) {
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     } else {
       const RowBuf b = row(a.f, R, rf);
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) R.f[c].load(b, col[c] * (uint32_t)sizeof(T));
+      for (int c = 0; c < NCH; ++c) R.f[c].template load<AUX>(b, col[c] * (uint32_t)sizeof(T));
     }
   };
   Row cur;
@@ -375,7 +379,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
           cur.dh[c].renew();
           cur.y[c].renew();
         }
-        if (NCH == 4) __builtin_amdgcn_sched_barrier(0);  // one piece's temporaries at a time
+        if (NCH > 2) __builtin_amdgcn_sched_barrier(0);  // one piece's temporaries at a time
       }
       row_sum2(0, m1, m2);
       m1 *= inv_n;
@@ -423,7 +427,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
         }
       }
       o.store(bx, col[c] * (uint32_t)sizeof(T));
-      if (NCH == 4) __builtin_amdgcn_sched_barrier(0);
+      if (NCH > 2) __builtin_amdgcn_sched_barrier(0);
     }
     if (KEEP && !PF) fetch_h(nxt);
     if (KEEP) fetch_d(nxt);
@@ -498,7 +502,8 @@ struct GnFinal {
 // chunk weighted by its gate; from 4 on the gate, `lanes` lanes to a gate row.
 // With one gate row (or none) job 4 forms the post norm's sums as well, so that
 // the partials of t and t fh are read once (16384 columns, 256 chunks: 100 MB
-// down to 67).
+// down to 67). Bound by latency but for the widest rows: a lane's loads are
+// issued four at a time.
 template <typename T>
 __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
   __shared__ f32x4 red[2][64][16];
@@ -522,47 +527,56 @@ __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
     if (a.accumulate) v += get(o);
     *reinterpret_cast<f32x4*>(o) = v;
   };
-  if (job < 4) {
-    const float* p = a.part + (int64_t)job * chunks * a.n + c;
+  // sum over the chunks k0, k0 + step, ... < kn of w(k) times the partial rows p
+  auto sum = [&](const float* p, int k0, int kn, int step, auto&& w) {
     f32x4 s = zero;
-    if (on) {
-      if (job < 2) {
-#pragma unroll 8
-        for (int k = q; k < chunks; k += 64) s += get(p + (int64_t)k * a.n);
-      } else {
-#pragma unroll 8
-        for (int k = q; k < chunks; k += 64) s += vec(gate, (int64_t)(k / a.cpg) * a.n + c) * get(p + (int64_t)k * a.n);
-      }
+    for (int k = k0; k < kn; k += 4 * step) {
+      f32x4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = on && k + j * step < kn ? w(k + j * step) * get(p + (int64_t)(k + j * step) * a.n) : zero;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += v[j];
     }
-    red[0][q][e] = s;
-    __syncthreads();
-    if (q != 0 || !on) return;
-    s = zero;
-#pragma unroll 8
-    for (int k = 0; k < 64; ++k) s += red[0][k][e];
-    if (job >= 2) s *= a.scale;
-    put((job == 0 ? a.dpre_b : job == 1 ? a.dpre_g : job == 2 ? a.dpost_b : a.dpost_g) + c, s);
-    return;
-  }
-  const int per = 64 / a.lanes, ql = q % a.lanes;
-  const int64_t g = (int64_t)(job - 4) * per + q / a.lanes;
+    return s;
+  };
+  auto unit = [](int) { return 1.f; };
+  const bool gated = job >= 4;
+  const int lanes = gated ? a.lanes : 64, ql = q % lanes;
+  const int64_t g = gated ? (int64_t)(job - 4) * (64 / lanes) + q / lanes : 0;
+  const bool there = on && (!gated || g < a.gates);
   f32x4 s1 = zero, s2 = zero;
-  if (on && g < a.gates) {
+  if (!gated) {
+    const float* p = a.part + (int64_t)job * chunks * a.n + c;
+    if (job < 2) s1 = sum(p, q, chunks, 64, unit);
+    else if (on) s1 = sum(p, q, chunks, 64, [&](int k) { return vec(gate, (int64_t)(k / a.cpg) * a.n + c); });
+  } else if (there) {
     const float* p2 = a.part + ((int64_t)3 * chunks + g * a.cpg) * a.n + c;
-    const float* p1 = p2 - (int64_t)chunks * a.n;
-#pragma unroll 8
-    for (int k = ql; k < a.cpg; k += a.lanes) {
-      s2 += get(p2 + (int64_t)k * a.n);
-      if (a.post) s1 += get(p1 + (int64_t)k * a.n);
-    }
+    s2 = sum(p2, ql, a.cpg, lanes, unit);
+    if (a.post) s1 = sum(p2 - (int64_t)chunks * a.n, ql, a.cpg, lanes, unit);
   }
   red[0][q][e] = s1;
   red[1][q][e] = s2;
   __syncthreads();
-  if (ql != 0 || !on || g >= a.gates) return;
-  for (int k = 1; k < a.lanes; ++k) {
+  // eight lanes' sums at a time, then the eights
+  const int span = min(8, lanes);
+  if (ql % span == 0) {
+    for (int k = 1; k < span; ++k) {
+      s1 += red[0][q + k][e];
+      s2 += red[1][q + k][e];
+    }
+    red[0][q][e] = s1;
+    red[1][q][e] = s2;
+  }
+  __syncthreads();
+  if (ql != 0 || !there) return;
+  for (int k = 8; k < lanes; k += 8) {
     s1 += red[0][q + k][e];
     s2 += red[1][q + k][e];
+  }
+  if (!gated) {
+    if (job >= 2) s1 *= a.scale;
+    put((job == 0 ? a.dpre_b : job == 1 ? a.dpre_g : job == 2 ? a.dpost_b : a.dpost_g) + c, s1);
+    return;
   }
   if (one && a.post) {
     const f32x4 w = gate ? vec(gate, c) * a.scale : f32x4{a.scale, a.scale, a.scale, a.scale};
@@ -576,14 +590,20 @@ __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
 }
 
 // The backward's launch shape. A thread owns one, two or four pieces (a row of up
-// to 1024 columns is a wave's), a block as many rows at once as 512 threads
-// hold. Chunks: about one per CU, whole turns of the block's groups.
+// to 2048 columns is a wave's), three from 8193 to 12288 columns, so that all 512
+// threads of a block have some; a block takes as many rows at once as that
+// gives. Chunks: about one per CU, in whole turns of the block's groups and of
+// at least 8 rows: more of them cost more partial rows than they hide latency
+// (8192 x 1024: 31 us, with 512 chunks 37).
+// pieces of 8 columns per thread
+int gn_pieces(int n) { return n <= 512 ? 1 : n <= 1024 ? 2 : n > 8192 && n <= 12288 ? 3 : 4; }
+
 struct GnShape {
   int nch, tpr, G, rpg, rpb, cpg;
 };
 GnShape gn_shape(const GnormDims& z) {
   GnShape h{};
-  h.nch = z.n <= 512 ? 1 : z.n <= 1024 ? 2 : 4;
+  h.nch = gn_pieces(z.n);
   h.tpr = (int)(cdiv(cdiv(z.n, 8 * h.nch), 64) * 64);
   h.G = 512 / h.tpr;
   h.rpg = z.rows / std::max(1, z.gates);
@@ -597,18 +617,18 @@ GnShape gn_shape(const GnormDims& z) {
 // A row of up to 2048 columns is a wave's (one, two or four pieces a thread);
 // wider ones take up to 512 threads with four pieces, or three from 8193 to 12288
 // columns (2048 x 12288: 50 us, with four pieces on 384 threads 57). Narrow
-// rows share blocks of 256 threads. Non-temporal loads from 96 MB of x, f, y
-// and h on, which the caches would not hold (bf16, 134 MB: 31.1 -> 29.1 us,
-// 67 MB: 15.2 -> 16.4).
+// rows share blocks of 256 threads. Non-temporal loads in bf16 from 96 MB of x,
+// f, y and h on, which the caches would not hold (134 MB: 31.1 -> 29.1 us, 67
+// MB: 15.2 -> 16.4).
 template <typename T, bool F8>
 orbit_status gnorm_fwd_t(GnFwd& a, const KernelInfo& ki, hipStream_t s) {
-  const int nch = a.n <= 512 ? 1 : a.n <= 1024 ? 2 : a.n > 8192 && a.n <= 12288 ? 3 : 4;
+  const int nch = gn_pieces(a.n);
   a.tpr = (int)(cdiv(cdiv(a.n, 8 * nch), 64) * 64);
   const int G = std::min(std::max(1, 256 / a.tpr), a.rows);
-  const bool stream = 4.0 * a.rows * a.n * sizeof(T) >= 96e6;
+  const bool stream = sizeof(T) == 2 && 8.0 * a.rows * a.n >= 96e6;
   const dim3 grid((unsigned)cdiv(a.rows, G)), block((unsigned)(G * a.tpr));
 #define GNF(C)                                                                              \
-  return stream ? launch(ki, gnorm_fwd_kernel<T, C, F8, true>, grid, block, 0, s, a)        \
+  return stream ? launch(ki, gnorm_fwd_kernel<T, C, F8, sizeof(T) == 2>, grid, block, 0, s, a) \
                 : launch(ki, gnorm_fwd_kernel<T, C, F8, false>, grid, block, 0, s, a)
   switch (nch) {
     case 1: GNF(1);
@@ -651,7 +671,7 @@ namespace {
 
 template <typename T, int NCH, bool F8>
 orbit_status gnorm_bwd_run(const GnBwd& a, const KernelInfo& ki, int chunks, int threads, hipStream_t s) {
-  constexpr bool KEEP = sizeof(T) == 2 || NCH < 4, PF = sizeof(T) == 2;
+  constexpr bool KEEP = sizeof(T) == 2 || NCH < 3, PF = sizeof(T) == 2;
   constexpr int LDS = 512 * NCH * 64;
   const auto kern = gnorm_bwd_kernel<T, NCH, F8, KEEP, PF>;
   static const bool once = [&] {
@@ -667,9 +687,12 @@ orbit_status gnorm_bwd_run(const GnBwd& a, const KernelInfo& ki, int chunks, int
 template <typename T, bool F8>
 orbit_status gnorm_bwd_t(const GnBwd& a, const GnShape& h, const KernelInfo& ki, int chunks, hipStream_t s) {
   const int threads = h.G * h.tpr;
-  if (h.nch == 4) return gnorm_bwd_run<T, 4, F8>(a, ki, chunks, threads, s);
-  if (h.nch == 2) return gnorm_bwd_run<T, 2, F8>(a, ki, chunks, threads, s);
-  return gnorm_bwd_run<T, 1, F8>(a, ki, chunks, threads, s);
+  switch (h.nch) {
+    case 1: return gnorm_bwd_run<T, 1, F8>(a, ki, chunks, threads, s);
+    case 2: return gnorm_bwd_run<T, 2, F8>(a, ki, chunks, threads, s);
+    case 3: return gnorm_bwd_run<T, 3, F8>(a, ki, chunks, threads, s);
+    default: return gnorm_bwd_run<T, 4, F8>(a, ki, chunks, threads, s);
+  }
 }
 
 }  // namespace

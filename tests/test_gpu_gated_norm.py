@@ -118,7 +118,8 @@ def _check_backward(lib, z, p, t, dtype, f8=0, accumulate=0, dy=True):
 
 
 SHAPES = [(1, 8, 1), (1, 2048, 1), (3, 40, 3), (4, 512, 2), (7, 1000, 1), (6, 1032, 3), (37, 2056, 0), (10, 4104, 2),
-          (5, 8200, 1), (3, 16384, 3), (515, 128, 5), (300, 1024, 4)]
+          (5, 8200, 1), (3, 16384, 3), (515, 128, 5), (300, 1024, 4),
+          (9, 520, 0), (5, 8192, 1), (2, 12288, 2), (3, 12296, 1), (1100, 1040, 1)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -160,6 +161,29 @@ def test_gate_per_row_and_hard_rows(lib, dtype):
     t["f"][6] = 0.0
     _check_forward(lib, z, p, t, dtype)
     _check_backward(lib, z, p, t, dtype)
+
+
+def test_streamed_rows(lib):
+    """From 96 MB of tensors on bf16 rows are loaded non-temporally: the same results, checked on some rows."""
+    z, p, t = _case(6144, 2056, 3, 1, 1, "bf16", seed=14)
+    y, h, stats, _ = _forward(lib, z, p, t, "bf16")
+    pick = torch.tensor([0, 1, 2047, 2048, 4096, 6143])
+    zs = dict(z, rows=len(pick), gate_rows=len(pick))
+    ps = dict(_64(p), gate=p["gate"].double()[pick // 2048])
+    ry, rh, ty, th = R.gated_norm_tol(zs, ps, t["x"].double()[pick], t["f"].double()[pick], R.HALF["bf16"])
+    _within(y[pick.cuda()], ry, ty, "y")
+    _within(h[pick.cuda()], rh, th, "h")
+    dx, df, g = _backward(lib, z, p, t, y, stats, "bf16")
+    rx, rf, rg = R.gated_norm_grad_ref(z, _64(p), t["f"].double(), y.cpu().double(), t["dh"].double(), t["dy"].double())
+    tx, tf, tg = R.gated_norm_grad_tol(z, _64(p), t["f"].double(), y.cpu().double(), t["dh"].double(), t["dy"].double(),
+                                       R.HALF["bf16"])
+    # the statistics are those of the unrounded y: its rounding moves the mean and the deviation by at most
+    # 2^-8 of the row's mean |y| and |y|^2 (halved at random signs; no more than that is allowed here)
+    slack = 2.0 ** -8
+    assert float((dx.cpu().double() - rx).norm()) <= slack * float(rx.norm())
+    assert float((df.cpu().double() - rf).norm()) <= slack * float(rf.norm())
+    for k in g:
+        assert float((g[k].cpu().double() - rg[k]).norm()) <= slack * float(rg[k].norm()), k
 
 
 def test_many_rows(lib):
