@@ -591,10 +591,12 @@ __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
 
 // The backward's launch shape. A thread owns one, two or four pieces (a row of up
 // to 2048 columns is a wave's), three from 8193 to 12288 columns, so that all 512
-// threads of a block have some; a block takes as many rows at once as that
-// gives. Chunks: about one per CU, in whole turns of the block's groups and of
-// at least 8 rows: more of them cost more partial rows than they hide latency
-// (8192 x 1024: 31 us, with 512 chunks 37).
+// threads of a block have some; float32 stays at two up to 8192 columns, which
+// its registers hold (4096 x 2048: 61 -> 55 us). A block takes as many rows at
+// once as that gives. Chunks: about one per CU, in whole turns of the block's
+// groups. More of them cost more partial rows than they hide latency (bf16 8192
+// x 1024: 31 us, with 512 chunks 37), fewer leave CUs idle where rows are few
+// (256 x 16384: 45 us, 84 with at least 8 rows a chunk).
 // pieces of 8 columns per thread
 int gn_pieces(int n) { return n <= 512 ? 1 : n <= 1024 ? 2 : n > 8192 && n <= 12288 ? 3 : 4; }
 
@@ -603,11 +605,11 @@ struct GnShape {
 };
 GnShape gn_shape(const GnormDims& z) {
   GnShape h{};
-  h.nch = gn_pieces(z.n);
+  h.nch = z.dt == ORBIT_F32 && z.n > 512 && z.n <= 8192 ? 2 : gn_pieces(z.n);
   h.tpr = (int)(cdiv(cdiv(z.n, 8 * h.nch), 64) * 64);
   h.G = 512 / h.tpr;
   h.rpg = z.rows / std::max(1, z.gates);
-  const int turns = std::max<int>({1, (8 + h.G - 1) / h.G, (z.rows + 128 * h.G) / (256 * h.G)});
+  const int turns = std::max(1, (int)(((int64_t)z.rows + 128 * h.G) / (256 * h.G)));
   h.rpb = std::min(h.rpg, turns * h.G);
   h.G = std::min(h.G, h.rpb);
   h.cpg = (int)cdiv(h.rpg, h.rpb);
@@ -671,7 +673,7 @@ namespace {
 
 template <typename T, int NCH, bool F8>
 orbit_status gnorm_bwd_run(const GnBwd& a, const KernelInfo& ki, int chunks, int threads, hipStream_t s) {
-  constexpr bool KEEP = sizeof(T) == 2 || NCH < 3, PF = sizeof(T) == 2;
+  constexpr bool KEEP = sizeof(T) == 2 || NCH < 4, PF = sizeof(T) == 2;
   constexpr int LDS = 512 * NCH * 64;
   const auto kern = gnorm_bwd_kernel<T, NCH, F8, KEEP, PF>;
   static const bool once = [&] {
