@@ -413,7 +413,8 @@ typedef struct {
 typedef struct { float *gate, *post_g, *post_b, *pre_g, *pre_b; } orbit_gated_norm_grads;
 
 /* f given: read from f; store (may be NULL) receives f in 8 bits. f NULL: f is
- * read from the store. x may not alias y or h. h: NULL without pre_norm.
+ * read from the store. y and h may not alias x, f or each other. h: unused
+ * without pre_norm.
  * stats [rows, 4] float32 receives mean and 1 / sqrt(variance + eps) of f
  * (zeros without post_norm) and of y (zeros without pre_norm). */
 orbit_status orbit_gated_norm_fwd(const orbit_gated_norm_desc* desc, const orbit_gated_norm_params* p, const void* x,
@@ -422,7 +423,7 @@ orbit_status orbit_gated_norm_fwd(const orbit_gated_norm_desc* desc, const orbit
 
 size_t orbit_gated_norm_bwd_workspace_bytes(const orbit_gated_norm_desc* desc);
 /* Gradients dx, df [rows, n] (dtype) and of the parameters from dh (gradient
- * of h; NULL without pre_norm) and dy (gradient of y from its other readers;
+ * of h; unused without pre_norm) and dy (gradient of y from its other readers;
  * NULL: none, with pre_norm only), given f or its store (as in the forward;
  * both may be NULL without post_norm and gate), the forward's y (may be NULL
  * without pre_norm) and stats. dx is the whole gradient of y and may be NULL.

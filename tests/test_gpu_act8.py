@@ -98,6 +98,21 @@ def test_unpack_gelu(lib, rows, n, pad, with_u, dtype):
     assert (err <= tol).all(), float((err - tol).max())
 
 
+def test_unpack_two_leading_dimensions(lib):
+    """x without gaps beside a GELU with them, and the other way round."""
+    rows, n = 19, 96
+    x = torch.randn(rows, n, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    store, _ = _packed(lib, x)
+    ref = torch.empty(2, rows, n, dtype=torch.bfloat16, device="cuda")
+    lib.orbit_act8_unpack(1, rows, n, store, ref[0], n, ref[1], n)
+    for lx, lg in ((n, n + 40), (n + 8, n)):
+        u = torch.full((rows, lx), 4.0, dtype=torch.bfloat16, device="cuda")
+        g = torch.full((rows, lg), 4.0, dtype=torch.bfloat16, device="cuda")
+        lib.orbit_act8_unpack(1, rows, n, store, u, lx, g, lg)
+        assert torch.equal(u[:, :n], ref[0]) and torch.equal(g[:, :n], ref[1])
+        assert bool((u[:, n:] == 4).all()) and bool((g[:, n:] == 4).all())
+
+
 @pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("rows,K,N", [(1, 8, 8), (1, 64, 40), (31, 40, 200), (100, 1000, 72), (513, 256, 1024), (2048, 520, 136)])
 @pytest.mark.parametrize("accumulate", [0, 1])
@@ -129,9 +144,10 @@ def test_weight_grad(lib, rows, K, N, accumulate, dtype):
     assert torch.equal(again, dw) or ((again - dw).abs().cpu().double() <= 2 * tol_w).all()
 
 
-def test_far_offsets(lib):
+@pytest.mark.parametrize("n", [32768, 32776])
+def test_far_offsets(lib, n):
     """A store past 2^31 bytes, its values past 2^32: the last rows read back as they were."""
-    rows, n = 70000, 32776
+    rows = 70000
     x = torch.zeros(rows, n, dtype=torch.bfloat16, device="cuda")
     x[-3:] = torch.randn(3, n, generator=torch.Generator().manual_seed(9)).to(torch.bfloat16).cuda()
     x[0] = 1.0

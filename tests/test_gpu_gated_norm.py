@@ -186,6 +186,53 @@ def test_streamed_rows(lib):
         assert float((g[k].cpu().double() - rg[k]).norm()) <= slack * float(rg[k].norm()), k
 
 
+@pytest.mark.parametrize("f8", [0, 1])
+def test_far_offsets(lib, f8):
+    """Tensors of 4.6 GB: rows past 2^31 values give what the same rows give alone."""
+    rows, n, last = 140000, 16384, 3
+    z, p, t = _case(last, n, 1, 1, 1, "bf16", seed=15)
+    small = _forward(lib, z, p, t, "bf16", 2 if f8 else 0)
+    sdx, sdf, _ = _backward(lib, z, p, t, small[0], small[2], "bf16", small[3])
+    P = _d(p)
+    big = {k: torch.zeros(rows, n, dtype=torch.bfloat16, device="cuda") for k in ("x", "f", "dh", "dy")}
+    for k in big:
+        big[k][-last:] = t[k].cuda()
+    zb = dict(z, rows=rows)
+    store = None
+    if f8:
+        store = torch.empty(lib.orbit_act8_bytes(rows, n), dtype=torch.uint8, device="cuda")
+        lib.orbit_act8_pack(1, rows, n, big["f"], n, store)
+    f = None if f8 else big["f"]
+    y, h = (torch.empty(rows, n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    stats = torch.empty(rows, 4, device="cuda")
+    lib.orbit_gated_norm_fwd(_desc(zb, "bf16"), P, big["x"], f, store, y, h, stats)
+    assert torch.equal(y[-last:], small[0]) and torch.equal(h[-last:], small[1])
+    assert torch.equal(stats[-last:], small[2])
+    ws = torch.empty(lib.orbit_gated_norm_bwd_workspace_bytes(_desc(zb, "bf16")), dtype=torch.uint8, device="cuda")
+    dx, df = h, torch.empty_like(h)
+    lib.orbit_gated_norm_bwd(_desc(zb, "bf16"), P, f, store, y, stats, big["dh"], big["dy"], dx, df, _grads(p), 0, ws)
+    assert torch.equal(dx[-last:], sdx) and torch.equal(df[-last:], sdf)
+
+
+def test_two_streams_at_once(lib):
+    """Calls in flight on two streams, each with its own buffers, give what they give alone."""
+    cases = [_case(900, 2056, 3, 1, 1, "bf16", seed=s) for s in (16, 17)]
+    runs = []
+    for z, p, t in cases:
+        y, _, stats, _ = _forward(lib, z, p, t, "bf16")
+        alone = _backward(lib, z, p, t, y, stats, "bf16")
+        D = {k: v.cuda() for k, v in t.items()}
+        ws = torch.empty(lib.orbit_gated_norm_bwd_workspace_bytes(_desc(z, "bf16")), dtype=torch.uint8, device="cuda")
+        runs.append((z, _d(p), D, y, stats, torch.empty_like(y), torch.empty_like(y), _grads(p), ws, alone, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for z, P, D, y, stats, dx, df, g, ws, _, s in runs:
+            lib.orbit_gated_norm_bwd(_desc(z, "bf16"), P, D["f"], None, y, stats, D["dh"], D["dy"], dx, df, g, 0, ws, stream=s)
+    torch.cuda.synchronize()
+    for _, _, _, _, _, dx, df, g, _, alone, _ in runs:
+        assert torch.equal(dx, alone[0]) and torch.equal(df, alone[1]) and all(torch.equal(g[k], alone[2][k]) for k in g)
+
+
 def test_many_rows(lib):
     """More rows than chunks of one size: ragged last chunks per gate row."""
     z, p, t = _case(3 * 1371, 72, 3, 1, 1, "f32", seed=6)
