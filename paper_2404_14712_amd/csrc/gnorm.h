@@ -26,8 +26,9 @@ orbit_status gnorm_fwd(const GnormDims& z, const GnormParams& p, const void* x, 
 
 // dh (null without the pre norm) and dy (null: zero) -> dx (may be null; the
 // gradient of x and of y's other readers together) and df (may be null without
-// the post norm and a gate), and the float32 parameter gradients. f == nullptr: from the store; neither is read without
-// the post norm and a gate. ws: gnorm_bwd_ws_bytes.
+// the post norm and a gate), and the float32 parameter gradients. f == nullptr:
+// from the store; neither is read without the post norm and a gate. ws:
+// gnorm_bwd_ws_bytes.
 size_t gnorm_bwd_ws_bytes(const GnormDims& z);
 struct GnormGrads {
   float *gate, *post_g, *post_b, *pre_g, *pre_b;

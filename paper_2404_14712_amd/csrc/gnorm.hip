@@ -207,8 +207,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
 //   d post_b = scale sum_G gate S1, d post_g = scale sum_G gate S2,
 //   d gate = scale (pg S2 + pb S1), or scale S2.
 // A block takes a chunk of rpb rows of one gate row and stores a partial row
-// of each of its four column sums; gnorm_final and ColFinal add the partials
-// in a fixed order.
+// of each of its four column sums; gnorm_final adds the partials in a fixed
+// order.
 struct GnBwd {
   const void *f, *y, *dh, *dy, *gate, *post_g, *pre_g;
   const uint8_t *fc, *fe;
@@ -237,9 +237,8 @@ struct GnRow {
 // register file at full width; the two of the pre norm live in LDS. That leaves
 // room for the next row's dh and y (PF, bf16), so that loads are in flight all
 // the time; its dy and f follow into the registers of the current row's once
-// these are used up. KEEP:
-// values stay in registers from their one load; the widest float32 rows are
-// loaded again where they are used instead.
+// these are used up. KEEP: values stay in registers from their one load; the
+// widest float32 rows are loaded again where they are used instead.
 template <typename T, int NCH, bool F8, bool KEEP, bool PF>
 __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   using Row = GnRow<T, NCH, F8>;
@@ -249,7 +248,9 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   // 126 us, float32 1024 x 16384: 167 -> 231)
   constexpr int AUX = sizeof(T) == 2 ? 2 : 0;
   constexpr int PIECES = NT * NCH;
-  __shared__ float red[2][NT / 64][2];
+  // wave sums: [turn parity][norm][wave]. By parity, as with one norm alone only
+  // one barrier lies between a turn's reads and the next turn's writes
+  __shared__ float red[2][2][NT / 64][2];
   // column sums: half h of a thread's piece c of sum k at (2 k + h) PIECES +
   // c NT + thread, so that consecutive lanes touch consecutive 16 bytes and the
   // offsets are constants
@@ -262,7 +263,8 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
   const int n = a.n, chunks = (int)gridDim.x, row_bytes = n * (int)sizeof(T);
   const int gi = (int)blockIdx.x / a.cpg, ci = (int)blockIdx.x % a.cpg;
-  const int r0 = gi * a.rpg + ci * a.rpb, r1 = min((gi + 1) * a.rpg, r0 + a.rpb);
+  const int64_t r0 = (int64_t)gi * a.rpg + (int64_t)ci * a.rpb;
+  const int64_t r1 = min((int64_t)(gi + 1) * a.rpg, r0 + a.rpb);
   const bool post = a.post, pre = a.pre, rf = post || a.gate;  // rf: f is read
   // an absent gain or gate is 1: its zeros or-ed with the bits of 1
   const RowBuf pre_g(a.pre_g, 0, pre ? row_bytes : 0), post_g(a.post_g, 0, post ? row_bytes : 0);
@@ -283,19 +285,19 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     for (int h = 0; h < 2; ++h) s2[c][h] = s3[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float inv_n = 1.f / (float)n;
   // sums of two values over the row's threads; every thread of the block calls
-  auto row_sum2 = [&](int k, float& u, float& v) {
+  auto row_sum2 = [&](int par, int k, float& u, float& v) {
     u = wave_add(u);
     v = wave_add(v);
     if (wpg > 1) {
       if (lane == 0) {
-        red[k][wave][0] = u;
-        red[k][wave][1] = v;
+        red[par][k][wave][0] = u;
+        red[par][k][wave][1] = v;
       }
       __syncthreads();
       u = v = 0.f;
       for (int w = q * wpg; w < (q + 1) * wpg; ++w) {
-        u += red[k][w][0];
-        v += red[k][w][1];
+        u += red[par][k][w][0];
+        v += red[par][k][w][1];
       }
     }
   };
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
         }
         if (NCH > 2) __builtin_amdgcn_sched_barrier(0);  // one piece's temporaries at a time
       }
-      row_sum2(0, m1, m2);
+      row_sum2(it & 1, 0, m1, m2);
       m1 *= inv_n;
       m2 *= inv_n;
     }
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     if (KEEP && !PF) fetch_h(nxt);
     if (KEEP) fetch_d(nxt);
     if (post) {
-      row_sum2(1, m3, m4);
+      row_sum2(it & 1, 1, m3, m4);
       m3 *= inv_n;
       m4 *= inv_n;
       if (!KEEP) fetch_f(cur);

@@ -152,6 +152,21 @@ def test_parts(lib, post, pre, gates, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("post,pre,gates", [(0, 1, 0), (1, 0, 1), (0, 1, 4)])
+@pytest.mark.parametrize("rows,n", [(1100, 8200), (2000, 4104)])
+def test_one_norm_over_many_turns(lib, rows, n, post, pre, gates, dtype):
+    """One norm alone, rows of several waves and chunks of several turns: a turn's wave sums are read
+    before the next turn's overwrite them, every time."""
+    z, p, t = _case(rows, n, gates, post, pre, dtype, seed=18)
+    dx, df, g = _check_backward(lib, z, p, t, dtype)
+    y, _, stats, _ = _forward(lib, z, p, t, dtype)
+    for _ in range(3):
+        dx2, df2, g2 = _backward(lib, z, p, t, y, stats, dtype)
+        dx3, df3, g3 = _backward(lib, z, p, t, y, stats, dtype)
+        assert torch.equal(dx2, dx3) and torch.equal(df2, df3) and all(torch.equal(g2[k], g3[k]) for k in g)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gate_per_row_and_hard_rows(lib, dtype):
     """A gate row for each token; rows far from zero, constant rows, empty (zero) rows."""
     z, p, t = _case(33, 328, 33, 1, 1, dtype, seed=5, mean=50.0)
