@@ -78,9 +78,10 @@ class ViTPass:
         (Sec. III-B): the forward keeps only each block's input and the backward
         recomputes the rest (orbit_vit_block_bwd with saved = NULL). "act8": the
         forward keeps the blocks' activations in 8 bits
-        (orbit_vit_block_ext_fwd with act8)."""
-        if checkpoint not in (False, True, "act8"):
+        (orbit_vit_block_ext_fwd with act8). Other values count by their truth."""
+        if isinstance(checkpoint, str) and checkpoint != "act8":
             raise ValueError(f"checkpoint must be False, True or 'act8', not {checkpoint!r}")
+        act8 = isinstance(checkpoint, str)
         self.lib, self.z, self.dev = lib, dims, torch.device(device)
         self.checkpoint = checkpoint
         z = dims
@@ -89,7 +90,7 @@ class ViTPass:
         code = _code(z.dtype)
         self.params = params
         self.bdesc = BlockDesc(z.B, z.L, z.d, z.heads, z.head_dim, z.mlp, z.qk_norm, z.eps, code)
-        self.bext = BlockExt(int(checkpoint == "act8"), z.post_norm, z.gate_rows, z.res_scale)
+        self.bext = BlockExt(int(act8), z.post_norm, z.gate_rows, z.res_scale)
         ws = lib.orbit_vit_block_ext_workspace_bytes(self.bdesc, self.bext)
         if ws == 0:
             raise ValueError(f"invalid block description: {lib.last_error()}")
@@ -97,7 +98,7 @@ class ViTPass:
         E = lambda *shape, dt=tdt: torch.empty(*shape, dtype=dt, device=self.dev)
         F32 = lambda *shape: torch.zeros(*shape, dtype=torch.float32, device=self.dev)
         self.xs = [E(z.B, z.L, z.d) for _ in range(z.blocks + 1)]
-        self.saved = [None if checkpoint is True else torch.empty(sb, dtype=torch.uint8, device=self.dev)
+        self.saved = [None if checkpoint and not act8 else torch.empty(sb, dtype=torch.uint8, device=self.dev)
                       for _ in range(z.blocks)]
         self.dxa = E(z.B, z.L, z.d)
         self.dxb = E(z.B, z.L, z.d)

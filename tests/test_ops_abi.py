@@ -227,3 +227,23 @@ def test_block_ext_reference_by_autograd(post, gates):
     assert set(gr) == set(p)
     for k in p:
         assert torch.allclose(gr[k], leaf[k].grad, rtol=1e-9, atol=1e-11), k
+
+
+@pytest.mark.parametrize("checkpoint,kept", [(False, "full"), (None, "full"), (0, "full"), (True, None), (1, None),
+                                             (np.True_, None), ("act8", "small")])
+def test_pass_checkpoint_values(lib, checkpoint, kept):
+    """What a pass keeps of its blocks: any value but "act8" counts by its truth."""
+    from paper_2404_14712_amd.model import PassDims, ViTPass
+    dims = PassDims("blocks", "bf16", 1, 4, 64, 1, 2, 32, 128)
+    vp = ViTPass(lib, dims, {"blocks": [{}]}, device="cpu", checkpoint=checkpoint)
+    want = {"full": lambda: lib.orbit_vit_block_saved_bytes(vp.bdesc),
+            "small": lambda: lib.orbit_vit_block_ext_saved_bytes(vp.bdesc, L.BlockExt(1, 0, 0, 1.0))}
+    got = [None if s is None else s.numel() for s in vp.saved]
+    assert got == [want[kept]() if kept else None]
+
+
+def test_pass_checkpoint_refusal(lib):
+    from paper_2404_14712_amd.model import PassDims, ViTPass
+    with pytest.raises(ValueError, match="checkpoint"):
+        ViTPass(lib, PassDims("blocks", "bf16", 1, 4, 64, 1, 2, 32, 128), {"blocks": [{}]}, device="cpu",
+                checkpoint="full")
