@@ -371,7 +371,7 @@ orbit_status orbit_layernorm_fwd(int32_t dtype, int32_t rows, int32_t n, const v
  * holds an infinity or a NaN has E = 0 and reads back as NaN.
  * In memory: the codes [rows, n], from the next multiple of 256 bytes on the
  * E [rows, (n + 31) / 32], the whole a multiple of 256 bytes. */
-size_t orbit_act8_bytes(int64_t rows, int32_t n); /* 0 on bad sizes */
+size_t orbit_act8_bytes(int64_t rows, int32_t n); /* 0 on bad sizes, and from 2^34 values on */
 /* x[rows, n] (dtype, leading dimension ldx >= n, a multiple of 8) -> store */
 orbit_status orbit_act8_pack(int32_t dtype, int64_t rows, int32_t n, const void* x, int64_t ldx, void* store,
                              size_t store_bytes, void* stream);
@@ -381,7 +381,8 @@ orbit_status orbit_act8_unpack(int32_t dtype, int64_t rows, int32_t n, const voi
                                int64_t ldx, void* gelu, int64_t ldgelu, void* stream);
 /* Weight and bias gradient of a linear layer whose input x[rows, K] is in a
  * store: dw[K, N] = X^T dy, db[N] = column sums of dy (db may be NULL), with
- * dy[rows, N] of dtype, leading dimension lddy. K and N are multiples of 8. */
+ * dy[rows, N] of dtype, leading dimension lddy. K and N are multiples of 8, K
+ * and lddy below 2^25. */
 size_t orbit_act8_weight_grad_workspace_bytes(int32_t dtype, int32_t rows, int32_t K, int32_t N);
 orbit_status orbit_act8_weight_grad(int32_t dtype, int32_t rows, int32_t K, int32_t N, const void* store,
                                     size_t store_bytes, const void* dy, int64_t lddy, float* dw, float* db,
@@ -397,7 +398,7 @@ orbit_status orbit_act8_weight_grad(int32_t dtype, int32_t rows, int32_t K, int3
  *   h = LN(y) pre_g + pre_b       (only with pre_norm: the next product's input)
  * gate [gate_rows, n]: row t uses gate row t / (rows / gate_rows), so that 1 is
  * a learned gate per channel and B one per sample of [B, L, n]; gate_rows
- * divides rows. n is a multiple of 8 up to 16384. LayerNorms use the biased
+ * divides rows. n is a multiple of 8 up to 16384, rows at most 2^26 - 64. LayerNorms use the biased
  * variance and eps. Each LayerNorm normalises the float32 value. */
 typedef struct {
   int32_t rows, n, gate_rows, post_norm, pre_norm;

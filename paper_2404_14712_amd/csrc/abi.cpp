@@ -1215,10 +1215,13 @@ orbit_status orbit_layernorm_fwd(int32_t dtype, int32_t rows, int32_t n, const v
 // ---------------------------------------------------------------------------
 // activations stored in 8 bits
 // ---------------------------------------------------------------------------
+// a launch has fewer than 2^32 threads along a dimension, at 8 values per thread
+static constexpr int64_t kAct8Values = 1ll << 34;
+
 static orbit_status act8_check(const char* fn, int64_t rows, int32_t n, const void* store, size_t bytes) {
   REQ(rows > 0 && n > 0 && n % 8 == 0, ORBIT_E_ARG, "%s: bad sizes rows=%lld n=%d (n must be a multiple of 8)", fn,
       (long long)rows, n);
-  REQ(rows < (1ll << 40) / n, ORBIT_E_UNSUPPORTED, "%s: rows=%lld x n=%d exceeds 2^40 values", fn, (long long)rows, n);
+  REQ(rows < kAct8Values / n, ORBIT_E_UNSUPPORTED, "%s: rows=%lld x n=%d exceeds 2^34 values", fn, (long long)rows, n);
   PTR(store, "store");
   REQ(bytes >= act8_store_bytes(rows, n), ORBIT_E_ARG, "%s: store of %zu bytes is smaller than the %zu required", fn,
       bytes, act8_store_bytes(rows, n));
@@ -1226,7 +1229,7 @@ static orbit_status act8_check(const char* fn, int64_t rows, int32_t n, const vo
 }
 
 size_t orbit_act8_bytes(int64_t rows, int32_t n) {
-  if (rows <= 0 || n <= 0 || n % 8 != 0 || rows >= (1ll << 40) / n) {
+  if (rows <= 0 || n <= 0 || n % 8 != 0 || rows >= kAct8Values / n) {
     set_error("orbit_act8_bytes: bad sizes rows=%lld n=%d", (long long)rows, n);
     return 0;
   }
@@ -1268,6 +1271,9 @@ struct Act8GradWs {
   size_t gws_bytes;
 };
 
+// the product addresses slices of 32 rows of each operand with 31-bit byte offsets
+constexpr int64_t kGradLd = 1ll << 25;
+
 Gemm act8_grad_gemm(int32_t dtype, int32_t rows, int32_t K, int32_t N) {
   Gemm g;
   g.dtype = (orbit_dtype)dtype; g.tag = "act8_dw";
@@ -1292,6 +1298,7 @@ orbit_status act8_grad_check(const char* fn, int32_t dtype, int32_t rows, int32_
   ORBIT_TRY(check_dtype(fn, dtype));
   REQ(rows > 0 && K > 0 && N > 0 && K % 8 == 0 && N % 8 == 0, ORBIT_E_ARG,
       "%s: bad sizes rows=%d K=%d N=%d (K and N must be multiples of 8)", fn, rows, K, N);
+  REQ(K < kGradLd, ORBIT_E_UNSUPPORTED, "%s: K=%d exceeds 2^25", fn, K);
   return ORBIT_OK;
 }
 
@@ -1311,6 +1318,7 @@ orbit_status orbit_act8_weight_grad(int32_t dtype, int32_t rows, int32_t K, int3
   ORBIT_TRY(act8_check(fn, rows, K, store, store_bytes));
   PTR(dy, "dy"); PTR(dw, "dw"); OPT_PTR(db, "db"); PTR(ws, "ws");
   REQ(lddy >= N && lddy % 8 == 0, ORBIT_E_ARG, "%s: lddy must be >= N and a multiple of 8", fn);
+  REQ(lddy < kGradLd, ORBIT_E_UNSUPPORTED, "%s: lddy=%lld exceeds 2^25", fn, (long long)lddy);
   REQ(accumulate == 0 || accumulate == 1, ORBIT_E_ARG, "%s: accumulate must be 0 or 1", fn);
   Act8GradWs w;
   const size_t need = act8_grad_ws(dtype, rows, K, N, ws, &w);
@@ -1344,6 +1352,8 @@ static orbit_status gnorm_check(const char* fn, const orbit_gated_norm_desc* des
   REQ(d.rows > 0 && d.n > 0 && d.n % 8 == 0, ORBIT_E_ARG, "%s: bad sizes rows=%d n=%d (n must be a multiple of 8)", fn,
       d.rows, d.n);
   REQ(d.n <= 16384, ORBIT_E_UNSUPPORTED, "%s: n=%d exceeds 16384", fn, d.n);
+  // a launch has fewer than 2^32 threads, at a wave per row
+  REQ(d.rows <= (1 << 26) - 64, ORBIT_E_UNSUPPORTED, "%s: rows=%d exceeds 2^26 - 64", fn, d.rows);
   REQ((d.post_norm == 0 || d.post_norm == 1) && (d.pre_norm == 0 || d.pre_norm == 1), ORBIT_E_ARG,
       "%s: post_norm and pre_norm must be 0 or 1", fn);
   REQ(d.gate_rows >= 0 && (d.gate_rows == 0 || d.rows % d.gate_rows == 0), ORBIT_E_ARG,

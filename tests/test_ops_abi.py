@@ -247,3 +247,22 @@ def test_pass_checkpoint_refusal(lib):
     with pytest.raises(ValueError, match="checkpoint"):
         ViTPass(lib, PassDims("blocks", "bf16", 1, 4, 64, 1, 2, 32, 128), {"blocks": [{}]}, device="cpu",
                 checkpoint="full")
+
+
+def test_refusals_of_the_largest_sizes(lib):
+    """Sizes whose launches or offsets would not fit are refused before anything is launched."""
+    c, big = lib.lib, 1 << 50
+    edge = (1 << 34) // 1024
+    assert lib.orbit_act8_bytes(edge, 1024) == 0 and lib.orbit_act8_bytes(edge - 1, 1024) > 0
+    assert c.orbit_act8_pack(1, edge, 1024, 0x100, 1024, 0x200, big, None) == L.ORBIT_E_UNSUPPORTED
+    assert c.orbit_act8_unpack(1, edge, 1024, 0x200, big, 0x100, 1024, None, 0, None) == L.ORBIT_E_UNSUPPORTED
+    wg = (1, 4, 40, 16, 0x100, big, 0x200, 16, 0x300, 0x400, 0, 0x500, big, None)
+    assert c.orbit_act8_weight_grad(*wg[:7], 1 << 25, *wg[8:]) == L.ORBIT_E_UNSUPPORTED and "lddy" in lib.last_error()
+    assert c.orbit_act8_weight_grad(*wg[:2], 1 << 25, *wg[3:]) == L.ORBIT_E_UNSUPPORTED and "K=" in lib.last_error()
+    assert lib.orbit_act8_weight_grad_workspace_bytes(1, 4, 1 << 25, 16) == 0
+    for rows, n in ((1 << 26, 8), ((1 << 26) - 63, 8)):
+        d = _desc(rows=rows, n=n, gate_rows=1)
+        assert _fwd(lib, d) == L.ORBIT_E_UNSUPPORTED and "rows" in lib.last_error()
+        assert _bwd(lib, d) == L.ORBIT_E_UNSUPPORTED
+        assert lib.orbit_gated_norm_bwd_workspace_bytes(d) == 0
+    assert lib.orbit_gated_norm_bwd_workspace_bytes(_desc(rows=(1 << 26) - 64, n=8, gate_rows=1)) > 0
