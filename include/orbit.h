@@ -131,13 +131,16 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
  * ones). The rest, shards included, is orbit_vit_block_fwd's, whose result this
  * is, bit for bit, with act8 = post_norm = gate_rows = 0 and scale 1.
  * act8 = 1: `saved` holds q, k, v, o, u and the sub-layers' outputs as 8-bit
- * stores (see orbit_act8_bytes below) and the softmax normalisers in float32:
- * about a fifth of the bytes in bf16. The forward's result does not depend on
- * it, bit for bit; the backward reads the stores back into its workspace, forms x1 and the
- * norms' and GELU's outputs from them, and runs as from stored tensors, so that
- * its gradients carry the stores' rounding (at most half a step of a group of
- * 32 values, below 2^-7 of its largest). saved == NULL is inference, and
- * activation checkpointing without that rounding, as in the plain calls. */
+ * stores (see orbit_act8_bytes below): about a fifth of the bytes in bf16. The
+ * forward's result does not depend on it, bit for bit; the backward reads the
+ * stores back into its workspace, forms x1 and the outputs of the norms, the
+ * GELU and the attention from them, and runs as from stored tensors. Its
+ * gradients are those at the stored values. The attention's are of the softmax
+ * of the stored q and k: the stores' rounding moves a score by up to some 2^-7
+ * of |q| |k| / sqrt(head_dim) and a probability by the exponential of that, so
+ * that with scores far in the tens the gradients of q, k and v are rough.
+ * saved == NULL is inference, and activation checkpointing without any such
+ * rounding, as in the plain calls. */
 typedef struct {
   int32_t act8, post_norm, gate_rows;
   float scale;

@@ -137,8 +137,7 @@ BlockSaved carve_block_saved(const BlockDims& z, const BlockExt& x, void* base, 
     s.qr = c.take<float>(z.T * 2 * z.H);
   }
   s.o = c.take<char>(z.T * z.A * e);
-  // a stored 8-bit o is exact in bf16: no float32 copy to keep beside it
-  s.o32 = z.dt == ORBIT_BF16 && !x.act8 ? c.take<float>(z.T * z.A) : nullptr;
+  s.o32 = z.dt == ORBIT_BF16 ? c.take<float>(z.T * z.A) : nullptr;
   s.lse = c.take<float>(z.T * z.H);
   s.x1 = c.take<char>(z.T * z.d * e);
   s.mu2 = c.take<float>(z.T);
@@ -151,11 +150,12 @@ BlockSaved carve_block_saved(const BlockDims& z, const BlockExt& x, void* base, 
 }
 
 // Saved tensors in 8 bits (act8.h). h1 and h2 are formed again by their norms,
-// g by the GELU, x1 from x and the store of f1; lse and f2's statistics stay
-// float32.
+// g by the GELU, x1 from x and the store of f1; f2's statistics stay float32.
+// The store of o is the projection's input; the attention's backward reads the
+// o and lse that the restored q, k, v give (block_restore).
 struct BlockSaved8 {
   void *qkv, *o, *f1, *u, *f2;  // f2: ext.branch() only
-  float *lse, *st2;
+  float* st2;
 };
 
 BlockSaved8 carve_block_saved8(const BlockDims& z, const BlockExt& x, void* base, size_t* used) {
@@ -166,7 +166,6 @@ BlockSaved8 carve_block_saved8(const BlockDims& z, const BlockExt& x, void* base
   s.f1 = c.take<char>(act8_store_bytes(z.T, z.d));
   s.u = c.take<char>(act8_store_bytes(z.T, z.F));
   if (x.branch()) s.f2 = c.take<char>(act8_store_bytes(z.T, z.d));
-  s.lse = c.take<float>(z.T * z.H);
   s.st2 = c.take<float>(z.T * 4);
   if (used) *used = c.used();
   return s;
@@ -275,6 +274,32 @@ GnormParams block_gnorm_params(const orbit_block_params* p, const orbit_block_ex
   return g;
 }
 
+// The attention's operands: q and k (through their norms where asked for) and v.
+AttnIO block_attn_io(const BlockDims& z, const BlockSaved& sv) {
+  const size_t e = esz(z.dt);
+  AttnIO io{};
+  io.B = z.B; io.H = z.H; io.L = z.L; io.dh = z.dh;
+  io.v = static_cast<char*>(sv.qkv) + 2 * z.A * e; io.ldv = 3 * z.A;
+  if (z.qk) {
+    io.q = sv.qkn; io.ldq = 2 * z.A; io.k = static_cast<char*>(sv.qkn) + z.A * e; io.ldk = 2 * z.A;
+  } else {
+    io.q = sv.qkv; io.ldq = 3 * z.A; io.k = static_cast<char*>(sv.qkv) + z.A * e; io.ldk = 3 * z.A;
+  }
+  return io;
+}
+
+// sv.qkv -> sv.o, sv.lse and o32 (may be null), with the norms of q and k.
+orbit_status block_attention(const BlockDims& z, const orbit_block_params* p, const BlockSaved& sv, float* o32,
+                             const BlockWs& w, hipStream_t s) {
+  if (z.qk)
+    ORBIT_TRY(qk_norm_fwd(z.dt, sv.qkv, 3 * z.A, sv.qkn, 2 * z.A, p->qn_g, p->qn_b, p->kn_g, p->kn_b, sv.qmu, sv.qr,
+                          (int)z.T, z.H, z.dh, z.eps, s));
+  // the attention backward's workspace is idle until it runs and holds the
+  // forward's split partials
+  return attn_fwd(z.dt, block_attn_io(z, sv), sv.o, z.A, sv.lse, o32, z.A, w.D,
+                  attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh), s);
+}
+
 // The forward's kernel sequence, writing the tensors the backward reads into
 // `sv`. With y == NULL the last product (fc2) is skipped where the backward
 // does not read its output: the recompute of the activation-checkpoint
@@ -284,7 +309,6 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
                                  const BlockSaved8* s8, const BlockWs& w, hipStream_t s) {
   const int T = (int)z.T;
   const orbit_dtype dt = z.dt;
-  float* lse = s8 ? s8->lse : sv.lse;
   ORBIT_TRY(layernorm_fwd(dt, x, z.d, p->ln1_g, p->ln1_b, sv.h1, z.d, sv.mu1, sv.r1, T, z.d, z.eps, s));
   {
     Gemm g; g.dtype = dt; g.tag = "qkv";
@@ -292,22 +316,8 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
     g.M = T; g.N = 3 * z.A; g.K = z.d; g.bias = p->b_qkv;
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
-  const size_t e = esz(dt);
-  AttnIO io{};
-  io.B = z.B; io.H = z.H; io.L = z.L; io.dh = z.dh;
-  io.v = static_cast<char*>(sv.qkv) + 2 * z.A * e; io.ldv = 3 * z.A;
-  if (z.qk) {
-    ORBIT_TRY(qk_norm_fwd(dt, sv.qkv, 3 * z.A, sv.qkn, 2 * z.A, p->qn_g, p->qn_b, p->kn_g, p->kn_b, sv.qmu, sv.qr,
-                          T, z.H, z.dh, z.eps, s));
-    io.q = sv.qkn; io.ldq = 2 * z.A;
-    io.k = static_cast<char*>(sv.qkn) + z.A * e; io.ldk = 2 * z.A;
-  } else {
-    io.q = sv.qkv; io.ldq = 3 * z.A;
-    io.k = static_cast<char*>(sv.qkv) + z.A * e; io.ldk = 3 * z.A;
-  }
-  // the attention backward's workspace is idle during the forward and holds
-  // the forward's split partials
-  ORBIT_TRY(attn_fwd(dt, io, sv.o, z.A, lse, sv.o32, z.A, w.D, attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh), s));
+  // the float32 o is for the backward, which forms it again from the stores
+  ORBIT_TRY(block_attention(z, p, sv, s8 ? nullptr : sv.o32, w, s));
   if (s8) {
     ORBIT_TRY(act8_pack(dt, sv.qkv, nullptr, 3 * z.A, T, 3 * z.A, s8->qkv, s));
     ORBIT_TRY(act8_pack(dt, sv.o, nullptr, z.A, T, z.A, s8->o, s));
@@ -354,17 +364,20 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
   return ORBIT_OK;
 }
 
-// The tensors the backward reads, from the 8-bit stores.
+// The tensors the backward reads, from the 8-bit stores. The attention runs
+// again over the restored q, k, v: the backward's probabilities exp(score - lse)
+// are a softmax, and its row sums dO o those of the same probabilities, only
+// with the lse and o of these very scores. With those of the exact ones a row
+// of probabilities sums to exp(score error), without bound as scores grow. The
+// projection's input, o of the forward, goes to o8.
 orbit_status block_restore(const BlockDims& z, const BlockExt& ext, const orbit_block_params* p,
                            const orbit_block_ext_params* ep, const void* x, const BlockSaved8& s8,
-                           const BlockSaved& sv, hipStream_t s) {
+                           const BlockSaved& sv, void* o8, const BlockWs& w, hipStream_t s) {
   const int T = (int)z.T;
   ORBIT_TRY(layernorm_fwd(z.dt, x, z.d, p->ln1_g, p->ln1_b, sv.h1, z.d, sv.mu1, sv.r1, T, z.d, z.eps, s));
   ORBIT_TRY(act8_unpack(z.dt, s8.qkv, T, 3 * z.A, sv.qkv, 3 * z.A, nullptr, 0, s));
-  if (z.qk)
-    ORBIT_TRY(qk_norm_fwd(z.dt, sv.qkv, 3 * z.A, sv.qkn, 2 * z.A, p->qn_g, p->qn_b, p->kn_g, p->kn_b, sv.qmu, sv.qr,
-                          T, z.H, z.dh, z.eps, s));
-  ORBIT_TRY(act8_unpack(z.dt, s8.o, T, z.A, sv.o, z.A, nullptr, 0, s));
+  ORBIT_TRY(block_attention(z, p, sv, sv.o32, w, s));
+  ORBIT_TRY(act8_unpack(z.dt, s8.o, T, z.A, o8, z.A, nullptr, 0, s));
   ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), x, nullptr, s8.f1, sv.x1, sv.h2, sv.st1,
                       s));
   return act8_unpack(z.dt, s8.u, T, z.F, sv.u, z.F, sv.g, z.F, s);
@@ -563,8 +576,10 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   BlockSaved8 s8{};
   if (restore) s8 = carve_block_saved8(z, ext, const_cast<void*>(saved), nullptr);
   if (recompute) ORBIT_TRY(block_forward_steps(z, ext, p, ep, x, nullptr, sv, nullptr, w, s));
-  if (restore) ORBIT_TRY(block_restore(z, ext, p, ep, x, s8, sv, s));
-  const float* lse = restore ? s8.lse : sv.lse;
+  // the projection's input; the store's goes to a buffer that is idle until the
+  // attention's backward
+  const void* o_proj = restore ? w.dqkv : sv.o;
+  if (restore) ORBIT_TRY(block_restore(z, ext, p, ep, x, s8, sv, w.dqkv, w, s));
   const int T = (int)z.T;
   const orbit_dtype dt = z.dt;
   const size_t e = esz(dt);
@@ -654,7 +669,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   }
   {
     Gemm g; g.dtype = dt; g.tag = "proj_dw";
-    g.A = sv.o; g.lda = z.A; g.a_kmajor = false; g.B = df1; g.ldb = z.d; g.b_kmajor = false;
+    g.A = o_proj; g.lda = z.A; g.a_kmajor = false; g.B = df1; g.ldb = z.d; g.b_kmajor = false;
     g.C = gr->w_proj; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
     g.M = z.A; g.N = z.d; g.K = T;
     const bool fused = !plain_ln2 && dw_bias(g, w.p_proj, gr->b_proj);
@@ -673,19 +688,12 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     g.C = w.dO; g.ldc = z.A; g.M = T; g.N = z.A; g.K = z.d;
     ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
   }
-  AttnIO io{};
-  io.B = z.B; io.H = z.H; io.L = z.L; io.dh = z.dh;
-  io.v = static_cast<char*>(sv.qkv) + 2 * z.A * e; io.ldv = 3 * z.A;
-  if (z.qk) {
-    io.q = sv.qkn; io.ldq = 2 * z.A; io.k = static_cast<char*>(sv.qkn) + z.A * e; io.ldk = 2 * z.A;
-  } else {
-    io.q = sv.qkv; io.ldq = 3 * z.A; io.k = static_cast<char*>(sv.qkv) + z.A * e; io.ldk = 3 * z.A;
-  }
+  const AttnIO io = block_attn_io(z, sv);
   char* dq = static_cast<char*>(w.dqkv);
   if (sv.o32)
-    ORBIT_TRY(attn_bwd(dt, io, sv.o32, z.A, 1, lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
+    ORBIT_TRY(attn_bwd(dt, io, sv.o32, z.A, 1, sv.lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
   else
-    ORBIT_TRY(attn_bwd(dt, io, sv.o, z.A, 0, lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
+    ORBIT_TRY(attn_bwd(dt, io, sv.o, z.A, 0, sv.lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
   if (z.qk) {
     ORBIT_TRY(qk_norm_bwd(dt, w.dqkv, 3 * z.A, sv.qkv, 3 * z.A, sv.qmu, sv.qr, p->qn_g, p->kn_g, gr->qn_g, gr->qn_b,
                           gr->kn_g, gr->kn_b, accumulate, T, z.H, z.dh, w.qws, &fin, s));

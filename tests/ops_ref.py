@@ -190,7 +190,8 @@ def block_ext_forward(x, p, H, z, qk=True, eps=1e-5):
 
 def block_ext_backward(x, p, H, z, c, dy, keep, qk=True, eps=1e-5):
     """Gradients from the tensors `keep(t)` makes of the forward's (identity: the exact gradients;
-    act8_values: those of 8-bit stores). The softmax normalisers and f2's statistics are the forward's."""
+    act8_values: those of 8-bit stores). The softmax is that of the kept q and k, and the o of its
+    backward their softmax's; f2's statistics are the forward's."""
     B, L, d = x.shape
     T = B * L
     flat = lambda t: t.reshape(T, -1)
@@ -251,8 +252,8 @@ def block_ext_backward(x, p, H, z, c, dy, keep, qk=True, eps=1e-5):
     if qk:
         q, k = ln_ref(q0, p["qn_g"], p["qn_b"], eps), ln_ref(k0, p["kn_g"], p["kn_b"], eps)
     dh = q.shape[-1]
-    P = torch.exp(q @ k.transpose(-1, -2).contiguous() / dh ** 0.5 - c["lse"])
-    dOh, oh = _heads(dO, H), _heads(o, H)
+    P = torch.softmax(q @ k.transpose(-1, -2).contiguous() / dh ** 0.5, -1)
+    dOh, oh = _heads(dO, H), P @ v
     dS = P * (dOh @ v.transpose(-1, -2).contiguous() - (dOh * oh).sum(-1, keepdim=True)) / dh ** 0.5
     dq, dk, dv = dS @ k, dS.transpose(-1, -2).contiguous() @ q, P.transpose(-1, -2).contiguous() @ dOh
     for name in ("qn_g", "qn_b", "kn_g", "kn_b"):
