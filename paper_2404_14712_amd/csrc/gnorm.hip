@@ -40,9 +40,11 @@ struct Raw8Q {
 
 // A block's G = blockDim / tpr groups of tpr threads take a row each; thread t
 // of a group owns the NCH 8-column pieces t + c tpr, so that a quad holds the 32
-// columns of a group of the store. Statistics: each thread's own mean and
-// squared deviations, merged pairwise over the wave, then over the row's waves
-// through LDS with one barrier. y is written rounded to the storage type, h and
+// columns of a group of the store. Statistics: each thread's own mean (corrected
+// by its deviations' sum, so that a constant's mean is that constant) and squared
+// deviations, merged pairwise over the wave, then over the row's waves through
+// LDS with one barrier. The mean is subtracted before anything is scaled: v r -
+// mean r would round at the mean's size. y is written rounded to the storage type, h and
 // the statistics come from its float32 value: h then carries one rounding
 // instead of two, and the backward's (rounded y - mean) differs from the exact
 // one by y's rounding alone.
@@ -121,22 +123,25 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[c][i];
-    float m = s * inv_own;
+    float m = s * inv_own, u = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
       if (on[c])
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float e = v[c][i] - m;
+          u += e;
           d = fmaf(e, e, d);
         }
+    m = fmaf(u, inv_own, m);
     wm.merge(m, d);
     if (wpg > 1) {
       if (lane == 0) red[k][wave] = make_float2(m, d);
       __syncthreads();
+      const float m0 = red[k][q * wpg].x;
       float sum = 0.f;
-      for (int w = q * wpg; w < (q + 1) * wpg; ++w) sum = fmaf(counts[w], red[k][w].x, sum);
-      m = sum / (float)n;
+      for (int w = q * wpg; w < (q + 1) * wpg; ++w) sum = fmaf(counts[w], red[k][w].x - m0, sum);
+      m = m0 + sum / (float)n;
       d = 0.f;
       for (int w = q * wpg; w < (q + 1) * wpg; ++w) {
         const float2 e = red[k][w];
@@ -148,7 +153,6 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
   };
   float mf = 0.f, rf = 1.f, my = 0.f, ry = 0.f;
   if (post) moments(0, mf, rf);
-  const float of = -mf * rf;
   const RowBuf by = row(a.y, r, rv);
   const RowBuf bpg = row(a.post_g, 0, post), bpb = row(a.post_b, 0, post);
   const RowBuf bgt = row(a.gate, a.gate && rv ? (int)r / a.rpg : 0, a.gate != nullptr);
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
       gt.get4(h, t4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = fmaf(fmaf(v[c][4 * h + i], rf, of), g4[i], b4[i]);
+        const float p = fmaf((v[c][4 * h + i] - mf) * rf, g4[i], b4[i]);
         v[c][4 * h + i] = fmaf(a.scale * t4[i], p, x4[i]);
       }
       o.put4(h, v[c] + 4 * h);
@@ -175,7 +179,6 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
   }
   if (pre) {
     moments(1, my, ry);
-    const float oy = -my * ry;
     const RowBuf bh = row(a.h, r, rv), bhg = row(a.pre_g, 0, true), bhb = row(a.pre_b, 0, true);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -187,7 +190,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
         hg.get4(h, g4);
         hb.get4(h, b4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b4[i] = fmaf(fmaf(v[c][4 * h + i], ry, oy), g4[i], b4[i]);
+        for (int i = 0; i < 4; ++i) b4[i] = fmaf((v[c][4 * h + i] - my) * ry, g4[i], b4[i]);
         o.put4(h, b4);
       }
       o.store(bh, col[c] * (uint32_t)sizeof(T));
@@ -350,8 +353,9 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     Row nxt;
     fetch_row(it + 1, nxt);
     if (PF) fetch_h(nxt);
-    // yh = y ry - my ry, fh = f rf - mf rf
-    const float ry = cur.st.w, oy = -cur.st.z * ry, rr = cur.st.y, of = -cur.st.x * rr;
+    // yh = (y - my) ry, fh = (f - mf) rr: the mean is subtracted first, so that
+    // rows far from zero keep their digits
+    const float ry = cur.st.w, my = cur.st.z, rr = cur.st.y, mf = cur.st.x;
     float m1 = 0.f, m2 = 0.f;
     if (pre) {
       if (!KEEP) fetch_h(cur);
@@ -368,7 +372,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
           f32x4 u = mine[h * PIECES + c * NT], v = mine[(2 + h) * PIECES + c * NT];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float yh = fmaf(y4[i], ry, oy), w = d4[i] * g4[i];
+            const float yh = (y4[i] - my) * ry, w = d4[i] * g4[i];
             u[i] += d4[i];
             v[i] = fmaf(d4[i], yh, v[i]);
             m1 += w;
@@ -392,6 +396,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
       fetch_d(cur);
       fetch_f(cur);
     }
+    const float m2r = m2 * ry;  // times y - my
     float w[NCH][8];
     float m3 = 0.f, m4 = 0.f;
     const RowBuf bx = row(a.dx, cur, a.dx != nullptr), bf = row(a.df, cur, a.df != nullptr);
@@ -412,14 +417,14 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
         g.get4(h, v4);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          t4[i] = fmaf(ry, fmaf(-m2, fmaf(f4[i], ry, oy), fmaf(d4[i], v4[i], -m1)), t4[i]);
+          t4[i] = fmaf(ry, fmaf(-m2r, f4[i] - my, fmaf(d4[i], v4[i], -m1)), t4[i]);
         o.put4(h, t4);
         cur.f[c].get4(h, f4);
         gg.get4(h, v4);
         pg.get4(h, d4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          f4[i] = fmaf(f4[i], rr, of);
+          f4[i] = (f4[i] - mf) * rr;
           s2[c][h][i] += t4[i];
           s3[c][h][i] = fmaf(t4[i], f4[i], s3[c][h][i]);
           t4[i] *= a.scale * v4[i] * d4[i];
@@ -436,7 +441,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
     if (post) {
       row_sum2(it & 1, 1, m3, m4);
       m3 *= inv_n;
-      m4 *= inv_n;
+      m4 *= inv_n * rr;  // times f - mf
       if (!KEEP) fetch_f(cur);
     }
 #pragma unroll
@@ -451,7 +456,7 @@ __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
         if (post) {
           cur.f[c].get4(h, f4);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) t4[i] = rr * fmaf(-m4, fmaf(f4[i], rr, of), t4[i] - m3);
+          for (int i = 0; i < 4; ++i) t4[i] = rr * fmaf(-m4, f4[i] - mf, t4[i] - m3);
         }
         o.put4(h, t4);
       }
