@@ -460,6 +460,11 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
 // ---------------------------------------------------------------------------
 // block with gated norms and / or saved tensors in 8 bits
 // ---------------------------------------------------------------------------
+// a launch has fewer than 2^32 threads along a dimension: at 8 values per thread
+// of the 8-bit store, at a wave per row of the gated norms
+static constexpr int64_t kAct8Values = (1ll << 34) - 1;
+static constexpr int kGnormRows = (1 << 26) - 64;
+
 static orbit_status block_ext(const char* fn, const BlockDims& z, const orbit_block_ext* e, BlockExt* o) {
   REQ(e != nullptr, ORBIT_E_ARG, "%s: ext is NULL", fn);
   REQ((e->act8 == 0 || e->act8 == 1) && (e->post_norm == 0 || e->post_norm == 1), ORBIT_E_ARG,
@@ -469,6 +474,11 @@ static orbit_status block_ext(const char* fn, const BlockDims& z, const orbit_bl
   o->act8 = e->act8 != 0; o->post = e->post_norm != 0; o->gates = e->gate_rows; o->scale = e->scale;
   // with nothing asked for this is the plain block
   o->on = o->act8 || o->branch() || o->scale != 1.f;
+  // the gated norms' and the stores' own limits
+  REQ(!o->on || z.T <= kGnormRows, ORBIT_E_UNSUPPORTED, "%s: %lld tokens exceed 2^26 - 64", fn, (long long)z.T);
+  const int64_t widest = std::max({(int64_t)3 * z.A, (int64_t)z.F, (int64_t)z.d});
+  REQ(!o->act8 || z.T <= kAct8Values / widest, ORBIT_E_UNSUPPORTED,
+      "%s: a store of %lld x %lld values reaches 2^34", fn, (long long)z.T, (long long)widest);
   return ORBIT_OK;
 }
 
@@ -1223,13 +1233,10 @@ orbit_status orbit_layernorm_fwd(int32_t dtype, int32_t rows, int32_t n, const v
 // ---------------------------------------------------------------------------
 // activations stored in 8 bits
 // ---------------------------------------------------------------------------
-// a launch has fewer than 2^32 threads along a dimension, at 8 values per thread
-static constexpr int64_t kAct8Values = 1ll << 34;
-
 static orbit_status act8_check(const char* fn, int64_t rows, int32_t n, const void* store, size_t bytes) {
   REQ(rows > 0 && n > 0 && n % 8 == 0, ORBIT_E_ARG, "%s: bad sizes rows=%lld n=%d (n must be a multiple of 8)", fn,
       (long long)rows, n);
-  REQ(rows < kAct8Values / n, ORBIT_E_UNSUPPORTED, "%s: rows=%lld x n=%d exceeds 2^34 values", fn, (long long)rows, n);
+  REQ(rows <= kAct8Values / n, ORBIT_E_UNSUPPORTED, "%s: rows=%lld x n=%d reaches 2^34 values", fn, (long long)rows, n);
   PTR(store, "store");
   REQ(bytes >= act8_store_bytes(rows, n), ORBIT_E_ARG, "%s: store of %zu bytes is smaller than the %zu required", fn,
       bytes, act8_store_bytes(rows, n));
@@ -1237,7 +1244,7 @@ static orbit_status act8_check(const char* fn, int64_t rows, int32_t n, const vo
 }
 
 size_t orbit_act8_bytes(int64_t rows, int32_t n) {
-  if (rows <= 0 || n <= 0 || n % 8 != 0 || rows >= kAct8Values / n) {
+  if (rows <= 0 || n <= 0 || n % 8 != 0 || rows > kAct8Values / n) {
     set_error("orbit_act8_bytes: bad sizes rows=%lld n=%d", (long long)rows, n);
     return 0;
   }
@@ -1360,8 +1367,7 @@ static orbit_status gnorm_check(const char* fn, const orbit_gated_norm_desc* des
   REQ(d.rows > 0 && d.n > 0 && d.n % 8 == 0, ORBIT_E_ARG, "%s: bad sizes rows=%d n=%d (n must be a multiple of 8)", fn,
       d.rows, d.n);
   REQ(d.n <= 16384, ORBIT_E_UNSUPPORTED, "%s: n=%d exceeds 16384", fn, d.n);
-  // a launch has fewer than 2^32 threads, at a wave per row
-  REQ(d.rows <= (1 << 26) - 64, ORBIT_E_UNSUPPORTED, "%s: rows=%d exceeds 2^26 - 64", fn, d.rows);
+  REQ(d.rows <= kGnormRows, ORBIT_E_UNSUPPORTED, "%s: rows=%d exceeds 2^26 - 64", fn, d.rows);
   REQ((d.post_norm == 0 || d.post_norm == 1) && (d.pre_norm == 0 || d.pre_norm == 1), ORBIT_E_ARG,
       "%s: post_norm and pre_norm must be 0 or 1", fn);
   REQ(d.gate_rows >= 0 && (d.gate_rows == 0 || d.rows % d.gate_rows == 0), ORBIT_E_ARG,

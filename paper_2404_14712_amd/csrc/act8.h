@@ -56,15 +56,11 @@ ORBIT_DEV uint32_t act8_encode(const float* f, uint2& q) {
   return a >= 0x7f800000u ? 0u : e;
 }
 
-// The values of 4 codes, and of a lane's 8.
+// The values of 4 codes.
 ORBIT_DEV void act8_decode4(uint32_t q, uint32_t e, float* f) {
   const float step = __uint_as_float(e == 0 ? 0x7fc00000u : (e - 6u) << 23);
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(q >> (8 * i)) * step;
-}
-ORBIT_DEV void act8_decode(uint2 q, uint32_t e, float* f) {
-  act8_decode4(q.x, e, f);
-  act8_decode4(q.y, e, f + 4);
 }
 
 // x[rows, n], or x - sub (sub may be null), both of leading dimension ldx -> store
