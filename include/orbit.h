@@ -136,9 +136,10 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
  * stores back into its workspace, forms x1 and the outputs of the norms, the
  * GELU and the attention from them, and runs as from stored tensors. Its
  * gradients are those at the stored values. The attention's are of the softmax
- * of the stored q and k: the stores' rounding moves a score by up to some 2^-7
- * of |q| |k| / sqrt(head_dim) and a probability by the exponential of that, so
- * that with scores far in the tens the gradients of q, k and v are rough.
+ * of the stored q and k: the stores' rounding moves a score by up to about a
+ * hundredth of |q| |k| / sqrt(head_dim), mostly by far less, and a probability by
+ * the exponential of that, so that with scores far in the tens the gradients of
+ * q, k and v are rough.
  * saved == NULL is inference, and activation checkpointing without any such
  * rounding, as in the plain calls. */
 typedef struct {
@@ -368,10 +369,12 @@ orbit_status orbit_layernorm_fwd(int32_t dtype, int32_t rows, int32_t n, const v
  * largest |x|,
  *   E = max(7, min(254, (a + 0x10000) >> 23)),  code = round(x 2^(133 - E))
  * (nearest, ties to even, within +-127), and a value reads back as
- * code 2^(E - 133): off by at most half a step 2^(E - 133), that is by less
- * than 2^-7 of the group's largest |x| (float32 values above 127.5 2^121 end
- * at 127 2^121, those below 2^-127 at 0), and exact in both dtypes. A group that
- * holds an infinity or a NaN has E = 0 and reads back as NaN.
+ * code 2^(E - 133): exact in both dtypes, and off by at most half a step
+ * 2^(E - 133). For groups whose largest |x| is 63.75 2^-126 or more that is at
+ * most 1 / 127.5 of it (reached where the largest is just 127.5 of the next
+ * smaller steps); smaller groups keep the step 2^-126, and float32 values above
+ * 127.5 2^121 end at 127 2^121. A group that holds an infinity or a NaN has
+ * E = 0 and reads back as NaN.
  * In memory: the codes [rows, n], from the next multiple of 256 bytes on the
  * E [rows, (n + 31) / 32], the whole a multiple of 256 bytes. */
 size_t orbit_act8_bytes(int64_t rows, int32_t n); /* 0 on bad sizes, and from 2^34 values on */

@@ -8,10 +8,10 @@
 // exponent from 127.5 / 64 on), within 7 .. 254 so that the step and its
 // reciprocal stay normal floats. A power of two makes the division, the
 // rounding (to nearest, ties to even) and the read back exact in any width, so
-// every value is off by at most half a step (below 2^-7 of the group's
-// largest) and reads back as an exact bf16. E = 0 marks a group that held an
-// infinity or a NaN: it reads back as NaN throughout, so that a diverged value
-// is not hidden.
+// every value is off by at most half a step (at most 1 / 127.5 of the group's
+// largest where E is not clamped) and reads back as an exact bf16. E = 0 marks a
+// group that held an infinity or a NaN: it reads back as NaN throughout, so that
+// a diverged value is not hidden.
 #pragma once
 #include "common.h"
 
