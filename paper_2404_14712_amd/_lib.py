@@ -188,9 +188,11 @@ def _nbytes(t) -> int:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        # the current stream's handle without a Stream object (0.4 us a call instead of 2.8)
+        # the current stream's handle without a Stream object (0.4 us a call instead of 2.8), where this
+        # torch has the private call for it
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
