@@ -38,19 +38,19 @@ struct Raw8Q {
   }
 };
 
-// A block's G = blockDim / tpr groups of tpr threads take a row each; thread t
-// of a group owns the NCH 8-column pieces t + c tpr, so that a quad holds the 32
-// columns of a group of the store. Statistics: each thread's own mean (corrected
-// by its deviations' sum, so that a constant's mean is that constant) and squared
-// deviations, merged pairwise over the wave, then over the row's waves through
-// LDS with one barrier. The mean is subtracted before anything is scaled: v r -
-// mean r would round at the mean's size. y is written rounded to the storage type, h and
-// the statistics come from its float32 value: h then carries one rounding
-// instead of two, and the backward's (rounded y - mean) differs from the exact
-// one by y's rounding alone.
+// A block's G = blockDim / tpr groups of tpr threads take a row each; thread t of
+// a group owns the NCH 8-column pieces t + c tpr, so that a quad holds the 32
+// columns of a group of the store. Statistics: each thread's own mean (pairwise
+// sums of 8 values, pieces and waves as differences from the first: a constant's
+// mean is that constant) and squared deviations, merged pairwise over the wave,
+// then over the row's waves through LDS with one barrier. The mean is subtracted
+// before anything is scaled: v r - mean r would round at the mean's size. y is
+// written rounded to the storage type, h and the statistics come from its float32
+// value: h then carries one rounding instead of two, and the backward's (rounded
+// y - mean) differs from the exact one by y's rounding alone.
 //
 // Many independent rows per CU (16 waves: at most 128 registers) hide the two
-// reductions of a row; 4096 x 8192 in bf16 moves 268 MB in 58 us (4.6 TB/s; a
+// reductions of a row; 4096 x 8192 in bf16 moves 268 MB in 59 us (4.5 TB/s; a
 // copy of that size 5.3). One block per CU that kept the parameter vectors in
 // registers and loaded its next row ahead took 85 us, 20 waves with their
 // spills 76. STREAM: x and f are loaded non-temporally.
@@ -118,22 +118,24 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) g
   }
   // mean and 1 / sqrt(variance + eps) of the row held as v; k: which norm
   auto moments = [&](int k, float& mu, float& rs) {
-    float s = 0.f, d = 0.f;
+    // the pieces' sums as differences from the first's
+    float s0 = 0.f, s = 0.f, d = 0.f;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += v[c][i];
-    float m = s * inv_own, u = 0.f;
+    for (int c = 0; c < NCH; ++c) {
+      const float* p = v[c];
+      const float sc = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      if (c == 0) s0 = sc;
+      else s += on[c] ? sc - s0 : 0.f;
+    }
+    float m = fmaf(s, inv_own, 0.125f * s0);
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
       if (on[c])
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float e = v[c][i] - m;
-          u += e;
           d = fmaf(e, e, d);
         }
-    m = fmaf(u, inv_own, m);
     wm.merge(m, d);
     if (wpg > 1) {
       if (lane == 0) red[k][wave] = make_float2(m, d);
@@ -233,15 +235,17 @@ struct GnRow {
   std::conditional_t<F8, Raw8Q, Raw8<T>> f[NCH];
 };
 
-// A block of 512 threads (one per CU, 256 registers each) whose G = blockDim /
-// tpr groups of tpr threads take the chunk's rows in turn; thread t of a group
-// owns the NCH 8-column pieces t + c tpr. Every group runs the same number of
-// rows, so the barriers line up. The four column sums would take half of the
-// register file at full width; the two of the pre norm live in LDS. That leaves
-// room for the next row's dh and y (PF, bf16), so that loads are in flight all
-// the time; its dy and f follow into the registers of the current row's once
-// these are used up. KEEP: values stay in registers from their one load; the
-// widest float32 rows are loaded again where they are used instead.
+// A block of 512 threads (one per CU: two waves per SIMD, 256 registers each)
+// whose G = blockDim / tpr groups of tpr threads take the chunk's rows in turn;
+// thread t of a group owns the NCH 8-column pieces t + c tpr. Every group runs
+// the same number of rows, so the barriers line up. The four column sums would
+// take half of the register file at full width; the two of the pre norm live in
+// LDS. That leaves room for the next row's dh and y (PF, bf16), so that loads are
+// in flight all the time; its dy and f follow into the registers of the current
+// row's once these are used up. With four pieces a thread that is all 256
+// registers, and a few spill (5 where f comes from the store, 1 else). KEEP:
+// values stay in registers from their one load; the widest float32 rows are
+// loaded again where they are used instead.
 template <typename T, int NCH, bool F8, bool KEEP, bool PF>
 __global__ void __launch_bounds__(512) gnorm_bwd_kernel(GnBwd a) {
   using Row = GnRow<T, NCH, F8>;
@@ -601,9 +605,11 @@ __global__ void __launch_bounds__(1024) gnorm_final_kernel(GnFinal a) {
 // threads of a block have some; float32 stays at two up to 8192 columns, which
 // its registers hold (4096 x 2048: 61 -> 55 us). A block takes as many rows at
 // once as that gives. Chunks: about one per CU, in whole turns of the block's
-// groups. More of them cost more partial rows than they hide latency (bf16 8192
-// x 1024: 31 us, with 512 chunks 37), fewer leave CUs idle where rows are few
-// (256 x 16384: 45 us, 84 with at least 8 rows a chunk).
+// groups. From two pieces a thread on a kernel's 147 to 256 registers let one
+// block onto a CU, so that more chunks run one after the other and add partial
+// rows (bf16 8192 x 1024: 31 us, with 512 chunks 37; two blocks at a time on a CU,
+// which would take 128 registers, were not tried); fewer leave CUs idle where rows
+// are few (256 x 16384: 45 us, 84 with at least 8 rows a chunk).
 // pieces of 8 columns per thread
 int gn_pieces(int n) { return n <= 512 ? 1 : n <= 1024 ? 2 : n > 8192 && n <= 12288 ? 3 : 4; }
 
