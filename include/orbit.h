@@ -135,11 +135,12 @@ orbit_status orbit_vit_block_bwd(const orbit_block_desc* desc, const orbit_block
  * forward's result does not depend on it, bit for bit; the backward reads the
  * stores back into its workspace, forms x1 and the outputs of the norms, the
  * GELU and the attention from them, and runs as from stored tensors. Its
- * gradients are those at the stored values. The attention's are of the softmax
- * of the stored q and k: the stores' rounding moves a score by up to about a
- * hundredth of |q| |k| / sqrt(head_dim), mostly by far less, and a probability by
- * the exponential of that, so that with scores far in the tens the gradients of
- * q, k and v are rough.
+ * gradients are those at the stored values, the norm of f_2 taken with the exact
+ * f_2's mean and deviation (f_1's are the stored f_1's). The attention's are of
+ * the softmax of the stored q and k: without outlier channels the stores'
+ * rounding moves a score by at most about a hundredth of |q| |k| /
+ * sqrt(head_dim), mostly by far less, and a probability by the exponential of
+ * that, so that with scores far in the tens the gradients of q, k and v are rough.
  * saved == NULL is inference, and activation checkpointing without any such
  * rounding, as in the plain calls. */
 typedef struct {
@@ -433,7 +434,9 @@ size_t orbit_gated_norm_bwd_workspace_bytes(const orbit_gated_norm_desc* desc);
  * of h; unused without pre_norm) and dy (gradient of y from its other readers;
  * NULL: none, with pre_norm only), given f or its store (as in the forward;
  * both may be NULL without post_norm and gate), the forward's y (may be NULL
- * without pre_norm) and stats. dx is the whole gradient of y and may be NULL.
+ * without pre_norm) and stats, which are used as given: with f from its store
+ * and the statistics of a forward that was given f, f^ is (stored f - mean of f)
+ * / deviation of f. dx is the whole gradient of y and may be NULL.
  * dx may alias dy, df may alias dh or f. Gradients of absent parameters are not
  * touched. Sums are formed in a fixed order (bitwise reproducible). */
 orbit_status orbit_gated_norm_bwd(const orbit_gated_norm_desc* desc, const orbit_gated_norm_params* p, const void* f,
