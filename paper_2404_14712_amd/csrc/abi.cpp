@@ -172,9 +172,8 @@ BlockSaved8 carve_block_saved8(const BlockDims& z, const BlockExt& x, void* base
 }
 
 // bytes of the tensors the backward reads, in full types
-size_t block_full_bytes(const BlockDims& z, BlockExt x) {
+size_t block_full_bytes(const BlockDims& z, const BlockExt& x) {
   size_t u = 0;
-  x.act8 = false;
   carve_block_saved(z, x, nullptr, &u);
   return u;
 }
