@@ -445,6 +445,154 @@ orbit_status orbit_gated_norm_bwd(const orbit_gated_norm_desc* desc, const orbit
                                   int accumulate, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* 8-bit floating point: stores with a scale per block of 128, their product, */
+/* and a linear layer on it                                                   */
+/* ------------------------------------------------------------------------ */
+
+/* The store of a matrix X[rows, n] keeps one e4m3 code (OCP: 4 exponent bits,
+ * bias 7, largest 448) per value and one byte E per block: 128 consecutive columns of
+ * a row (tile_rows 1; the last may be shorter), or a tile of 128 rows x 128 columns
+ * (tile_rows 128). With a the float32 bits of a block's largest finite |x|,
+ *   E = min(246, max(10, ((a + 0x1fffff) >> 23) - 8)),
+ *   code = e4m3(x 2^(127 - E))   (nearest, ties to even, within +-448)
+ * and a value reads back as code 2^(E - 127), exact in both dtypes: the scale is the
+ * smallest power of two that brings the block within 448, and a value is off by at
+ * most 2^-4 of itself or half the smallest code, 2^-10, of the scale. Float32 values above
+ * 448 2^119 end there. An infinity or a NaN becomes the NaN code alone, and a
+ * product's results that read it are NaN.
+ * In memory: the codes [rows, wide], wide = n up to a multiple of 128 (zero codes
+ * past n), from the next multiple of 256 bytes on the E [rows, groups], groups = the
+ * blocks of a row up to a multiple of 4 (zeros past them), the whole a multiple of
+ * 256 bytes. Rows of one tile hold equal E. */
+size_t orbit_fp8_bytes(int64_t rows, int64_t n); /* 0 on bad sizes, and beyond the limits below */
+/* x[rows, n] (dtype, leading dimension ldx >= n, a multiple of 8; any n) -> its store,
+ * and / or store_t, the store of its transpose X^T[n, rows], whose blocks run along
+ * the rows of X. With tile_rows 128 both hold the same values. Either store may be
+ * NULL, not both. A store has fewer than 2^34 codes and the matrix fewer than 2^24
+ * tiles of 128 x 128. */
+orbit_status orbit_fp8_pack(int32_t dtype, int64_t rows, int64_t n, int32_t tile_rows, const void* x, int64_t ldx,
+                            void* store, size_t store_bytes, void* store_t, size_t store_t_bytes, void* stream);
+/* store -> x[rows, n] (dtype, leading dimension ldx >= n, a multiple of 8) */
+orbit_status orbit_fp8_unpack(int32_t dtype, int64_t rows, int64_t n, const void* store, size_t store_bytes, void* x,
+                              int64_t ldx, void* stream);
+
+/* C[M, N] = A B^T (+ bias[n]) (+ C if accumulate) over the stores of A[M, K] and
+ * B[N, K], float32 accumulation. C is float32 if c_f32 or dtype is ORBIT_F32, else
+ * bf16 (accumulate needs float32); bias is dtype [N] or NULL. N and ldc >= N are
+ * multiples of 8, M and K any; K below 2^22. For y = x W take the store of x and the
+ * transposed one of W; for dx = dy W^T the stores of dy and of W; for dw = x^T dy the
+ * transposed stores of both. Sums are formed in an order that depends on the
+ * sizes alone (bitwise reproducible). */
+size_t orbit_fp8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K); /* may be 0; ws may then be NULL */
+orbit_status orbit_fp8_gemm(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* A, size_t a_bytes,
+                            const void* B, size_t b_bytes, void* C, int64_t ldc, int32_t c_f32, const void* bias,
+                            int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* A linear layer y = x W + b on 8-bit products. With Q the values of a store in
+ * blocks along a row and Qt those of a transposed store (blocks along the rows), and
+ * Qw the weight's in 128 x 128 tiles:
+ *   y = Q(x) Qw + b,   dx = Q(dy) Qw^T,   dw = Qt(x)^T Qt(dy),   db = column sums of dy
+ * (the gradients pass the rounding straight through). The weight W[in, out] comes as
+ * the two stores of orbit_fp8_pack(dtype, in, out, 128, W, ...): w (store) and w_t
+ * (store_t), packed once for every pass until the weight changes. in and out are
+ * multiples of 8, rows any; each below 2^22. Leading dimensions are multiples of 8. */
+typedef struct {
+  int32_t rows, in, out;
+  int32_t dtype;
+} orbit_fp8_linear_desc;
+size_t orbit_fp8_linear_saved_bytes(const orbit_fp8_linear_desc* desc);
+size_t orbit_fp8_linear_workspace_bytes(const orbit_fp8_linear_desc* desc); /* of either direction */
+/* x[rows, in] -> y[rows, out]; saved (may be NULL: inference) receives the
+ * transposed store of x for the backward. y must not alias x. */
+orbit_status orbit_fp8_linear_fwd(const orbit_fp8_linear_desc* desc, const void* x, int64_t ldx, const void* w_t,
+                                  size_t w_t_bytes, const void* bias, void* y, int64_t ldy, void* saved, void* ws,
+                                  size_t ws_bytes, void* stream);
+/* dy[rows, out] -> dx[rows, in] (may be NULL; must not alias dy), dw[in, out] and
+ * db[out] (may be NULL) float32. w may be NULL without dx. */
+orbit_status orbit_fp8_linear_bwd(const orbit_fp8_linear_desc* desc, const void* saved, const void* w, size_t w_bytes,
+                                  const void* dy, int64_t lddy, void* dx, int64_t lddx, float* dw, float* db,
+                                  int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary positions with several axes on q and k, after their LayerNorm      */
+/* ------------------------------------------------------------------------ */
+
+/* src[tokens, (q_heads + k_heads) head_dim]: the query heads, then the key heads (the
+ * first two of [q | k | v]; k_heads may be smaller, where heads share keys). Each head
+ *   norm ? LN(head) g + b : head      (biased variance; qn_* for query heads, kn_* for key heads)
+ * and then its pairs turn: pair i, i < head_dim / 2, is columns (i, head_dim/2 + i), or
+ * (2i, 2i + 1) if near, and
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),
+ *   t = pos[token % pos_rows, axis[i]] freq[i]
+ * with pos [pos_rows, axes] and freq [head_dim / 2] float32 on the device. Angles are
+ * formed and reduced in 64 bits; |t| is meant to stay below 2^50. A pair with freq 0
+ * stays as it is. axes is 1 to 4 (time, latitude, longitude, level, say), pos_rows
+ * divides tokens (L of [B, L]), head_dim is 32, 64, 128, 192 or 256 in either dtype,
+ * tokens below 2^24, tokens * heads below 2^31. */
+typedef struct {
+  int32_t tokens, q_heads, k_heads, head_dim;
+  int32_t norm, near, axes, pos_rows;
+  float eps;
+  int32_t dtype;
+  uint8_t axis[128]; /* of each pair, below axes; those past head_dim / 2 are ignored */
+} orbit_qk_rope_desc;
+typedef struct { const void *qn_g, *qn_b, *kn_g, *kn_b; } orbit_qk_rope_params; /* [head_dim]; may be NULL without norm */
+typedef struct { float *qn_g, *qn_b, *kn_g, *kn_b; } orbit_qk_rope_grads;
+
+/* Leading dimensions >= (q_heads + k_heads) head_dim, multiples of 8. dst may be src
+ * with the same leading dimension. mean, rstd [tokens, q_heads + k_heads] float32 receive the
+ * norms' statistics (unused without norm; NULL with norm: not written, inference). */
+orbit_status orbit_qk_rope_fwd(const orbit_qk_rope_desc* desc, const orbit_qk_rope_params* p, const float* pos,
+                               const float* freq, const void* src, int64_t lds, void* dst, int64_t ldd, float* mean,
+                               float* rstd, void* stream);
+size_t orbit_qk_rope_bwd_workspace_bytes(const orbit_qk_rope_desc* desc); /* 0 without norm; ws may then be NULL */
+/* dy (gradient of dst) -> dx (of src; may be dy with the same leading dimension) and
+ * the parameters' gradients, from the forward's src, mean and rstd, which are used as
+ * given (all three may be NULL without norm, as may the grads). Sums are formed in a fixed
+ * order (bitwise reproducible). dx must not alias src. */
+orbit_status orbit_qk_rope_bwd(const orbit_qk_rope_desc* desc, const orbit_qk_rope_params* p, const float* pos,
+                               const float* freq, const void* src, int64_t lds, const float* mean, const float* rstd,
+                               const void* dy, int64_t lddy, void* dx, int64_t lddx, const orbit_qk_rope_grads* g,
+                               int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* The block with rotary positions and / or 8-bit products                    */
+/* ------------------------------------------------------------------------ */
+
+/* orbit_vit_block_ext_* with two more options; with both NULL its result, bit for
+ * bit. rope: q and k, after their norms where qk_norm is set, turn as in
+ * orbit_qk_rope_desc (pos_rows divides B*L). fp8: the four linear layers are those
+ * of orbit_fp8_linear_fwd / _bwd, on the stores of the four weights in 128 x 128 tiles
+ * (w_qkv and w_qkv_t, ... as orbit_fp8_pack(dtype, in, out, 128, ...) gives them); the
+ * weights in the block's params are then not read (but checked). `saved` keeps their
+ * inputs as transposed stores. fp8 with ext's act8 is ORBIT_E_UNSUPPORTED. */
+typedef struct {
+  int32_t axes, pos_rows, near;
+  uint8_t axis[128];
+  const float *pos, *freq;
+} orbit_block_rope;
+typedef struct { const void *w_qkv, *w_qkv_t, *w_proj, *w_proj_t, *w_fc1, *w_fc1_t, *w_fc2, *w_fc2_t; } orbit_block_fp8;
+typedef struct {
+  const orbit_block_rope* rope;
+  const orbit_block_fp8* fp8;
+} orbit_block_opt;
+
+/* the size queries read no device pointer of opt (they may be NULL there) */
+size_t orbit_vit_block_opt_saved_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                       const orbit_block_opt* opt);
+size_t orbit_vit_block_opt_workspace_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                           const orbit_block_opt* opt);
+orbit_status orbit_vit_block_opt_fwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_opt* opt, const orbit_block_params* p,
+                                     const orbit_block_ext_params* ep, const void* x, void* y, void* saved, void* ws,
+                                     size_t ws_bytes, void* stream);
+orbit_status orbit_vit_block_opt_bwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_opt* opt, const orbit_block_params* p,
+                                     const orbit_block_ext_params* ep, const void* x, const void* saved, const void* dy,
+                                     void* dx, const orbit_block_grads* g, const orbit_block_ext_grads* eg,
+                                     int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Diagnostics and measurement support                                       */
 /* ------------------------------------------------------------------------ */
 

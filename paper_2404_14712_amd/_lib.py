@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint8, c_void_p
 from typing import Dict, Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -24,7 +24,29 @@ BLOCK_PARAMS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "qn_g", "qn_b", "kn_g", "kn_
 AGG_PARAMS = ("q0", "w_q", "b_q", "w_k", "b_k", "w_v", "b_v", "w_o", "b_o", "pos")
 BLOCK_EXT_PARAMS = ("post1_g", "post1_b", "gate1", "post2_g", "post2_b", "gate2")
 GATED_NORM_PARAMS = ("gate", "post_g", "post_b", "pre_g", "pre_b")
+QK_NORM_PARAMS = ("qn_g", "qn_b", "kn_g", "kn_b")
+BLOCK_FP8_WEIGHTS = ("w_qkv", "w_proj", "w_fc1", "w_fc2")
+BLOCK_FP8_STORES = tuple(w + t for w in BLOCK_FP8_WEIGHTS for t in ("", "_t"))
+ROPE_PAIRS = 128
 HEAD_PARAMS = ("lnf_g", "lnf_b", "w_h", "b_h", "w_hid", "b_hid")
+
+
+def _ptr(t) -> Optional[int]:
+    if t is None:
+        return None
+    if isinstance(t, int):
+        return t
+    return t.data_ptr()
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _axis(axis):
+    if len(axis) > ROPE_PAIRS or not all(0 <= a < 256 for a in axis):
+        raise ValueError(f"an axis for each of at most {ROPE_PAIRS} pairs, not {list(axis)}")
+    return (c_uint8 * ROPE_PAIRS)(*axis)
 
 
 class BlockDesc(ctypes.Structure):
@@ -101,6 +123,52 @@ class GatedNormGrads(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in GATED_NORM_PARAMS]
 
 
+class Fp8LinearDesc(ctypes.Structure):
+    _fields_ = [("rows", c_int32), ("n_in", c_int32), ("n_out", c_int32), ("dtype", c_int32)]
+
+
+class QkRopeDesc(ctypes.Structure):
+    _fields_ = [("tokens", c_int32), ("q_heads", c_int32), ("k_heads", c_int32), ("head_dim", c_int32),
+                ("norm", c_int32), ("near", c_int32), ("axes", c_int32), ("pos_rows", c_int32), ("eps", c_float),
+                ("dtype", c_int32), ("axis", c_uint8 * ROPE_PAIRS)]
+
+    @classmethod
+    def of(cls, tokens, q_heads, k_heads, head_dim, dtype, axis, axes, pos_rows, norm=True, near=False, eps=1e-5):
+        """axis: the axis of each of the head's head_dim / 2 pairs."""
+        return cls(tokens, q_heads, k_heads, head_dim, int(norm), int(near), axes, pos_rows, eps, dtype, _axis(axis))
+
+
+class BlockRope(ctypes.Structure):
+    _fields_ = [("axes", c_int32), ("pos_rows", c_int32), ("near", c_int32), ("axis", c_uint8 * ROPE_PAIRS),
+                ("pos", c_void_p), ("freq", c_void_p)]
+
+    @classmethod
+    def of(cls, axis, axes, pos_rows, pos, freq, near=False):
+        return cls(axes, pos_rows, int(near), _axis(axis), _ptr(pos), _ptr(freq))
+
+
+class BlockFp8(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in BLOCK_FP8_STORES]
+
+
+class BlockOpt(ctypes.Structure):
+    _fields_ = [("rope", POINTER(BlockRope)), ("fp8", POINTER(BlockFp8))]
+
+    @classmethod
+    def of(cls, rope: Optional[BlockRope] = None, fp8: Optional[Dict[str, object]] = None):
+        """fp8: the weights' stores by name (w_qkv, w_qkv_t, ...)."""
+        f = None if fp8 is None else BlockFp8(*[_ptr(fp8.get(n)) for n in BLOCK_FP8_STORES])
+        return cls(None if rope is None else ctypes.pointer(rope), None if f is None else ctypes.pointer(f))
+
+
+class QkRopeParams(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in QK_NORM_PARAMS]
+
+
+class QkRopeGrads(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in QK_NORM_PARAMS]
+
+
 class OrbitError(RuntimeError):
     def __init__(self, fn: str, status: int, detail: str):
         super().__init__(f"{fn} failed with status {status}: {detail}")
@@ -160,6 +228,27 @@ _PROTOS = {
     "orbit_gated_norm_bwd_workspace_bytes": (c_size_t, [POINTER(GatedNormDesc)]),
     "orbit_gated_norm_bwd": (c_int, [POINTER(GatedNormDesc), POINTER(GatedNormParams), P, P, c_size_t, P, P, P, P, P,
                                      P, POINTER(GatedNormGrads), c_int, P, c_size_t, P]),
+    "orbit_fp8_bytes": (c_size_t, [c_int64, c_int64]),
+    "orbit_fp8_pack": (c_int, [c_int32, c_int64, c_int64, c_int32, P, c_int64, P, c_size_t, P, c_size_t, P]),
+    "orbit_fp8_unpack": (c_int, [c_int32, c_int64, c_int64, P, c_size_t, P, c_int64, P]),
+    "orbit_fp8_gemm_workspace_bytes": (c_size_t, [c_int32] * 3),
+    "orbit_fp8_gemm": (c_int, [c_int32] * 4 + [P, c_size_t, P, c_size_t, P, c_int64, c_int32, P, c_int32, P, c_size_t, P]),
+    "orbit_fp8_linear_saved_bytes": (c_size_t, [POINTER(Fp8LinearDesc)]),
+    "orbit_fp8_linear_workspace_bytes": (c_size_t, [POINTER(Fp8LinearDesc)]),
+    "orbit_fp8_linear_fwd": (c_int, [POINTER(Fp8LinearDesc), P, c_int64, P, c_size_t, P, P, c_int64, P, P, c_size_t, P]),
+    "orbit_fp8_linear_bwd": (c_int, [POINTER(Fp8LinearDesc), P, P, c_size_t, P, c_int64, P, c_int64, P, P, c_int32, P,
+                                     c_size_t, P]),
+    "orbit_qk_rope_fwd": (c_int, [POINTER(QkRopeDesc), POINTER(QkRopeParams), P, P, P, c_int64, P, c_int64, P, P, P]),
+    "orbit_qk_rope_bwd_workspace_bytes": (c_size_t, [POINTER(QkRopeDesc)]),
+    "orbit_qk_rope_bwd": (c_int, [POINTER(QkRopeDesc), POINTER(QkRopeParams), P, P, P, c_int64, P, P, P, c_int64, P,
+                                  c_int64, POINTER(QkRopeGrads), c_int32, P, c_size_t, P]),
+    "orbit_vit_block_opt_saved_bytes": (c_size_t, [POINTER(BlockDesc), POINTER(BlockExt), POINTER(BlockOpt)]),
+    "orbit_vit_block_opt_workspace_bytes": (c_size_t, [POINTER(BlockDesc), POINTER(BlockExt), POINTER(BlockOpt)]),
+    "orbit_vit_block_opt_fwd": (c_int, [POINTER(BlockDesc), POINTER(BlockExt), POINTER(BlockOpt), POINTER(BlockParams),
+                                        POINTER(BlockExtParams), P, P, P, P, c_size_t, P]),
+    "orbit_vit_block_opt_bwd": (c_int, [POINTER(BlockDesc), POINTER(BlockExt), POINTER(BlockOpt), POINTER(BlockParams),
+                                        POINTER(BlockExtParams), P, P, P, P, POINTER(BlockGrads),
+                                        POINTER(BlockExtGrads), c_int, P, c_size_t, P]),
     "orbit_status_string": (c_char_p, [c_int]),
     "orbit_last_error": (c_char_p, []),
     "orbit_abi_version": (c_int, []),
@@ -172,18 +261,6 @@ _PROTOS = {
 }
 
 EXPORTS = tuple(_PROTOS)
-
-
-def _ptr(t) -> Optional[int]:
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
-
-
-def _nbytes(t) -> int:
-    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _stream(stream) -> Optional[int]:
@@ -416,6 +493,81 @@ class OrbitLib:
         self._check("orbit_gated_norm_bwd", self.lib.orbit_gated_norm_bwd(
             ctypes.byref(desc), ctypes.byref(p), _ptr(f), _ptr(store), _nbytes(store), _ptr(y), _ptr(stats), _ptr(dh),
             _ptr(dy), _ptr(dx), _ptr(df), ctypes.byref(g), int(accumulate), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    # -- 8-bit floating point --------------------------------------------------
+    def orbit_fp8_bytes(self, rows, n) -> int:
+        return self.lib.orbit_fp8_bytes(int(rows), int(n))
+
+    def orbit_fp8_pack(self, dtype, rows, n, tile_rows, x, ldx, store, store_t=None, stream=None):
+        self._check("orbit_fp8_pack", self.lib.orbit_fp8_pack(
+            dtype, rows, n, tile_rows, _ptr(x), ldx, _ptr(store), _nbytes(store), _ptr(store_t), _nbytes(store_t),
+            _stream(stream)))
+
+    def orbit_fp8_unpack(self, dtype, rows, n, store, x, ldx, stream=None):
+        self._check("orbit_fp8_unpack", self.lib.orbit_fp8_unpack(
+            dtype, rows, n, _ptr(store), _nbytes(store), _ptr(x), ldx, _stream(stream)))
+
+    def orbit_fp8_gemm_workspace_bytes(self, M, N, K) -> int:
+        return self.lib.orbit_fp8_gemm_workspace_bytes(M, N, K)
+
+    def orbit_fp8_gemm(self, dtype, M, N, K, A, B, C, ldc, c_f32=0, bias=None, accumulate=0, ws=None, stream=None):
+        self._check("orbit_fp8_gemm", self.lib.orbit_fp8_gemm(
+            dtype, M, N, K, _ptr(A), _nbytes(A), _ptr(B), _nbytes(B), _ptr(C), ldc, int(c_f32), _ptr(bias),
+            int(accumulate), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    def orbit_fp8_linear_saved_bytes(self, desc) -> int:
+        return self.lib.orbit_fp8_linear_saved_bytes(ctypes.byref(desc))
+
+    def orbit_fp8_linear_workspace_bytes(self, desc) -> int:
+        return self.lib.orbit_fp8_linear_workspace_bytes(ctypes.byref(desc))
+
+    def orbit_fp8_linear_fwd(self, desc, x, ldx, w_t, bias, y, ldy, saved, ws, stream=None):
+        self._check("orbit_fp8_linear_fwd", self.lib.orbit_fp8_linear_fwd(
+            ctypes.byref(desc), _ptr(x), ldx, _ptr(w_t), _nbytes(w_t), _ptr(bias), _ptr(y), ldy, _ptr(saved), _ptr(ws),
+            _nbytes(ws), _stream(stream)))
+
+    def orbit_fp8_linear_bwd(self, desc, saved, w, dy, lddy, dx, lddx, dw, db, accumulate, ws, stream=None):
+        self._check("orbit_fp8_linear_bwd", self.lib.orbit_fp8_linear_bwd(
+            ctypes.byref(desc), _ptr(saved), _ptr(w), _nbytes(w), _ptr(dy), lddy, _ptr(dx), lddx, _ptr(dw), _ptr(db),
+            int(accumulate), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    # -- rotary positions ------------------------------------------------------
+    def orbit_qk_rope_fwd(self, desc, params, pos, freq, src, lds, dst, ldd, mean=None, rstd=None, stream=None):
+        p = self._struct(QkRopeParams, params)
+        self._check("orbit_qk_rope_fwd", self.lib.orbit_qk_rope_fwd(
+            ctypes.byref(desc), ctypes.byref(p), _ptr(pos), _ptr(freq), _ptr(src), lds, _ptr(dst), ldd, _ptr(mean),
+            _ptr(rstd), _stream(stream)))
+
+    def orbit_qk_rope_bwd_workspace_bytes(self, desc) -> int:
+        return self.lib.orbit_qk_rope_bwd_workspace_bytes(ctypes.byref(desc))
+
+    def orbit_qk_rope_bwd(self, desc, params, pos, freq, src, lds, mean, rstd, dy, lddy, dx, lddx, grads, accumulate=0,
+                          ws=None, stream=None):
+        p, g = self._struct(QkRopeParams, params), self._struct(QkRopeGrads, grads)
+        self._check("orbit_qk_rope_bwd", self.lib.orbit_qk_rope_bwd(
+            ctypes.byref(desc), ctypes.byref(p), _ptr(pos), _ptr(freq), _ptr(src), lds, _ptr(mean), _ptr(rstd),
+            _ptr(dy), lddy, _ptr(dx), lddx, ctypes.byref(g), int(accumulate), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    # -- block with rotary positions and / or 8-bit products ---------------------
+    def orbit_vit_block_opt_saved_bytes(self, desc, ext, opt) -> int:
+        return self.lib.orbit_vit_block_opt_saved_bytes(ctypes.byref(desc), ctypes.byref(ext), ctypes.byref(opt))
+
+    def orbit_vit_block_opt_workspace_bytes(self, desc, ext, opt) -> int:
+        return self.lib.orbit_vit_block_opt_workspace_bytes(ctypes.byref(desc), ctypes.byref(ext), ctypes.byref(opt))
+
+    def orbit_vit_block_opt_fwd(self, desc, ext, opt, params, x, y, saved, ws, stream=None):
+        p, e = self._struct(BlockParams, params), self._struct(BlockExtParams, params)
+        self._check("orbit_vit_block_opt_fwd", self.lib.orbit_vit_block_opt_fwd(
+            ctypes.byref(desc), ctypes.byref(ext), ctypes.byref(opt), ctypes.byref(p), ctypes.byref(e), _ptr(x),
+            _ptr(y), _ptr(saved), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+    def orbit_vit_block_opt_bwd(self, desc, ext, opt, params, x, saved, dy, dx, grads, accumulate, ws, stream=None):
+        p, e = self._struct(BlockParams, params), self._struct(BlockExtParams, params)
+        g, eg = self._struct(BlockGrads, grads), self._struct(BlockExtGrads, grads)
+        self._check("orbit_vit_block_opt_bwd", self.lib.orbit_vit_block_opt_bwd(
+            ctypes.byref(desc), ctypes.byref(ext), ctypes.byref(opt), ctypes.byref(p), ctypes.byref(e), _ptr(x),
+            _ptr(saved), _ptr(dy), _ptr(dx), ctypes.byref(g), ctypes.byref(eg), int(accumulate), _ptr(ws), _nbytes(ws),
+            _stream(stream)))
 
     # -- measurement aid -------------------------------------------------------
     def orbit_mfma_probe(self, blocks, iters, seed, x, out, stream=None):

@@ -4,44 +4,18 @@
 
 #include <algorithm>
 
+#include "abi_check.h"
 #include "act8.h"
 #include "agg.h"
+#include "fp8.h"
 #include "gemm.h"
 #include "gnorm.h"
 #include "kernels.h"
+#include "rope.h"
 
 using namespace orbit;
 
 namespace {
-
-size_t esz(int dt) { return dt == ORBIT_BF16 ? 2 : 4; }
-hipStream_t S(void* st) { return static_cast<hipStream_t>(st); }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-#define REQ(cond, code, ...)        \
-  do {                              \
-    if (!(cond)) {                  \
-      set_error(__VA_ARGS__);       \
-      return code;                  \
-    }                               \
-  } while (0)
-
-#define PTR(p, name)                                                        \
-  do {                                                                      \
-    REQ((p) != nullptr, ORBIT_E_ARG, "%s: %s is NULL", fn, name);           \
-    REQ(aligned16(p), ORBIT_E_ARG, "%s: %s is not 16-byte aligned", fn, name); \
-  } while (0)
-
-#define OPT_PTR(p, name)                                                    \
-  do {                                                                      \
-    if (p) REQ(aligned16(p), ORBIT_E_ARG, "%s: %s is not 16-byte aligned", fn, name); \
-  } while (0)
-
-orbit_status check_dtype(const char* fn, int dt) {
-  REQ(dt == ORBIT_F32 || dt == ORBIT_BF16, ORBIT_E_ARG, "%s: dtype %d is not ORBIT_F32 or ORBIT_BF16", fn, dt);
-  return ORBIT_OK;
-}
 
 // attention head widths with kernels: 32, 64 and 128 in both dtypes; 192 and
 // 256 (the paper's 1B/113B and 10B head widths) in bf16
@@ -60,6 +34,12 @@ struct BlockDims {
   int qk;
   float eps;
   orbit_dtype dt;
+  // the options' (block_opt): rotary positions of q and k, 8-bit products
+  bool rope = false, fp8 = false;
+  RopeDims rd{};
+  const float *pos = nullptr, *freq = nullptr;
+  orbit_block_fp8 w8{};
+  bool turned() const { return qk || rope; }  // q and k differ from the QKV product's
 };
 
 orbit_status block_dims(const char* fn, const orbit_block_desc* desc, BlockDims* o) {
@@ -113,6 +93,9 @@ struct BlockSaved {
   void* h2;
   void* u;
   void* g;
+  // 8-bit products: the transposed stores of h1, o, h2 and g, whose full tensors
+  // then pass through the workspace (o stays where the attention's backward reads it)
+  void *h1t, *ot, *h2t, *gt;
 };
 
 BlockSaved carve_block_saved(const BlockDims& z, const BlockExt& x, void* base, size_t* used) {
@@ -129,22 +112,26 @@ BlockSaved carve_block_saved(const BlockDims& z, const BlockExt& x, void* base, 
   }
   s.mu1 = c.take<float>(z.T);
   s.r1 = c.take<float>(z.T);
-  s.h1 = c.take<char>(z.T * z.d * e);
+  if (z.fp8) s.h1t = c.take<char>(fp8_store_bytes(z.d, z.T));
+  else s.h1 = c.take<char>(z.T * z.d * e);
   s.qkv = c.take<char>(z.T * 3 * z.A * e);
+  if (z.turned()) s.qkn = c.take<char>(z.T * 2 * z.A * e);
   if (z.qk) {
-    s.qkn = c.take<char>(z.T * 2 * z.A * e);
     s.qmu = c.take<float>(z.T * 2 * z.H);
     s.qr = c.take<float>(z.T * 2 * z.H);
   }
-  s.o = c.take<char>(z.T * z.A * e);
+  if (z.fp8) s.ot = c.take<char>(fp8_store_bytes(z.A, z.T));
+  if (!z.fp8 || z.dt == ORBIT_F32) s.o = c.take<char>(z.T * z.A * e);
   s.o32 = z.dt == ORBIT_BF16 ? c.take<float>(z.T * z.A) : nullptr;
   s.lse = c.take<float>(z.T * z.H);
   s.x1 = c.take<char>(z.T * z.d * e);
   s.mu2 = c.take<float>(z.T);
   s.r2 = c.take<float>(z.T);
-  s.h2 = c.take<char>(z.T * z.d * e);
+  if (z.fp8) s.h2t = c.take<char>(fp8_store_bytes(z.d, z.T));
+  else s.h2 = c.take<char>(z.T * z.d * e);
   s.u = c.take<char>(z.T * z.F * e);
-  s.g = c.take<char>(z.T * z.F * e);
+  if (z.fp8) s.gt = c.take<char>(fp8_store_bytes(z.F, z.T));
+  else s.g = c.take<char>(z.T * z.F * e);
   if (used) *used = c.used();
   return s;
 }
@@ -203,6 +190,9 @@ struct BlockWs {
   float* p_proj;
   void *gn1, *gn2;
   void* qws;
+  // 8-bit products only: a layer's input before it is packed [T, max(d, A, F)],
+  // and the stores of an input or of an output gradient and its transpose
+  void *act, *q8, *q8t;
   void* gws;
   size_t gws_bytes;
 };
@@ -219,6 +209,10 @@ size_t block_gemm_ws(const BlockDims& z) {
       {z.F, z.d, T, 0, 0},     {T, z.F, z.d, 1, 1}, {z.d, z.F, T, 0, 0}, {T, z.d, z.F, 1, 1},
       {z.A, z.d, T, 0, 0},     {T, z.A, z.d, 1, 1}, {z.d, 3 * z.A, T, 0, 0}, {T, z.d, 3 * z.A, 1, 1}};
   for (auto& sh : shapes) {
+    if (z.fp8) {
+      m = std::max(m, fp8_gemm_workspace_bytes(sh[0], sh[1], sh[2]));
+      continue;
+    }
     g.M = sh[0]; g.N = sh[1]; g.K = sh[2]; g.a_kmajor = sh[3]; g.b_kmajor = sh[4];
     m = std::max(m, gemm_workspace_bytes(g));
   }
@@ -239,18 +233,28 @@ size_t block_ws_layout(const BlockDims& z, const BlockExt& x, void* base, size_t
   t.D = static_cast<float*>(static_cast<void*>(c.take<char>(attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh))));
   // partials of the block's column reductions (all finished by one launch)
   const int T = (int)z.T;
-  t.p_fc1 = c.take<float>(colsum_part_bytes(T, z.F, false) / sizeof(float));
-  t.p_fc2 = c.take<float>(colsum_part_bytes(T, z.d, false) / sizeof(float));
+  // of a bias gradient: the packing of the output gradient leaves a row per 128 tokens
+  auto bias_part = [&](int n) {
+    return z.fp8 ? (size_t)cdiv(T, 128) * n : colsum_part_bytes(T, n, false) / sizeof(float);
+  };
+  t.p_fc1 = c.take<float>(bias_part(z.F));
+  t.p_fc2 = c.take<float>(bias_part(z.d));
   t.p_ln2 = c.take<float>(ln_bwd_cols_part_bytes(T, z.d, true) / sizeof(float));
-  t.p_qkv = c.take<float>(colsum_part_bytes(T, 3 * z.A, false) / sizeof(float));
+  t.p_qkv = c.take<float>(bias_part(3 * z.A));
   t.p_ln1 = c.take<float>(ln_bwd_cols_part_bytes(T, z.d, false) / sizeof(float));
   if (x.on) {
     t.df = c.take<char>(z.T * z.d * e);
-    t.p_proj = c.take<float>(colsum_part_bytes(T, z.d, false) / sizeof(float));
+    t.p_proj = c.take<float>(bias_part(z.d));
     t.gn1 = c.take<char>(gnorm_bwd_ws_bytes(block_gnorm(z, x, true)));
     t.gn2 = c.take<char>(gnorm_bwd_ws_bytes(block_gnorm(z, x, false)));
   }
-  t.qws = c.take<char>(qk_norm_bwd_workspace_bytes(z.dh));
+  t.qws = c.take<char>(z.rope ? rope_bwd_ws_bytes(z.rd) : qk_norm_bwd_workspace_bytes(z.dh));
+  if (z.fp8) {
+    const int widest = std::max({z.d, z.F, 3 * z.A});
+    t.act = c.take<char>(z.T * std::max({z.d, z.A, z.F}) * e);
+    t.q8 = c.take<char>(fp8_store_bytes(z.T, widest));
+    t.q8t = c.take<char>(fp8_store_bytes(widest, z.T));
+  }
   const size_t g = block_gemm_ws(z);
   t.gws = c.take<char>(g);
   const size_t used = c.used();
@@ -279,7 +283,7 @@ AttnIO block_attn_io(const BlockDims& z, const BlockSaved& sv) {
   AttnIO io{};
   io.B = z.B; io.H = z.H; io.L = z.L; io.dh = z.dh;
   io.v = static_cast<char*>(sv.qkv) + 2 * z.A * e; io.ldv = 3 * z.A;
-  if (z.qk) {
+  if (z.turned()) {
     io.q = sv.qkn; io.ldq = 2 * z.A; io.k = static_cast<char*>(sv.qkn) + z.A * e; io.ldk = 2 * z.A;
   } else {
     io.q = sv.qkv; io.ldq = 3 * z.A; io.k = static_cast<char*>(sv.qkv) + z.A * e; io.ldk = 3 * z.A;
@@ -287,10 +291,13 @@ AttnIO block_attn_io(const BlockDims& z, const BlockSaved& sv) {
   return io;
 }
 
-// sv.qkv -> sv.o, sv.lse and o32 (may be null), with the norms of q and k.
+// sv.qkv -> sv.o, sv.lse and o32 (may be null), with the norms and turns of q and k.
 orbit_status block_attention(const BlockDims& z, const orbit_block_params* p, const BlockSaved& sv, float* o32,
                              const BlockWs& w, hipStream_t s) {
-  if (z.qk)
+  if (z.rope)
+    ORBIT_TRY(rope_fwd(z.rd, RopeParams{p->qn_g, p->qn_b, p->kn_g, p->kn_b}, z.pos, z.freq, sv.qkv, 3 * z.A, sv.qkn,
+                       2 * z.A, sv.qmu, sv.qr, s));
+  else if (z.qk)
     ORBIT_TRY(qk_norm_fwd(z.dt, sv.qkv, 3 * z.A, sv.qkn, 2 * z.A, p->qn_g, p->qn_b, p->kn_g, p->kn_b, sv.qmu, sv.qr,
                           (int)z.T, z.H, z.dh, z.eps, s));
   // the attention backward's workspace is idle until it runs and holds the
@@ -299,22 +306,45 @@ orbit_status block_attention(const BlockDims& z, const orbit_block_params* p, co
                   attn_bwd_workspace_bytes(z.B, z.H, z.L, z.dh), s);
 }
 
+// A linear layer's product in the forward: x [T, in] W + bias with the residual or
+// the GELU that its epilogue takes. In 8 bits x is packed first, its transposed
+// store into xt for the backward.
+orbit_status block_linear(const BlockDims& z, const char* tag, const void* x, int in, const void* w, const void* w8t,
+                          const void* bias, void* xt, void* y, int out, const void* res, void* gelu_out,
+                          const BlockWs& ws, hipStream_t s) {
+  if (z.fp8) {
+    ORBIT_TRY(fp8_pack(z.dt, x, in, z.T, in, false, ws.q8, xt, nullptr, s));
+    Fp8Gemm g; g.dtype = z.dt; g.tag = tag;
+    g.A = ws.q8; g.B = w8t; g.C = y; g.ldc = out; g.M = (int)z.T; g.N = out; g.K = in;
+    g.epi.bias = bias; g.epi.res = res; g.epi.ldr = out; g.epi.gelu_out = gelu_out; g.epi.ldgo = out;
+    return fp8_gemm(g, ws.gws, ws.gws_bytes, s);
+  }
+  Gemm g; g.dtype = z.dt; g.tag = tag;
+  g.A = x; g.lda = in; g.B = w; g.ldb = out; g.C = y; g.ldc = out;
+  g.M = (int)z.T; g.N = out; g.K = in; g.bias = bias;
+  if (res) { g.res = res; g.ldr = out; }
+  if (gelu_out) { g.gelu_out = gelu_out; g.ldgo = out; }
+  return gemm(g, ws.gws, ws.gws_bytes, s);
+}
+
 // The forward's kernel sequence, writing the tensors the backward reads into
 // `sv`. With y == NULL the last product (fc2) is skipped where the backward
 // does not read its output: the recompute of the activation-checkpoint
 // backward. s8 (may be null): the 8-bit stores, written as the tensors appear.
 orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const orbit_block_params* p,
-                                 const orbit_block_ext_params* ep, const void* x, void* y, const BlockSaved& sv,
+                                 const orbit_block_ext_params* ep, const void* x, void* y, const BlockSaved& stored,
                                  const BlockSaved8* s8, const BlockWs& w, hipStream_t s) {
   const int T = (int)z.T;
   const orbit_dtype dt = z.dt;
-  ORBIT_TRY(layernorm_fwd(dt, x, z.d, p->ln1_g, p->ln1_b, sv.h1, z.d, sv.mu1, sv.r1, T, z.d, z.eps, s));
-  {
-    Gemm g; g.dtype = dt; g.tag = "qkv";
-    g.A = sv.h1; g.lda = z.d; g.B = p->w_qkv; g.ldb = 3 * z.A; g.C = sv.qkv; g.ldc = 3 * z.A;
-    g.M = T; g.N = 3 * z.A; g.K = z.d; g.bias = p->b_qkv;
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+  BlockSaved sv = stored;
+  if (z.fp8) {
+    // packed as soon as they are there
+    sv.h1 = sv.h2 = sv.g = w.act;
+    if (!sv.o) sv.o = w.act;
   }
+  ORBIT_TRY(layernorm_fwd(dt, x, z.d, p->ln1_g, p->ln1_b, sv.h1, z.d, sv.mu1, sv.r1, T, z.d, z.eps, s));
+  ORBIT_TRY(block_linear(z, "qkv", sv.h1, z.d, p->w_qkv, z.w8.w_qkv_t, p->b_qkv, sv.h1t, sv.qkv, 3 * z.A, nullptr, nullptr,
+                         w, s));
   // the float32 o is for the backward, which forms it again from the stores
   ORBIT_TRY(block_attention(z, p, sv, s8 ? nullptr : sv.o32, w, s));
   if (s8) {
@@ -325,13 +355,8 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
   // buffer of the backward that is idle here
   void* f1 = ext.branch() ? sv.f1 : w.dx1;
   void* f2 = ext.branch() ? sv.f2 : w.dh;
-  {
-    Gemm g; g.dtype = dt; g.tag = "proj";
-    g.A = sv.o; g.lda = z.A; g.B = p->w_proj; g.ldb = z.d; g.C = ext.normed() ? f1 : sv.x1; g.ldc = z.d;
-    g.M = T; g.N = z.d; g.K = z.A; g.bias = p->b_proj;
-    if (!ext.normed()) { g.res = x; g.ldr = z.d; }
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
+  ORBIT_TRY(block_linear(z, "proj", sv.o, z.A, p->w_proj, z.w8.w_proj_t, p->b_proj, sv.ot, ext.normed() ? f1 : sv.x1, z.d,
+                         ext.normed() ? nullptr : x, nullptr, w, s));
   if (ext.normed()) {
     ORBIT_TRY(gnorm_fwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), x, f1, s8 ? s8->f1 : nullptr, sv.x1,
                         sv.h2, sv.st1, s));
@@ -341,20 +366,13 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
     // smaller than the residual stream, and stored with a step to match
     if (s8) ORBIT_TRY(act8_pack(dt, sv.x1, x, z.d, T, z.d, s8->f1, s));
   }
-  {
-    Gemm g; g.dtype = dt; g.tag = "fc1";
-    g.A = sv.h2; g.lda = z.d; g.B = p->w_fc1; g.ldb = z.F; g.C = sv.g; g.ldc = z.F;
-    g.M = T; g.N = z.F; g.K = z.d; g.bias = p->b_fc1; g.gelu_out = sv.u; g.ldgo = z.F;
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
+  ORBIT_TRY(block_linear(z, "fc1", sv.h2, z.d, p->w_fc1, z.w8.w_fc1_t, p->b_fc1, sv.h2t, sv.g, z.F, nullptr, sv.u, w, s));
   if (s8) ORBIT_TRY(act8_pack(dt, sv.u, nullptr, z.F, T, z.F, s8->u, s));
-  if (y || ext.branch()) {
-    Gemm g; g.dtype = dt; g.tag = "fc2";
-    g.A = sv.g; g.lda = z.F; g.B = p->w_fc2; g.ldb = z.d; g.C = ext.normed() ? f2 : y; g.ldc = z.d;
-    g.M = T; g.N = z.d; g.K = z.F; g.bias = p->b_fc2;
-    if (!ext.normed()) { g.res = sv.x1; g.ldr = z.d; }
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
+  if (y || ext.branch())
+    ORBIT_TRY(block_linear(z, "fc2", sv.g, z.F, p->w_fc2, z.w8.w_fc2_t, p->b_fc2, sv.gt, ext.normed() ? f2 : y, z.d,
+                           ext.normed() ? nullptr : sv.x1, nullptr, w, s));
+  else if (z.fp8)  // the backward reads its input's store
+    ORBIT_TRY(fp8_pack(dt, sv.g, z.F, T, z.F, false, nullptr, sv.gt, nullptr, s));
   // the recompute runs this norm too where the backward reads its statistics;
   // its output then goes to an idle buffer
   if (ext.normed() && (y || ext.post))
@@ -407,7 +425,8 @@ orbit_status block_forward(const BlockDims& z, BlockExt ext, const orbit_block_p
   BlockWs w;
   block_ws_layout(z, ext, ws, ws_bytes, &w);
   if (!saved) ext.act8 = false;
-  const BlockSaved sv = carve_block_saved(z, ext, saved == nullptr || ext.act8 ? ws : saved, nullptr);
+  BlockSaved sv = carve_block_saved(z, ext, saved == nullptr || ext.act8 ? ws : saved, nullptr);
+  if (!saved) sv.h1t = sv.ot = sv.h2t = sv.gt = nullptr;  // nothing reads them
   BlockSaved8 s8{};
   if (ext.act8) s8 = carve_block_saved8(z, ext, saved, nullptr);
   return block_forward_steps(z, ext, p, ep, x, y, sv, ext.act8 ? &s8 : nullptr, w, s);
@@ -491,6 +510,17 @@ static orbit_status block_ext_params_check(const char* fn, const BlockExt& x, co
   return ORBIT_OK;
 }
 
+static orbit_status block_ext_grads_check(const char* fn, const BlockExt& x, const orbit_block_ext_grads* eg) {
+  if (!x.branch()) return ORBIT_OK;
+  REQ(eg != nullptr, ORBIT_E_ARG, "%s: ext grads is NULL", fn);
+  if (x.gates) { PTR(eg->gate1, "grads.gate1"); PTR(eg->gate2, "grads.gate2"); }
+  if (x.post) {
+    PTR(eg->post1_g, "grads.post1_g"); PTR(eg->post1_b, "grads.post1_b");
+    PTR(eg->post2_g, "grads.post2_g"); PTR(eg->post2_b, "grads.post2_b");
+  }
+  return ORBIT_OK;
+}
+
 size_t orbit_vit_block_ext_saved_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext) {
   const char* fn = "orbit_vit_block_ext_saved_bytes";
   BlockDims z;
@@ -533,14 +563,91 @@ orbit_status orbit_vit_block_ext_bwd(const orbit_block_desc* desc, const orbit_b
   ORBIT_TRY(block_dims(fn, desc, &z));
   ORBIT_TRY(block_ext(fn, z, ext, &e));
   ORBIT_TRY(block_ext_params_check(fn, e, ep));
-  if (e.branch()) {
-    REQ(eg != nullptr, ORBIT_E_ARG, "%s: ext grads is NULL", fn);
-    if (e.gates) { PTR(eg->gate1, "grads.gate1"); PTR(eg->gate2, "grads.gate2"); }
-    if (e.post) {
-      PTR(eg->post1_g, "grads.post1_g"); PTR(eg->post1_b, "grads.post1_b");
-      PTR(eg->post2_g, "grads.post2_g"); PTR(eg->post2_b, "grads.post2_b");
+  ORBIT_TRY(block_ext_grads_check(fn, e, eg));
+  return block_backward(fn, z, e, p, ep, x, saved, dy, dx, gr, eg, accumulate, ws, ws_bytes, S(stream));
+}
+
+// ---------------------------------------------------------------------------
+// block with rotary positions and / or 8-bit products
+// ---------------------------------------------------------------------------
+// Fills z with the options. launch: the device pointers are needed too.
+static orbit_status block_opt(const char* fn, const orbit_block_opt* o, const BlockExt& ext, bool launch, BlockDims* z) {
+  REQ(o != nullptr, ORBIT_E_ARG, "%s: opt is NULL", fn);
+  if (o->rope) {
+    const orbit_block_rope& r = *o->rope;
+    z->rope = true;
+    z->rd.T = (int)z->T; z->rd.qh = z->rd.kh = z->H; z->rd.dh = z->dh;
+    z->rd.norm = z->qk != 0; z->rd.eps = z->eps; z->rd.dt = z->dt;
+    REQ(z->T < (1 << 24), ORBIT_E_UNSUPPORTED, "%s: %lld tokens reach 2^24, too many for rope", fn, (long long)z->T);
+    ORBIT_TRY(rope_axes(fn, r.axes, r.pos_rows, r.near, r.axis, &z->rd));
+    if (launch) { PTR(r.pos, "rope.pos"); PTR(r.freq, "rope.freq"); }
+    z->pos = r.pos; z->freq = r.freq;
+  }
+  if (o->fp8) {
+    REQ(!ext.act8, ORBIT_E_UNSUPPORTED, "%s: fp8 and act8 do not go together", fn);
+    z->fp8 = true;
+    z->w8 = *o->fp8;
+    const int64_t widest = std::max({(int64_t)3 * z->A, (int64_t)z->F, (int64_t)z->d});
+    REQ(z->T < (1 << 22) && widest < (1 << 22) && cdiv(z->T, 128) * cdiv(widest, 128) < (1 << 23), ORBIT_E_UNSUPPORTED,
+        "%s: %lld tokens of %lld values are too many for 8-bit products", fn, (long long)z->T, (long long)widest);
+    if (launch) {
+      const orbit_block_fp8& w = z->w8;
+      PTR(w.w_qkv, "fp8.w_qkv"); PTR(w.w_qkv_t, "fp8.w_qkv_t"); PTR(w.w_proj, "fp8.w_proj"); PTR(w.w_proj_t, "fp8.w_proj_t");
+      PTR(w.w_fc1, "fp8.w_fc1"); PTR(w.w_fc1_t, "fp8.w_fc1_t"); PTR(w.w_fc2, "fp8.w_fc2"); PTR(w.w_fc2_t, "fp8.w_fc2_t");
     }
   }
+  return ORBIT_OK;
+}
+
+static orbit_status block_opt_dims(const char* fn, const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                   const orbit_block_opt* opt, bool launch, BlockDims* z, BlockExt* x) {
+  ORBIT_TRY(block_dims(fn, desc, z));
+  ORBIT_TRY(block_ext(fn, *z, ext, x));
+  return block_opt(fn, opt, *x, launch, z);
+}
+
+size_t orbit_vit_block_opt_saved_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                       const orbit_block_opt* opt) {
+  BlockDims z;
+  BlockExt x;
+  if (block_opt_dims("orbit_vit_block_opt_saved_bytes", desc, ext, opt, false, &z, &x) != ORBIT_OK) return 0;
+  return block_saved_bytes(z, x);
+}
+
+size_t orbit_vit_block_opt_workspace_bytes(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                           const orbit_block_opt* opt) {
+  BlockDims z;
+  BlockExt x;
+  if (block_opt_dims("orbit_vit_block_opt_workspace_bytes", desc, ext, opt, false, &z, &x) != ORBIT_OK) return 0;
+  return block_ws_bytes(z, x);
+}
+
+orbit_status orbit_vit_block_opt_fwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_opt* opt, const orbit_block_params* p,
+                                     const orbit_block_ext_params* ep, const void* x, void* y, void* saved, void* ws,
+                                     size_t ws_bytes, void* stream) {
+  const char* fn = "orbit_vit_block_opt_fwd";
+  clear_error();
+  BlockDims z;
+  BlockExt e;
+  ORBIT_TRY(block_opt_dims(fn, desc, ext, opt, true, &z, &e));
+  ORBIT_TRY(block_fwd_check(fn, z, e, p, x, y, saved, ws, ws_bytes));
+  ORBIT_TRY(block_ext_params_check(fn, e, ep));
+  return block_forward(z, e, p, ep, x, y, saved, ws, ws_bytes, S(stream));
+}
+
+orbit_status orbit_vit_block_opt_bwd(const orbit_block_desc* desc, const orbit_block_ext* ext,
+                                     const orbit_block_opt* opt, const orbit_block_params* p,
+                                     const orbit_block_ext_params* ep, const void* x, const void* saved, const void* dy,
+                                     void* dx, const orbit_block_grads* gr, const orbit_block_ext_grads* eg,
+                                     int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "orbit_vit_block_opt_bwd";
+  clear_error();
+  BlockDims z;
+  BlockExt e;
+  ORBIT_TRY(block_opt_dims(fn, desc, ext, opt, true, &z, &e));
+  ORBIT_TRY(block_ext_params_check(fn, e, ep));
+  ORBIT_TRY(block_ext_grads_check(fn, e, eg));
   return block_backward(fn, z, e, p, ep, x, saved, dy, dx, gr, eg, accumulate, ws, ws_bytes, S(stream));
 }
 
@@ -609,6 +716,21 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   auto bias_job = [](ColJob& j, const void* src, int64_t n, float* part, float* out) {
     j.src = src; j.ld = n; j.n = (int)n; j.part = part; j.out_sum = out;
   };
+  // a linear layer's backward in 8 bits: the output gradient is packed in both
+  // orientations, and leaves its column sums (the bias gradient) where part is given
+  auto linear8 = [&](const char* tag_dx, const char* tag_dw, const void* g_out, int out, const void* xt, int in,
+                     const void* w8, void* g_in, const void* gelu_in, float* dw, float* part, float* db) -> orbit_status {
+    ORBIT_TRY(fp8_pack(dt, g_out, out, T, out, false, w.q8, w.q8t, part, s));
+    if (part) fin.add(part, out, (int)cdiv(T, 128), out, db);
+    Fp8Gemm g; g.dtype = dt; g.tag = tag_dw;
+    g.A = xt; g.B = w.q8t; g.C = dw; g.ldc = out; g.M = in; g.N = out; g.K = T; g.out_f32 = true;
+    g.epi.accumulate = accumulate;
+    ORBIT_TRY(fp8_gemm(g, w.gws, w.gws_bytes, s));
+    Fp8Gemm h; h.dtype = dt; h.tag = tag_dx;
+    h.A = w.q8; h.B = w8; h.C = g_in; h.ldc = in; h.M = T; h.N = in; h.K = out;
+    h.epi.gelu_in = gelu_in; h.epi.ldgi = in;
+    return fp8_gemm(h, w.gws, w.gws_bytes, s);
+  };
   // the feed-forward sub-layer's output gradient: dy, or through its gated norm
   const void* dff = dy;
   if (ext.normed()) {
@@ -620,42 +742,47 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     dff = w.df;
   }
   // feed-forward sub-layer
-  bool fused_fc2, fused_fc1;
-  {
-    Gemm g; g.dtype = dt; g.tag = "fc2_dw";
-    g.A = sv.g; g.lda = z.F; g.a_kmajor = false; g.B = dff; g.ldb = z.d; g.b_kmajor = false;
-    g.C = gr->w_fc2; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
-    g.M = z.F; g.N = z.d; g.K = T;
-    fused_fc2 = dw_bias(g, w.p_fc2, gr->b_fc2);
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
-  {
-    Gemm g; g.dtype = dt; g.tag = "fc2_dx";
-    g.A = dff; g.lda = z.d; g.B = p->w_fc2; g.ldb = z.d; g.b_kmajor = true;
-    g.C = w.du; g.ldc = z.F; g.M = T; g.N = z.F; g.K = z.d; g.gelu_in = sv.u; g.ldgi = z.F;
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
-  {
-    Gemm g; g.dtype = dt; g.tag = "fc1_dw";
-    g.A = sv.h2; g.lda = z.d; g.a_kmajor = false; g.B = w.du; g.ldb = z.F; g.b_kmajor = false;
-    g.C = gr->w_fc1; g.ldc = z.F; g.out_f32 = true; g.accumulate = acc;
-    g.M = z.d; g.N = z.F; g.K = T;
-    fused_fc1 = dw_bias(g, w.p_fc1, gr->b_fc1);
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
-  {
-    ColJob j[2];
-    int nj = 0;
-    if (!fused_fc1) bias_job(j[nj++], w.du, z.F, w.p_fc1, gr->b_fc1);
-    if (!fused_fc2) bias_job(j[nj++], dff, z.d, w.p_fc2, gr->b_fc2);
-    if (nj) ORBIT_TRY(colsum_partials(dt, j, nj, T, s));
-    for (int i = 0; i < nj; ++i) fin.add_job(j[i], T);
-  }
-  {
-    Gemm g; g.dtype = dt; g.tag = "fc1_dx";
-    g.A = w.du; g.lda = z.F; g.B = p->w_fc1; g.ldb = z.F; g.b_kmajor = true;
-    g.C = w.dh; g.ldc = z.d; g.M = T; g.N = z.d; g.K = z.F;
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+  if (z.fp8) {
+    ORBIT_TRY(linear8("fc2_dx", "fc2_dw", dff, z.d, sv.gt, z.F, z.w8.w_fc2, w.du, sv.u, gr->w_fc2, w.p_fc2, gr->b_fc2));
+    ORBIT_TRY(linear8("fc1_dx", "fc1_dw", w.du, z.F, sv.h2t, z.d, z.w8.w_fc1, w.dh, nullptr, gr->w_fc1, w.p_fc1, gr->b_fc1));
+  } else {
+    bool fused_fc2, fused_fc1;
+    {
+      Gemm g; g.dtype = dt; g.tag = "fc2_dw";
+      g.A = sv.g; g.lda = z.F; g.a_kmajor = false; g.B = dff; g.ldb = z.d; g.b_kmajor = false;
+      g.C = gr->w_fc2; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
+      g.M = z.F; g.N = z.d; g.K = T;
+      fused_fc2 = dw_bias(g, w.p_fc2, gr->b_fc2);
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
+    {
+      Gemm g; g.dtype = dt; g.tag = "fc2_dx";
+      g.A = dff; g.lda = z.d; g.B = p->w_fc2; g.ldb = z.d; g.b_kmajor = true;
+      g.C = w.du; g.ldc = z.F; g.M = T; g.N = z.F; g.K = z.d; g.gelu_in = sv.u; g.ldgi = z.F;
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
+    {
+      Gemm g; g.dtype = dt; g.tag = "fc1_dw";
+      g.A = sv.h2; g.lda = z.d; g.a_kmajor = false; g.B = w.du; g.ldb = z.F; g.b_kmajor = false;
+      g.C = gr->w_fc1; g.ldc = z.F; g.out_f32 = true; g.accumulate = acc;
+      g.M = z.d; g.N = z.F; g.K = T;
+      fused_fc1 = dw_bias(g, w.p_fc1, gr->b_fc1);
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
+    {
+      ColJob j[2];
+      int nj = 0;
+      if (!fused_fc1) bias_job(j[nj++], w.du, z.F, w.p_fc1, gr->b_fc1);
+      if (!fused_fc2) bias_job(j[nj++], dff, z.d, w.p_fc2, gr->b_fc2);
+      if (nj) ORBIT_TRY(colsum_partials(dt, j, nj, T, s));
+      for (int i = 0; i < nj; ++i) fin.add_job(j[i], T);
+    }
+    {
+      Gemm g; g.dtype = dt; g.tag = "fc1_dx";
+      g.A = w.du; g.lda = z.F; g.B = p->w_fc1; g.ldb = z.F; g.b_kmajor = true;
+      g.C = w.dh; g.ldc = z.d; g.M = T; g.N = z.d; g.K = z.F;
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
   }
   // LN2 backward; the chunk sums of its rows give the LN2 parameter gradients
   // and, summed over its output dx1, the projection's bias gradient
@@ -676,26 +803,32 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     ORBIT_TRY(gnorm_bwd(block_gnorm(z, ext, true), block_gnorm_params(p, ep, 1), restore ? nullptr : sv.f1, s8.f1,
                         sv.x1, sv.st1, w.dh, dy, w.dx1, same ? nullptr : w.df, gg, accumulate, w.gn1, s));
   }
-  {
-    Gemm g; g.dtype = dt; g.tag = "proj_dw";
-    g.A = o_proj; g.lda = z.A; g.a_kmajor = false; g.B = df1; g.ldb = z.d; g.b_kmajor = false;
-    g.C = gr->w_proj; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
-    g.M = z.A; g.N = z.d; g.K = T;
-    const bool fused = !plain_ln2 && dw_bias(g, w.p_proj, gr->b_proj);
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-    if (!plain_ln2 && !fused) {
-      ColJob j[1];
-      bias_job(j[0], df1, z.d, w.p_proj, gr->b_proj);
-      ORBIT_TRY(colsum_partials(dt, j, 1, T, s));
-      fin.add_job(j[0], T);
+  if (z.fp8) {
+    // the LN2 backward has formed the bias gradient in the plain residual
+    ORBIT_TRY(linear8("proj_dx", "proj_dw", df1, z.d, sv.ot, z.A, z.w8.w_proj, w.dO, nullptr, gr->w_proj,
+                      plain_ln2 ? nullptr : w.p_proj, gr->b_proj));
+  } else {
+    {
+      Gemm g; g.dtype = dt; g.tag = "proj_dw";
+      g.A = o_proj; g.lda = z.A; g.a_kmajor = false; g.B = df1; g.ldb = z.d; g.b_kmajor = false;
+      g.C = gr->w_proj; g.ldc = z.d; g.out_f32 = true; g.accumulate = acc;
+      g.M = z.A; g.N = z.d; g.K = T;
+      const bool fused = !plain_ln2 && dw_bias(g, w.p_proj, gr->b_proj);
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+      if (!plain_ln2 && !fused) {
+        ColJob j[1];
+        bias_job(j[0], df1, z.d, w.p_proj, gr->b_proj);
+        ORBIT_TRY(colsum_partials(dt, j, 1, T, s));
+        fin.add_job(j[0], T);
+      }
     }
-  }
-  // attention sub-layer
-  {
-    Gemm g; g.dtype = dt; g.tag = "proj_dx";
-    g.A = df1; g.lda = z.d; g.B = p->w_proj; g.ldb = z.d; g.b_kmajor = true;
-    g.C = w.dO; g.ldc = z.A; g.M = T; g.N = z.A; g.K = z.d;
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    // attention sub-layer
+    {
+      Gemm g; g.dtype = dt; g.tag = "proj_dx";
+      g.A = df1; g.lda = z.d; g.B = p->w_proj; g.ldb = z.d; g.b_kmajor = true;
+      g.C = w.dO; g.ldc = z.A; g.M = T; g.N = z.A; g.K = z.d;
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
   }
   const AttnIO io = block_attn_io(z, sv);
   char* dq = static_cast<char*>(w.dqkv);
@@ -703,29 +836,39 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
     ORBIT_TRY(attn_bwd(dt, io, sv.o32, z.A, 1, sv.lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
   else
     ORBIT_TRY(attn_bwd(dt, io, sv.o, z.A, 0, sv.lse, w.dO, z.A, dq, dq + z.A * e, dq + 2 * z.A * e, 3 * z.A, w.D, s));
-  if (z.qk) {
+  if (z.rope) {
+    ORBIT_TRY(rope_bwd(z.rd, RopeParams{p->qn_g, p->qn_b, p->kn_g, p->kn_b}, z.pos, z.freq, sv.qkv, 3 * z.A, sv.qmu, sv.qr,
+                       w.dqkv, 3 * z.A, w.dqkv, 3 * z.A, RopeGrads{gr->qn_g, gr->qn_b, gr->kn_g, gr->kn_b}, accumulate,
+                       w.qws, &fin, s));
+  } else if (z.qk) {
     ORBIT_TRY(qk_norm_bwd(dt, w.dqkv, 3 * z.A, sv.qkv, 3 * z.A, sv.qmu, sv.qr, p->qn_g, p->kn_g, gr->qn_g, gr->qn_b,
                           gr->kn_g, gr->kn_b, accumulate, T, z.H, z.dh, w.qws, &fin, s));
-  } else if (!acc) {
+  }
+  if (!z.qk && !acc) {
     ORBIT_TRY(fill_f32(gr->qn_g, z.dh, 0.f, s));
     ORBIT_TRY(fill_f32(gr->qn_b, z.dh, 0.f, s));
     ORBIT_TRY(fill_f32(gr->kn_g, z.dh, 0.f, s));
     ORBIT_TRY(fill_f32(gr->kn_b, z.dh, 0.f, s));
   }
-  bool fused_qkv;
-  {
-    Gemm g; g.dtype = dt; g.tag = "qkv_dw";
-    g.A = sv.h1; g.lda = z.d; g.a_kmajor = false; g.B = w.dqkv; g.ldb = 3 * z.A; g.b_kmajor = false;
-    g.C = gr->w_qkv; g.ldc = 3 * z.A; g.out_f32 = true; g.accumulate = acc;
-    g.M = z.d; g.N = 3 * z.A; g.K = T;
-    fused_qkv = dw_bias(g, w.p_qkv, gr->b_qkv);
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
-  }
-  {
-    Gemm g; g.dtype = dt; g.tag = "qkv_dx";
-    g.A = w.dqkv; g.lda = 3 * z.A; g.B = p->w_qkv; g.ldb = 3 * z.A; g.b_kmajor = true;
-    g.C = w.dh; g.ldc = z.d; g.M = T; g.N = z.d; g.K = 3 * z.A;
-    ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+  bool fused_qkv = true;
+  if (z.fp8) {
+    ORBIT_TRY(linear8("qkv_dx", "qkv_dw", w.dqkv, 3 * z.A, sv.h1t, z.d, z.w8.w_qkv, w.dh, nullptr, gr->w_qkv, w.p_qkv,
+                      gr->b_qkv));
+  } else {
+    {
+      Gemm g; g.dtype = dt; g.tag = "qkv_dw";
+      g.A = sv.h1; g.lda = z.d; g.a_kmajor = false; g.B = w.dqkv; g.ldb = 3 * z.A; g.b_kmajor = false;
+      g.C = gr->w_qkv; g.ldc = 3 * z.A; g.out_f32 = true; g.accumulate = acc;
+      g.M = z.d; g.N = 3 * z.A; g.K = T;
+      fused_qkv = dw_bias(g, w.p_qkv, gr->b_qkv);
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
+    {
+      Gemm g; g.dtype = dt; g.tag = "qkv_dx";
+      g.A = w.dqkv; g.lda = 3 * z.A; g.B = p->w_qkv; g.ldb = 3 * z.A; g.b_kmajor = true;
+      g.C = w.dh; g.ldc = z.d; g.M = T; g.N = z.d; g.K = 3 * z.A;
+      ORBIT_TRY(gemm(g, w.gws, w.gws_bytes, s));
+    }
   }
   ORBIT_TRY(layernorm_bwd_cols(dt, w.dh, z.d, x, z.d, sv.mu1, sv.r1, p->ln1_g, w.dx1, dx, z.d, T, z.d, w.p_ln1,
                                gr->ln1_b, gr->ln1_g, nullptr, fin, s));

@@ -96,4 +96,8 @@ ORBIT_DEV void epi_apply8(const Epi& e, int64_t bz, int r, int c0, float* v, Out
   st8(C + off, v);
 }
 
+// C = epilogue(sum over a.splits of the float32 partials), the second launch of a
+// product with split K
+orbit_status splitk_finish(orbit_dtype dt, bool out_f32, const GemmKArgs& a, hipStream_t s);
+
 }  // namespace orbit

@@ -11,7 +11,8 @@ enqueues the entry points in order on the current stream:
     agg + stack: orbit_var_aggregate -> blocks -> blocks backward -> orbit_var_aggregate_bwd
 
 (the _ext calls are the plain block's, bit for bit, unless the dims ask for
-gates, norms or a scale of the residuals, or checkpoint is "act8")
+gates, norms or a scale of the residuals, or checkpoint is "act8"; with rotary
+positions or 8-bit products they are orbit_vit_block_opt_fwd / _bwd)
 
 Only marshalling happens here; every step runs in the HIP library.
 """
@@ -22,7 +23,8 @@ from typing import Dict, List, Optional
 
 import torch
 
-from ._lib import (AggDesc, BlockDesc, BlockExt, EmbedDesc, HeadDesc, ORBIT_BF16, ORBIT_F32, OrbitLib, WmseDesc)
+from ._lib import (AggDesc, BLOCK_FP8_WEIGHTS, BlockDesc, BlockExt, BlockOpt, BlockRope, EmbedDesc, HeadDesc, ORBIT_BF16,
+                   ORBIT_F32, OrbitLib, WmseDesc)
 
 
 @dataclasses.dataclass
@@ -69,12 +71,36 @@ def _code(dt: str) -> int:
     return ORBIT_BF16 if dt == "bf16" else ORBIT_F32
 
 
+@dataclasses.dataclass
+class Rope:
+    """Rotary positions of the blocks' queries and keys: pair i of a head turns by
+    pos[token % len(pos), axis[i]] * freq[i] (see orbit_qk_rope_desc in orbit.h)."""
+    pos: torch.Tensor     # [rows, axes] float32, rows dividing the tokens
+    freq: torch.Tensor    # [head_dim / 2] float32
+    axis: List[int]       # [head_dim / 2]
+    near: bool = False    # pairs (2i, 2i + 1) instead of (i, i + head_dim / 2)
+
+
+def grid_rope(rows: int, cols: int, head_dim: int, theta: float = 100.0, device="cuda") -> Rope:
+    """Positions of a rows x cols grid of patches (latitude, longitude), token by
+    token in rows: the first half of a head's pairs turns with the row, the second
+    with the column, at frequencies theta^(-j / n) of the n pairs of an axis."""
+    half = head_dim // 2
+    axis = [int(2 * i >= half) for i in range(half)]
+    freq = [theta ** (-(i - axis.index(a)) / axis.count(a)) for i, a in enumerate(axis)]
+    r, c = torch.meshgrid(torch.arange(rows), torch.arange(cols), indexing="ij")
+    pos = torch.stack([r.flatten(), c.flatten()], -1).float()
+    return Rope(pos.to(device), torch.tensor(freq, dtype=torch.float32).to(device), axis)
+
+
 class ViTPass:
     """Device state of one forward+backward pass (see module docstring)."""
 
     def __init__(self, lib: OrbitLib, dims: PassDims, params: Dict[str, object], device="cuda",
-                 checkpoint=False):
-        """checkpoint: True for activation checkpointing of the blocks
+                 checkpoint=False, fp8: bool = False, rope: Optional[Rope] = None):
+        """fp8: the blocks' linear layers as 8-bit floating-point products; every
+        pass packs the weights first (pack_weights). rope: rotary positions on the
+        blocks' queries and keys. checkpoint: True for activation checkpointing of the blocks
         (Sec. III-B): the forward keeps only each block's input and the backward
         recomputes the rest (orbit_vit_block_bwd with saved = NULL). "act8": the
         forward keeps the blocks' activations in 8 bits
@@ -91,10 +117,23 @@ class ViTPass:
         self.params = params
         self.bdesc = BlockDesc(z.B, z.L, z.d, z.heads, z.head_dim, z.mlp, z.qk_norm, z.eps, code)
         self.bext = BlockExt(int(act8), z.post_norm, z.gate_rows, z.res_scale)
-        ws = lib.orbit_vit_block_ext_workspace_bytes(self.bdesc, self.bext)
+        self.fp8, self.rope, self.opts = fp8, rope, None
+        if fp8 or rope is not None:
+            if rope is not None and not (len(rope.axis) == rope.freq.numel() == z.head_dim // 2):
+                raise ValueError(f"rope needs a frequency and an axis for each of {z.head_dim // 2} pairs")
+            r = None if rope is None else BlockRope.of(rope.axis, rope.pos.shape[1], rope.pos.shape[0], rope.pos,
+                                                       rope.freq, rope.near)
+            self.w8 = [{n + t: torch.empty(lib.orbit_fp8_bytes(*(bp[n].shape[::-1] if t else bp[n].shape)),
+                                           dtype=torch.uint8, device=self.dev)
+                        for n in BLOCK_FP8_WEIGHTS for t in ("", "_t")} if fp8 else None for bp in params["blocks"]]
+            self.opts = [BlockOpt.of(r, w) for w in self.w8]
+            ws = lib.orbit_vit_block_opt_workspace_bytes(self.bdesc, self.bext, self.opts[0])
+            sb = lib.orbit_vit_block_opt_saved_bytes(self.bdesc, self.bext, self.opts[0])
+        else:
+            ws = lib.orbit_vit_block_ext_workspace_bytes(self.bdesc, self.bext)
+            sb = lib.orbit_vit_block_ext_saved_bytes(self.bdesc, self.bext)
         if ws == 0:
             raise ValueError(f"invalid block description: {lib.last_error()}")
-        sb = lib.orbit_vit_block_ext_saved_bytes(self.bdesc, self.bext)
         E = lambda *shape, dt=tdt: torch.empty(*shape, dtype=dt, device=self.dev)
         F32 = lambda *shape: torch.zeros(*shape, dtype=torch.float32, device=self.dev)
         self.xs = [E(z.B, z.L, z.d) for _ in range(z.blocks + 1)]
@@ -132,6 +171,27 @@ class ViTPass:
         self.ws = torch.empty(ws, dtype=torch.uint8, device=self.dev)
 
     # ------------------------------------------------------------------------
+    def pack_weights(self):
+        """The blocks' weights into their 8-bit stores, in both orientations."""
+        for bp, w8 in zip(self.params["blocks"], self.w8):
+            for n in BLOCK_FP8_WEIGHTS:
+                rows, cols = bp[n].shape
+                self.lib.orbit_fp8_pack(self.bdesc.dtype, rows, cols, 128, bp[n], cols, w8[n], w8[n + "_t"])
+
+    def _block_fwd(self, i):
+        a = (self.params["blocks"][i], self.xs[i], self.xs[i + 1], self.saved[i], self.ws)
+        if self.opts:
+            self.lib.orbit_vit_block_opt_fwd(self.bdesc, self.bext, self.opts[i], *a)
+        else:
+            self.lib.orbit_vit_block_ext_fwd(self.bdesc, self.bext, *a)
+
+    def _block_bwd(self, i, dy, dx, accumulate):
+        a = (self.params["blocks"][i], self.xs[i], self.saved[i], dy, dx, self.grads["blocks"][i], accumulate, self.ws)
+        if self.opts:
+            self.lib.orbit_vit_block_opt_bwd(self.bdesc, self.bext, self.opts[i], *a)
+        else:
+            self.lib.orbit_vit_block_ext_bwd(self.bdesc, self.bext, *a)
+
     def forward_backward(self, inputs: Dict[str, torch.Tensor], accumulate: int = 0, marks=None):
         """inputs: full -> img, tgt; blocks -> x, dy; agg_blocks -> tok, dy.
         Returns the loss tensor (full) or the input gradient. With a list for
@@ -160,9 +220,10 @@ class ViTPass:
         else:
             self.xs[0] = inputs["x"]
         mark("blocks_fwd")
+        if self.fp8:
+            self.pack_weights()
         for i in range(z.blocks):
-            lib.orbit_vit_block_ext_fwd(self.bdesc, self.bext, P["blocks"][i], self.xs[i], self.xs[i + 1],
-                                        self.saved[i], self.ws)
+            self._block_fwd(i)
         mark("blocks_fwd_end")
         if z.mode == "full":
             lib.orbit_head_fwd(self.hdesc, self.xs[-1], P["head"], self.pred, self.hsaved, self.ws)
@@ -179,8 +240,7 @@ class ViTPass:
         mark("blocks_bwd")
         for i in range(z.blocks - 1, -1, -1):
             dx = bufs[i % 2] if dy is not bufs[i % 2] else bufs[(i + 1) % 2]
-            lib.orbit_vit_block_ext_bwd(self.bdesc, self.bext, P["blocks"][i], self.xs[i], self.saved[i], dy, dx,
-                                        G["blocks"][i], accumulate, self.ws)
+            self._block_bwd(i, dy, dx, accumulate)
             dy = dx
         mark("blocks_bwd_end")
         self.dx = dy
