@@ -43,10 +43,13 @@ def _nbytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+_AxisArray = c_uint8 * ROPE_PAIRS
+
+
 def _axis(axis):
-    if len(axis) > ROPE_PAIRS or not all(0 <= a < 256 for a in axis):
-        raise ValueError(f"an axis for each of at most {ROPE_PAIRS} pairs, not {list(axis)}")
-    return (c_uint8 * ROPE_PAIRS)(*axis)
+    if len(axis) > ROPE_PAIRS:
+        raise ValueError(f"an axis for each of at most {ROPE_PAIRS} pairs, not {len(axis)}")
+    return _AxisArray.from_buffer_copy(bytes(axis).ljust(ROPE_PAIRS, b"\0"))
 
 
 class BlockDesc(ctypes.Structure):
@@ -130,7 +133,7 @@ class Fp8LinearDesc(ctypes.Structure):
 class QkRopeDesc(ctypes.Structure):
     _fields_ = [("tokens", c_int32), ("q_heads", c_int32), ("k_heads", c_int32), ("head_dim", c_int32),
                 ("norm", c_int32), ("near", c_int32), ("axes", c_int32), ("pos_rows", c_int32), ("eps", c_float),
-                ("dtype", c_int32), ("axis", c_uint8 * ROPE_PAIRS)]
+                ("dtype", c_int32), ("axis", _AxisArray)]
 
     @classmethod
     def of(cls, tokens, q_heads, k_heads, head_dim, dtype, axis, axes, pos_rows, norm=True, near=False, eps=1e-5):
@@ -139,7 +142,7 @@ class QkRopeDesc(ctypes.Structure):
 
 
 class BlockRope(ctypes.Structure):
-    _fields_ = [("axes", c_int32), ("pos_rows", c_int32), ("near", c_int32), ("axis", c_uint8 * ROPE_PAIRS),
+    _fields_ = [("axes", c_int32), ("pos_rows", c_int32), ("near", c_int32), ("axis", _AxisArray),
                 ("pos", c_void_p), ("freq", c_void_p)]
 
     @classmethod

@@ -40,30 +40,22 @@ ORBIT_DEV uint32_t fp8_mag(float x) {
 ORBIT_DEV uint32_t fp8_exp(uint32_t a) {
   return (uint32_t)min(246, max(10, (int)((a + 0x1fffffu) >> 23) - 8));
 }
-// codes of 8 values, f[i * STRIDE], with the scale 2^(E - 127)
-template <int STRIDE = 1>
+// codes of 8 values of any size with the scale 2^(E - 127)
 ORBIT_DEV uint2 fp8_encode8(const float* f, uint32_t e) {
   const float up = __uint_as_float((254u - e) << 23);
   uint32_t w[2];
-  float bad = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float t[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = f[(4 * h + i) * STRIDE];
-      bad = fmaf(x, 0.f, bad);  // NaN from the first infinity or NaN on
-      t[i] = __builtin_amdgcn_fmed3f(x * up, -448.f, 448.f);
-    }
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+    for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_fmed3f(f[4 * h + i] * up, -448.f, 448.f);
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
     w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], r, true);
   }
-  if (bad != bad) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((__float_as_uint(f[i * STRIDE]) & 0x7fffffffu) >= 0x7f800000u)
-        w[i >> 2] = (w[i >> 2] & ~(0xffu << (8 * (i & 3)))) | 0x7fu << (8 * (i & 3));
-  }
+  for (int i = 0; i < 8; ++i)
+    if ((__float_as_uint(f[i]) & 0x7fffffffu) >= 0x7f800000u)
+      w[i >> 2] = (w[i >> 2] & ~(0xffu << (8 * (i & 3)))) | 0x7fu << (8 * (i & 3));
   return make_uint2(w[0], w[1]);
 }
 // values of 8 codes
@@ -80,7 +72,8 @@ ORBIT_DEV void fp8_decode8(uint2 q, uint32_t e, float* f) {
 
 // x[rows, n] -> its store and / or its transposed one ([n, rows], blocks along the
 // rows; either may be null). tiled: 128 x 128 tiles share their E. part (may be
-// null): float32 column sums of x, one row of n per 128 rows.
+// null; not with tiles, and with store_t): float32 column sums of x, one row of n
+// per 128 rows.
 orbit_status fp8_pack(orbit_dtype dt, const void* x, int64_t ldx, int64_t rows, int64_t n, bool tiled, void* store,
                       void* store_t, float* part, hipStream_t s);
 orbit_status fp8_unpack(orbit_dtype dt, const void* store, int64_t rows, int64_t n, void* x, int64_t ldx,
