@@ -12,15 +12,18 @@
 // turned into bf16 with their scales in the fragments, which is exact, and the bf16
 // instructions keep every bit a float32 sum can, at half the rate.
 //
-// A row of a K slice is 64 bytes here as in the bf16 kernels, and an instruction
-// of 64 k takes as long as two of theirs of 16: tiles, LDS ring, copies and swizzle
-// are theirs (dma.h), with twice the operations per byte of LDS traffic. The E words
-// of 512 k (8 slices) come by the same copies into two LDS slots of their own and
-// are shifted by one block every two slices.
+// Results of more than 64 rows go through LDS, whose rings are filled by copies without
+// registers (dma.h). Three kernels share that work:
+//   wide   256 x 256 on 4 waves, one block per CU that walks over tiles: bf16 results of
+//          192 tiles of 256 x 256 on;
+//   exact  256 x 256 on two groups of 4 waves that take turns at decoding and multiplying:
+//          float32 results of as many tiles and K of 2048 on;
+//   tile   128 x 128 on 4 waves, K split where there are few tiles: the rest.
 //
 // Up to 64 rows of A (single tokens) the product is bound by reading B once:
 // fp8_thin_kernel streams it past 16x16x128 instructions without LDS.
 #include <algorithm>
+#include <type_traits>
 
 #include "dma.h"
 #include "fp8.h"
@@ -31,6 +34,7 @@ namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct Fp8Args {
   const uint8_t *A, *B, *Ae, *Be;  // codes and E bytes
@@ -39,7 +43,7 @@ struct Fp8Args {
   void* C;
   int64_t ldc;
   int M, N, slices;                // 64-deep slices of K
-  int splits, per_split;           // slices of a split (a multiple of 8)
+  int splits;                      // of K, each of whole blocks of 128
   float* partial;                  // splits > 1: [splits][M][N]
   Epi epi;
 };
@@ -50,6 +54,11 @@ ORBIT_DEV void dma4(__amdgpu_buffer_rsrc_t r, unsigned lds, unsigned voff) {
                : "memory", "m0");
 }
 
+// 2 and 8 floats as bf16, a conversion for two
+ORBIT_DEV uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(bf16)a, (bf16)b}); }
+ORBIT_DEV U128 pack8(const float* f) {
+  return U128{{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])}};
+}
 // 2^(E - 127) from the low byte of an E word
 ORBIT_DEV float fp8_scale(int e) { return __uint_as_float((unsigned)(e & 0xff) << 23); }
 // 8 codes as bf16 values with their scale (exact)
@@ -113,158 +122,46 @@ ORBIT_DEV void mma_slice(f32x16 (&c)[TM][TN], const i32x8* a, const i32x8* b, co
   }
 }
 
-template <typename CF> constexpr int fp8_ring() { return CF::NS * CF::STB; }
-template <typename CF> constexpr int fp8_lds() {
-  return std::max(fp8_ring<CF>() + 2 * (CF::BM + CF::BN) * 4, CF::EPB);
-}
-
-template <typename T, typename OutT, typename CF>
-__global__ void __launch_bounds__(CF::NT, CF::OCC) gemm_fp8_kernel(Fp8Args g) {
-  constexpr int BM = CF::BM, BN = CF::BN, WM = CF::WM, NS = CF::NS;
-  constexpr int TM = CF::TM, TN = CF::TN, OPA = CF::OPA, STB = CF::STB;
-  using PA = DmaPlan<true, BM, CF::NW>;
-  using PB = DmaPlan<true, BN, CF::NW>;
-  constexpr int NLS = PA::NL + PB::NL;  // copies of codes per stage per wave
-  constexpr int EW = BM + BN;           // E words of 8 slices
-  constexpr bool EXACT = sizeof(OutT) == 4;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave % WM, wn = wave / WM;
-  int split = blockIdx.z;
-
-  // tile order as in gemm_dma_kernel: XCD-contiguous ranges of tile ids, walked in
-  // groups of tile rows; with split K an XCD takes one K range
+// The lin-th of nt tiles, as in gemm_dma_kernel: XCD-contiguous ranges of tile ids,
+// walked in groups of tile rows.
+template <int BM, int BN>
+ORBIT_DEV void fp8_tile_of(const Fp8Args& g, int id, int& m0, int& n0) {
   const int tiles_n = (g.N + BN - 1) / BN, tiles_m = (g.M + BM - 1) / BM;
-  const int nt = tiles_m * tiles_n;
-  int id = blockIdx.x;
-  const int full = nt - nt % 8;
-  if (g.splits > 1 && 8 % g.splits == 0 && (nt * g.splits) % 8 == 0) {
-    const int lin = blockIdx.x + nt * (int)blockIdx.z, xcd = lin % 8;
-    split = xcd % g.splits;
-    id = (xcd / g.splits) * (nt * g.splits / 8) + lin / 8;
-  } else if (id < full) {
-    id = (id % 8) * (full / 8) + id / 8;
-  }
   constexpr int GR = BN == 128 ? 4 : 8;
   const int per_group = GR * tiles_n;
   const int first_m = (id / per_group) * GR;
   const int gsize = min(tiles_m - first_m, GR);
-  const int m0 = (first_m + (id % per_group) % gsize) * BM, n0 = ((id % per_group) / gsize) * BN;
-  const int sbeg = split * g.per_split;
-  const int nk = min(g.slices - sbeg, g.per_split);  // even: K is padded to whole blocks
-
-  const uint8_t* Ab = g.A + (int64_t)m0 * g.lda + (int64_t)sbeg * 64;
-  const uint8_t* Bb = g.B + (int64_t)n0 * g.ldb + (int64_t)sbeg * 64;
-  const uint8_t* Aeb = g.Ae + (int64_t)m0 * g.gpa + (sbeg >> 1);
-  const uint8_t* Beb = g.Be + (int64_t)n0 * g.gpb + (sbeg >> 1);
-
-  PA pa;
-  PB pb;
-  pa.init(g.lda >> 1, m0, g.M, wave, lane);
-  pb.init(g.ldb >> 1, n0, g.N, wave, lane);
-  Fp8Frag<TM> ra;
-  Fp8Frag<TN> rb;
-  ra.init(wm * TM * 32, lane);
-  rb.init(wn * TN * 32, lane);
-
-  f32x16 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-
-  const unsigned lds0 = (unsigned)(uintptr_t)(ORBIT_LDS void*)smem;
-  auto issue = [&](int st) {
-    if ((st & 7) == 0) {
-      // E words first: they have landed when the slice's codes have
-      for (int w = wave; w < EW / 64; w += CF::NW) {
-        const bool isa = w < BM / 64;
-        const int r = (isa ? w : w - BM / 64) * 64 + lane;
-        const unsigned vo = isa ? (m0 + r < g.M ? (unsigned)(r * g.gpa) : kOobOffset)
-                                : (n0 + r < g.N ? (unsigned)(r * g.gpb) : kOobOffset);
-        dma4(buffer_rsrc((isa ? Aeb : Beb) + (st >> 1)), lds0 + NS * STB + ((st >> 3) & 1) * (EW * 4) + w * 256, vo);
-      }
-    }
-    const unsigned b = lds0 + (st % NS) * STB;
-    pa.template issue<false>(reinterpret_cast<const bf16*>(Ab + st * 64), 0, DBK, b, wave, lane);
-    pb.template issue<false>(reinterpret_cast<const bf16*>(Bb + st * 64), 0, DBK, b + OPA, wave, lane);
-  };
-  int ea[TM], eb[TN];
-  auto scales = [&](int st) {
-    if ((st & 7) == 0) {
-      const int* E = reinterpret_cast<const int*>(smem + NS * STB + ((st >> 3) & 1) * (EW * 4));
-#pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] = E[wm * TM * 32 + i * 32 + (lane & 31)];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = E[BM + wn * TN * 32 + j * 32 + (lane & 31)];
-    } else if ((st & 1) == 0) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)ea[i] >> 8);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)eb[j] >> 8);
-    }
-  };
-  // prologue: stages 0 .. NS-2 in flight, then wait for stage 0
-#pragma unroll
-  for (int st = 0; st < NS - 1; ++st)
-    if (st < nk) issue(st);
-  wait_stage<NLS, NS>(min(nk - 1, NS - 2));
-  __syncthreads();
-
-  i32x8 fa[TM], fb[TN];
-  if constexpr (CF::PP) {
-    // two wave groups half a slice apart (see gemm_dma_kernel)
-    const int grp = wave >> 2;
-    if (grp) __builtin_amdgcn_s_barrier();
-    for (int kt = 0; kt < nk; ++kt) {
-      const char* cur = smem + (kt % NS) * STB;
-      ra.read(fa, cur);
-      rb.read(fb, cur + OPA);
-      scales(kt);
-      if (kt + NS - 1 < nk) issue(kt + NS - 1);
-      wait_stage<NLS, NS>(min(nk - kt - 2, NS - 2));
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_setprio(1);
-      mma_slice<TM, TN, EXACT>(acc, fa, fb, ea, eb);
-      __builtin_amdgcn_s_setprio(0);
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if (!grp) __builtin_amdgcn_s_barrier();
+  m0 = (first_m + (id % per_group) % gsize) * BM;
+  n0 = ((id % per_group) / gsize) * BN;
+}
+template <int BM, int BN>
+ORBIT_DEV void fp8_tile(const Fp8Args& g, int lin, int nt, int& m0, int& n0) {
+  const int full = nt - nt % 8;
+  fp8_tile_of<BM, BN>(g, lin < full ? (lin % 8) * (full / 8) + lin / 8 : lin, m0, n0);
+}
+// The first block of 128 k of split s: the splits differ by one at most.
+ORBIT_DEV int fp8_split_at(const Fp8Args& g, int s) { return (int)((int64_t)(g.slices >> 1) * s / g.splits); }
+// A block's tile and K range: with split K an XCD takes one range.
+template <int BM, int BN>
+ORBIT_DEV void fp8_tile(const Fp8Args& g, int& m0, int& n0, int& split) {
+  split = blockIdx.z;
+  const int nt = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+  if (g.splits > 1 && 8 % g.splits == 0 && (nt * g.splits) % 8 == 0) {
+    const int lin = blockIdx.x + nt * (int)blockIdx.z, xcd = lin % 8;
+    split = xcd % g.splits;
+    fp8_tile_of<BM, BN>(g, (xcd / g.splits) * (nt * g.splits / 8) + lin / 8, m0, n0);
   } else {
-    // a slice's MFMAs run while the next slice's fragments are read
-    i32x8 ga[TM], gb[TN];
-    auto step = [&](int kt, const i32x8* ua, const i32x8* ub, i32x8* va, i32x8* vb) {
-      if (kt + NS - 1 < nk) issue(kt + NS - 1);
-      scales(kt);
-      wait_stage<NLS, NS>(min(nk - kt - 2, NS - 2));
-      __syncthreads();
-      // past the last slice this reads a stale but in-bounds slot
-      const char* nxt = smem + ((kt + 1) % NS) * STB;
-      ra.read(va, nxt);
-      rb.read(vb, nxt + OPA);
-      mma_slice<TM, TN, EXACT>(acc, ua, ub, ea, eb);
-    };
-    ra.read(fa, smem);
-    rb.read(fb, smem + OPA);
-    for (int kt = 0; kt < nk; kt += 2) {
-      step(kt, fa, fb, ga, gb);
-      step(kt + 1, ga, gb, fa, fb);
-    }
+    fp8_tile<BM, BN>(g, blockIdx.x, nt, m0, n0);
   }
-  wait_vmcnt<0>();
-  __syncthreads();
+}
 
-  // epilogue through LDS: each wave parks 32 rows of its accumulators and reads
-  // them back as 8 consecutive columns per lane
-  constexpr int WTN = TN * 32, EP = WTN + 8, LPR = WTN / 8, RPI = 64 / LPR;
+// Through LDS: each wave parks 32 rows of its accumulators and reads them back as 8
+// consecutive columns per lane.
+template <typename T, typename OutT, typename CF>
+ORBIT_DEV void fp8_epilogue(const Fp8Args& g, f32x16 (&acc)[CF::TM][CF::TN], char* smem, int wave, int lane, int m0,
+                            int n0, int split) {
+  constexpr int TM = CF::TM, TN = CF::TN, WTN = TN * 32, EP = WTN + 8, LPR = WTN / 8, RPI = 64 / LPR;
+  const int wm = wave % CF::WM, wn = wave / CF::WM;
   float* ew = reinterpret_cast<float*>(smem) + wave * 32 * EP;
   OutT* C = static_cast<OutT*>(g.C);
   const bool raw = g.splits > 1;
@@ -299,6 +196,598 @@ __global__ void __launch_bounds__(CF::NT, CF::OCC) gemm_fp8_kernel(Fp8Args g) {
   }
 }
 
+// Float32 results of long K and many tiles. Decoding the fragments takes about as many
+// cycles as their products, so the block's two groups of waves, one wave of each per SIMD,
+// work half a slice apart: one decodes and multiplies while the other reads and copies
+// (measured against one group of 4 waves, tile kernel below: 4096 x 4096 x 8192 206 us
+// against 239, 4096 x 8192 x 2048 136 against 139, but 8192 x 8192 x 1024 182 against 166).
+using ExactCfg = DmaPP;
+constexpr int kExactE = ExactCfg::NS * ExactCfg::STB;
+constexpr int kExactLds = std::max(kExactE + 2 * (ExactCfg::BM + ExactCfg::BN) * 4, ExactCfg::EPB);
+template <typename T>
+__global__ void __launch_bounds__(ExactCfg::NT, ExactCfg::OCC) gemm_fp8_exact_kernel(Fp8Args g) {
+  using CF = ExactCfg;
+  constexpr int BM = CF::BM, BN = CF::BN, WM = CF::WM, NS = CF::NS;
+  constexpr int TM = CF::TM, TN = CF::TN, OPA = CF::OPA, STB = CF::STB;
+  using PA = DmaPlan<true, BM, CF::NW>;
+  using PB = DmaPlan<true, BN, CF::NW>;
+  constexpr int NLS = PA::NL + PB::NL;  // copies of codes per stage per wave
+  constexpr int EW = BM + BN;           // E words of 8 slices
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+  int m0, n0;
+  fp8_tile<BM, BN>(g, blockIdx.x, gridDim.x, m0, n0);
+  const int nk = g.slices;
+
+  const uint8_t* Ab = g.A + (int64_t)m0 * g.lda;
+  const uint8_t* Bb = g.B + (int64_t)n0 * g.ldb;
+  const uint8_t* Aeb = g.Ae + (int64_t)m0 * g.gpa;
+  const uint8_t* Beb = g.Be + (int64_t)n0 * g.gpb;
+
+  PA pa;
+  PB pb;
+  pa.init(g.lda >> 1, m0, g.M, wave, lane);
+  pb.init(g.ldb >> 1, n0, g.N, wave, lane);
+  Fp8Frag<TM> ra;
+  Fp8Frag<TN> rb;
+  ra.init(wm * TM * 32, lane);
+  rb.init(wn * TN * 32, lane);
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  const unsigned lds0 = (unsigned)(uintptr_t)(ORBIT_LDS void*)smem;
+  auto issue = [&](int st) {
+    if ((st & 7) == 0) {
+      // E words first: they have landed when the slice's codes have
+      for (int w = wave; w < EW / 64; w += CF::NW) {
+        const bool isa = w < BM / 64;
+        const int r = (isa ? w : w - BM / 64) * 64 + lane;
+        const unsigned vo = isa ? (m0 + r < g.M ? (unsigned)(r * g.gpa) : kOobOffset)
+                                : (n0 + r < g.N ? (unsigned)(r * g.gpb) : kOobOffset);
+        dma4(buffer_rsrc((isa ? Aeb : Beb) + (st >> 1)), lds0 + kExactE + ((st >> 3) & 1) * (EW * 4) + w * 256, vo);
+      }
+    }
+    const unsigned b = lds0 + (st % NS) * STB;
+    pa.template issue<false>(reinterpret_cast<const bf16*>(Ab + st * 64), 0, DBK, b, wave, lane);
+    pb.template issue<false>(reinterpret_cast<const bf16*>(Bb + st * 64), 0, DBK, b + OPA, wave, lane);
+  };
+  int ea[TM], eb[TN];
+  auto scales = [&](int st) {
+    if ((st & 7) == 0) {
+      const int* E = reinterpret_cast<const int*>(smem + kExactE + ((st >> 3) & 1) * (EW * 4));
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ea[i] = E[wm * TM * 32 + i * 32 + (lane & 31)];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) eb[j] = E[BM + wn * TN * 32 + j * 32 + (lane & 31)];
+    } else if ((st & 1) == 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)ea[i] >> 8);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)eb[j] >> 8);
+    }
+  };
+  // prologue: stages 0 .. NS-2 in flight, then wait for stage 0
+#pragma unroll
+  for (int st = 0; st < NS - 1; ++st)
+    if (st < nk) issue(st);
+  wait_stage<NLS, NS>(min(nk - 1, NS - 2));
+  __syncthreads();
+
+  i32x8 fa[TM], fb[TN];
+  const int grp = wave >> 2;
+  if (grp) __builtin_amdgcn_s_barrier();
+  for (int kt = 0; kt < nk; ++kt) {
+    const char* cur = smem + (kt % NS) * STB;
+    ra.read(fa, cur);
+    rb.read(fb, cur + OPA);
+    scales(kt);
+    if (kt + NS - 1 < nk) issue(kt + NS - 1);
+    wait_stage<NLS, NS>(min(nk - kt - 2, NS - 2));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+    mma_slice<TM, TN, true>(acc, fa, fb, ea, eb);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (!grp) __builtin_amdgcn_s_barrier();
+  wait_vmcnt<0>();
+  __syncthreads();
+
+  fp8_epilogue<T, float, CF>(g, acc, smem, wave, lane, m0, n0, 0);
+}
+
+// Tiles of 128 x 128 on 4 waves of 64 x 64. A stage is a block of 128 k: rows of 128 bytes,
+// whole cache lines, as in the wide kernel below; its halves of 64 k pass through two sets
+// of registers, so that products cover the reads, and one barrier serves 128 k (stages of
+// 64 k and rows of 64 bytes: 8192 x 1024 x 4096 46 us against 39, 2048 x 4096 x 2048 25.7
+// against 22.8). Two stages leave room for two blocks per CU; up to 256 blocks there is one
+// per CU anyway and bf16 results take four (1024 x 4096 x 4096 24.8 us against 28.0, and with
+// 512 tiles 48.9 against 39.2); float32 results, which are bound by decoding, do not gain
+// (1024 x 1024 x 1024 13.1 us against 12.5).
+template <int NS>
+struct TileCfg {
+  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, TM = 2, TN = 2;
+  static constexpr int OPA = BM * 128, STB = OPA + BN * 128, E = NS * STB, LDS = E + 2 * (BM + BN) * 4;
+  static_assert(LDS >= 4 * 32 * (TN * 32 + 8) * 4, "the epilogue's rows");
+};
+template <typename T, typename OutT, int NS>
+__global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8Args g) {
+  using CF = TileCfg<NS>;
+  constexpr int BM = CF::BM, BN = CF::BN, TM = CF::TM, TN = CF::TN;
+  constexpr bool EXACT = sizeof(OutT) == 4;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % CF::WM, wn = wave / CF::WM;
+  int m0, n0, split;
+  fp8_tile<BM, BN>(g, m0, n0, split);
+  m0 = __builtin_amdgcn_readfirstlane(m0);
+  n0 = __builtin_amdgcn_readfirstlane(n0);
+  split = __builtin_amdgcn_readfirstlane(split);
+  const int b0 = fp8_split_at(g, split), nk = fp8_split_at(g, split + 1) - b0;  // stages
+  const int rm = min(g.M - m0, BM), rn = min(g.N - n0, BN);
+  const uint8_t* Ab = g.A + (int64_t)m0 * g.lda + (int64_t)b0 * 128;
+  const uint8_t* Bb = g.B + (int64_t)n0 * g.ldb + (int64_t)b0 * 128;
+  const uint8_t* Aeb = g.Ae + (int64_t)m0 * g.gpa;
+  const uint8_t* Beb = g.Be + (int64_t)n0 * g.gpb;
+
+  // copy c of a wave: rows 8 (4 wave + c) + lane / 8 of the operand; rows behind its last
+  // one read zeros
+  unsigned va[4], vb[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int r = (wave * 4 + c) * 8 + (lane >> 3), k = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    va[c] = r < rm ? (unsigned)(r * (int)g.lda + k) : kOobOffset;
+    vb[c] = r < rn ? (unsigned)(r * (int)g.ldb + k) : kOobOffset;
+  }
+  // E words: wave w copies those of 64 rows, of A (w < 2) or of B
+  const int er = (wave & 1) * 64 + lane;
+  const unsigned ve = wave < 2 ? (er < rm ? (unsigned)(er * g.gpa) : kOobOffset) : (er < rn ? (unsigned)(er * g.gpb) : kOobOffset);
+  const unsigned lds0 = (unsigned)(uintptr_t)(ORBIT_LDS void*)smem;
+  auto issue = [&](int st) {
+    const int b = b0 + st;
+    if ((b & 3) == 0 || st == 0)  // before the stage's codes: landed when these have
+      dma4(buffer_rsrc((wave < 2 ? Aeb : Beb) + (b >> 2) * 4), lds0 + CF::E + ((b >> 2) & 1) * ((BM + BN) * 4) + wave * 256, ve);
+    const unsigned at = lds0 + (st % NS) * CF::STB + wave * 4096;
+    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(Ab + (int64_t)st * 128), rb = buffer_rsrc(Bb + (int64_t)st * 128);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) dma16(ra, at + c * 1024, va[c]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) dma16(rb, at + CF::OPA + c * 1024, vb[c]);
+  };
+  int ea[TM], eb[TN];
+  auto scales = [&](int st) {
+    const int b = b0 + st;
+    if ((b & 3) == 0 || st == 0) {
+      const int* E = reinterpret_cast<const int*>(smem + CF::E + ((b >> 2) & 1) * ((BM + BN) * 4));
+      const int by = (b & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)E[wm * 64 + i * 32 + (lane & 31)] >> by);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)E[BM + wn * 64 + j * 32 + (lane & 31)] >> by);
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)ea[i] >> 8);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)eb[j] >> 8);
+    }
+  };
+  const int lr = lane & 31;
+  const unsigned oa = (unsigned)((wm * 64 + lr) * 128), ob = (unsigned)(CF::OPA + (wn * 64 + lr) * 128);
+  unsigned x[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[q] = (unsigned)(((2 * q + (lane >> 5)) ^ ((lr >> 1) & 7)) << 4);
+  // half hf (64 k) of a stage's fragments
+  auto read = [&](i32x8* fa, i32x8* fb, const char* S, int hf) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      fa[i] = __builtin_shufflevector(*reinterpret_cast<const i32x4*>(S + oa + i * 4096 + x[2 * hf]),
+                                      *reinterpret_cast<const i32x4*>(S + oa + i * 4096 + x[2 * hf + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+      fb[j] = __builtin_shufflevector(*reinterpret_cast<const i32x4*>(S + ob + j * 4096 + x[2 * hf]),
+                                      *reinterpret_cast<const i32x4*>(S + ob + j * 4096 + x[2 * hf + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+#pragma unroll
+  for (int st = 0; st < NS; ++st)
+    if (st < nk) issue(st);
+  wait_stage<8, NS + 1>(min(nk - 1, NS - 1));
+  __syncthreads();
+  i32x8 fa[TM], fb[TN], ga[TM], gb[TN];
+  read(fa, fb, smem, 0);
+  for (int kt = 0; kt < nk; ++kt) {
+    const char* here = smem + (kt % NS) * CF::STB;
+    scales(kt);
+    read(ga, gb, here, 1);
+    mma_slice<TM, TN, EXACT>(acc, fa, fb, ea, eb);
+    // the stage is in registers everywhere and the next one has landed
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wait_stage<8, NS + 1>(max(min(nk - kt - 2, NS - 2), 0));
+    __syncthreads();
+    // past the last stage this reads a stale but in-bounds slot
+    read(fa, fb, smem + ((kt + 1) % NS) * CF::STB, 0);
+    if (kt + NS < nk) issue(kt + NS);
+    mma_slice<TM, TN, EXACT>(acc, ga, gb, ea, eb);
+  }
+  wait_vmcnt<0>();
+  __syncthreads();
+  fp8_epilogue<T, OutT, CF>(g, acc, smem, wave, lane, m0, n0, split);
+}
+
+// bf16 results of many tiles: 256 x 256 on 4 waves of 128 x 128, one per SIMD. A
+// fragment is then read for four products instead of two or four (half of the LDS
+// time that the MFMAs take), and a wave's own order of instructions overlaps
+// everything: after an MFMA, which takes 64 cycles, come reads of the next
+// fragments or a copy of the stage after the next.
+//
+// A stage is a block of 128 k: rows of 128 bytes, a whole cache line, since copies of
+// 64-byte pieces of rows take the L2 twice the requests (measured beside the MFMAs: 77
+// to 109 cycles an MFMA by the rows' distance, against 65.5). LDS holds two stages;
+// chunk c of row r lies at c ^ ((r >> 1) & 7), so that fragment reads of 16
+// consecutive rows meet every bank once. A stage's two halves of 64 k pass through
+// two sets of registers:
+//   half 0: products of X, reads of half 1 into Y; when these are done everywhere the
+//           stage's slot is free and the copies of the stage after the next begin;
+//   half 1: products of Y, reads of the next stage's half 0 into X, more copies.
+// Blocks stay, one per CU, and walk over tiles: the stage after a tile's last is the
+// next tile's first, which is in LDS when a tile's results go out through LDS of their
+// own. All 256 accumulation registers hold sums, so the epilogue's 256 vector registers
+// have to do without a spill: one would wait for every copy and store in flight (22
+// spilled registers: 4 to 14 us a round of tiles).
+//
+// Measured: 8192 x 8192 x 8192 415 us (2650 TFLOP/s; two groups of 4 waves that take turns,
+// as in the exact kernel, 456), 4096 x 4096 x 8192 114 (121), 4096 x 8192 x 4096 109 (123),
+// 8192 x 8192 x 1024 75 (92). A stage takes 1.49 us, 2880 TFLOP/s, near what the matrix
+// cores reach on random codes at the card's power limit (3200); a round of tiles costs 9 to
+// 18 us beside its stages, of which 7 are 32 MB of results at the memory's rate: there is
+// no room in LDS or registers to let the next tile's sums begin before these are out.
+constexpr int kWideStage = 2 * 256 * 128;
+constexpr int kWideE = 2 * kWideStage, kWideBias = kWideE + 2 * 512 * 4, kWideOut = kWideBias + 2 * 1024;
+constexpr int kWidePitch = 272, kWideLds = kWideOut + 4 * 16 * kWidePitch;  // 16 rows of 128 bf16 per wave
+static_assert(kWideLds <= 160 * 1024, "LDS");
+
+// what happens to a sum (with its bias) before it is stored
+enum WideEpi { kWidePlain, kWideGelu, kWideGeluGrad, kWideRes };
+
+template <WideEpi EPI>
+__global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
+  constexpr int OPA = 256 * 128;  // bytes of A in a stage
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
+  const int nk = g.slices >> 1;  // stages of a tile, at least 2
+  const int nt = ((g.M + 255) >> 8) * ((g.N + 255) >> 8);
+
+  struct Tile {
+    const uint8_t *A, *B, *Ae, *Be;
+    int m0, n0, rm, rn;  // rows of A and of B, 0 past the last tile
+  };
+  auto tile_at = [&](int lin) {
+    Tile t;
+    fp8_tile<256, 256>(g, min(lin, nt - 1), nt, t.m0, t.n0);
+    // (a division: left in vector registers otherwise)
+    t.m0 = __builtin_amdgcn_readfirstlane(t.m0);
+    t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
+    t.A = g.A + (int64_t)t.m0 * g.lda;
+    t.B = g.B + (int64_t)t.n0 * g.ldb;
+    t.Ae = g.Ae + (int64_t)t.m0 * g.gpa;
+    t.Be = g.Be + (int64_t)t.n0 * g.gpb;
+    t.rm = lin < nt ? min(g.M - t.m0, 256) : 0;
+    t.rn = lin < nt ? min(g.N - t.n0, 256) : 0;
+    return t;
+  };
+  // copy c of a wave: rows 8 (8 wave + c) + lane / 8 of the operand, 16 (c / 2) rows behind
+  // those of copy c & 1; the descriptor ends behind the tile's last row
+  unsigned va[2], vb[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int r = (wave * 8 + c) * 8 + (lane >> 3), k = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    va[c] = (unsigned)(r * (int)g.lda + k);
+    vb[c] = (unsigned)(r * (int)g.ldb + k);
+  }
+  // E words: wave w copies those of 64 rows of A and of B; bias: 64 words each of waves 0, 1
+  const unsigned vea = (unsigned)((wave * 64 + lane) * g.gpa), veb = (unsigned)((wave * 64 + lane) * g.gpb);
+  const unsigned vbias = wave < 2 ? (unsigned)((wave * 64 + lane) * 4) : kOobOffset;
+
+  const unsigned lds0 = (unsigned)(uintptr_t)(ORBIT_LDS void*)smem;
+  Tile cur = tile_at(blockIdx.x), nxt = tile_at(blockIdx.x + gridDim.x);
+  int par = 0, epar = 0, bpar = 0;  // slots of the tile's first stage, first E words, bias
+
+  // what stage st of the tile copies, st >= nk being the next tile's
+  struct Src {
+    __amdgpu_buffer_rsrc_t a, b;
+    unsigned lds;
+  };
+  auto source = [&](int st) {
+    const bool here = st < nk;
+    const int s = here ? st : st - nk;
+    const int rm = here ? cur.rm : nxt.rm, rn = here ? cur.rn : nxt.rn;
+    Src x;
+    x.a = buffer_rsrc((here ? cur.A : nxt.A) + s * 128, max(rm * (int)g.lda - s * 128, 0));
+    x.b = buffer_rsrc((here ? cur.B : nxt.B) + s * 128, max(rn * (int)g.ldb - s * 128, 0));
+    x.lds = lds0 + ((par + st) & 1) * kWideStage + wave * 8192;
+    return x;
+  };
+  auto copy = [&](const Src& x, int c) {
+    const int d = c & 7;
+    if (c < 8) dma16(x.a, x.lds + c * 1024, va[d & 1] + (unsigned)((d >> 1) * 16 * (int)g.lda));
+    else dma16(x.b, x.lds + OPA + d * 1024, vb[d & 1] + (unsigned)((d >> 1) * 16 * (int)g.ldb));
+  };
+  // the E words of stage st's 512 k, copied again with every stage of these (the same
+  // words: no branch in a stage), the first time with the first one's codes
+  auto copy_e = [&](int st) {
+    const bool here = st < nk;
+    const int s = (here ? st : st - nk) & ~3;
+    const int slot = here ? epar ^ ((st >> 2) & 1) : epar ^ (((nk + 3) >> 2) & 1);
+    const int rm = here ? cur.rm : nxt.rm, rn = here ? cur.rn : nxt.rn;
+    const unsigned b = lds0 + kWideE + slot * 2048 + wave * 256;
+    dma4(buffer_rsrc((here ? cur.Ae : nxt.Ae) + s, max(rm * g.gpa - s, 0)), b, vea);
+    dma4(buffer_rsrc((here ? cur.Be : nxt.Be) + s, max(rn * g.gpb - s, 0)), b + 1024, veb);
+  };
+  auto copy_bias = [&](const Tile& t, int slot) {
+    const int bytes = g.epi.bias ? t.rn * 2 : 0;
+    dma4(buffer_rsrc(g.epi.bias ? static_cast<const char*>(g.epi.bias) + t.n0 * 2 : reinterpret_cast<const char*>(g.A), bytes),
+         lds0 + kWideBias + slot * 1024 + wave * 256, vbias);
+  };
+
+  struct Set {
+    i32x8 f[8];  // fragments: 4 of A, 4 of B
+  };
+  const int lr = lane & 31;
+  const unsigned oa = (unsigned)((wm * 128 + lr) * 128), ob = (unsigned)(OPA + (wn * 128 + lr) * 128);
+  unsigned x[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[q] = (unsigned)(((2 * q + (lane >> 5)) ^ ((lr >> 1) & 7)) << 4);
+  // chunk q of fragment f of half hf
+  auto read = [&](Set& s, const char* S, int hf, int f, int q) {
+    const i32x4 v = *reinterpret_cast<const i32x4*>(S + (f < 4 ? oa : ob) + (f & 3) * 4096 + x[2 * hf + q]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s.f[f][4 * q + w] = v[w];
+  };
+  // E words of the fragments' rows: the stage's byte lies lowest, the next stage's above it
+  int ea[4], eb[4];
+  auto scales = [&](int slot) {
+    const char* E = smem + kWideE + slot * 2048;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ea[i] = *reinterpret_cast<const int*>(E + (wm * 128 + i * 32 + lr) * 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) eb[j] = *reinterpret_cast<const int*>(E + 1024 + (wn * 128 + j * 32 + lr) * 4);
+  };
+  // the waves meet: what each waited for holds for all
+  auto meet = [&] {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  copy_bias(cur, 0);
+  copy_e(0);
+  {
+    const Src s = source(0);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) copy(s, c);
+  }
+  copy_e(1);
+  {
+    const Src s = source(1);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) copy(s, c);
+  }
+  wait_vmcnt<18>();
+  __syncthreads();
+  for (int lin = blockIdx.x; lin < nt; lin += gridDim.x) {
+    // the first half stage (read again here, so that its registers are free between
+    // two tiles)
+    Set X, Y;
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      read(X, smem + par * kWideStage, 0, f, 0);
+      read(X, smem + par * kWideStage, 0, f, 1);
+    }
+    // the sums begin with the bias: lane l holds columns 8 q + 4 (l >> 5) .. +3
+    f32x16 acc[4][4];
+    {
+      const char* bias = smem + kWideBias + bpar * 1024 + (wn * 128 + (lane >> 5) * 4) * 2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint2 b = *reinterpret_cast<const uint2*>(bias + (j * 32 + q * 8) * 2);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[i][j][4 * q] = __uint_as_float(b.x << 16);
+            acc[i][j][4 * q + 1] = __uint_as_float(b.x & 0xffff0000u);
+            acc[i][j][4 * q + 2] = __uint_as_float(b.y << 16);
+            acc[i][j][4 * q + 3] = __uint_as_float(b.y & 0xffff0000u);
+          }
+        }
+    }
+    copy_bias(nxt, bpar ^ 1);
+    auto product = [&](const Set& s, int m) {
+      const int i = m / 4, j = m % 4;
+      // B's rows first: a lane then holds four consecutive columns of a row of C
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(s.f[4 + j], s.f[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+    };
+    int t = 0;
+#pragma unroll 1
+    do {
+      const char* here = smem + ((par + t) & 1) * kWideStage;
+      const char* then = smem + ((par + t + 1) & 1) * kWideStage;
+      if ((t & 3) == 0) {
+        scales(epar ^ ((t >> 2) & 1));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ea[i] = (int)((unsigned)ea[i] >> 8);
+          eb[i] = (int)((unsigned)eb[i] >> 8);
+        }
+      }
+      const Src s = source(t + 2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 16; ++m) {
+        if (m == 10) {
+          // the whole stage is in registers
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          meet();
+        }
+        product(X, m);
+        if (m < 8) {
+          read(Y, here, 1, m, 0);
+          read(Y, here, 1, m, 1);
+        }
+        if (m >= 10 && m != 12 && m != 15) copy(s, m < 12 ? m - 10 : m - 11);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // the next stage has landed (four copies of the one after it may be in flight)
+      wait_vmcnt<4>();
+      meet();
+      copy_e(t + 2);
+#pragma unroll
+      for (int m = 0; m < 16; ++m) {
+        product(Y, m);
+        if (m < 8) {
+          read(X, then, 0, m, 0);
+          read(X, then, 0, m, 1);
+        }
+        if ((m & 3) != 3) copy(s, 4 + m - (m >> 2));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } while (++t < nk);
+    // Results, 32 rows x 128 columns at a time: lane l holds row l & 31 of a product's
+    // tile and of its columns 8 q + 4 (l >> 5) .. +3, q = 0 .. 3. Halves of the wave swap
+    // such fours, so that a lane has 8 consecutive columns; rounded to bf16 they pass
+    // through the wave's LDS, 16 rows at a time, and leave as runs of 256 bytes (runs of
+    // 128 take the memory half as long again).
+    char* out = smem + kWideOut + wave * 16 * kWidePitch;
+    const int mw = cur.m0 + wm * 128, nc = cur.n0 + wn * 128;
+    // rows mw + 32 i .. of a matrix from column nc: offsets behind the last row are out of
+    // bounds, which reads zeros and stores nothing
+    auto matrix = [&](const void* D, int64_t ld, int i) {
+      const int mr = mw + i * 32;
+      const uint64_t p = (uint64_t)(uintptr_t)(static_cast<const bf16*>(D) + (int64_t)mr * ld + nc);
+      // (uniform, as the compiler does not see)
+      const unsigned lo = __builtin_amdgcn_readfirstlane((int)p), hi = __builtin_amdgcn_readfirstlane((int)(p >> 32));
+      return buffer_rsrc(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo),
+                         __builtin_amdgcn_readfirstlane(max(min(g.M - mr, 32), 0) * (int)ld * 2));
+    };
+    auto leave = [&](void* D, int64_t ld, int i, const U128* q) {
+      const __amdgpu_buffer_rsrc_t to = matrix(D, ld, i);
+      const unsigned at = nc + (lane & 15) * 8 < g.N ? (unsigned)((lane >> 4) * (int)ld * 2 + (lane & 15) * 16) : kOobOffset;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if ((lr >> 4) == h) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) st128(out + (lr & 15) * kWidePitch + (k * 16 + (lane >> 5) * 8) * 2, q[k]);
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(out + (it * 4 + (lane >> 4)) * kWidePitch + (lane & 15) * 16);
+          __builtin_amdgcn_raw_buffer_store_b128(v, to, at + (unsigned)((h * 16 + it * 4) * 2 * (int)ld), 0, 0);
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    };
+    // the rows of the epilogue's operands, read before the rows before them leave: their
+    // wait is none for those stores
+    u32x4 ops[8];
+    auto fetch = [&](auto at) {
+      constexpr int i = decltype(at)::value;
+      if constexpr (EPI == kWideGeluGrad || EPI == kWideRes) {
+        const int64_t ld = EPI == kWideRes ? g.epi.ldr : g.epi.ldgi;
+        const __amdgpu_buffer_rsrc_t r = matrix(EPI == kWideRes ? g.epi.res : g.epi.gelu_in, ld, i);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int c = k * 16 + (lane >> 5) * 8;
+          ops[k] = __builtin_amdgcn_raw_buffer_load_b128(r, nc + c < g.N ? (unsigned)(lr * (int)ld * 2 + c * 2) : kOobOffset, 0, 0);
+        }
+      }
+    };
+    auto rows = [&](auto at) {
+      constexpr int i = decltype(at)::value;
+      // (from here on, not before: moved up, these rows' sums would not fit the registers)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) asm volatile("" : "+a"(acc[i][j]));
+      U128 q[8];
+      // the sums as they are, rounded before the halves swap: half the swaps
+      auto sums = [&] {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const f32x16& c = acc[i][k >> 1];
+          const int p = 8 * (k & 1);
+          const auto w0 = __builtin_amdgcn_permlane32_swap(pack2(c[p], c[p + 1]), pack2(c[p + 4], c[p + 5]), false, false);
+          const auto w1 = __builtin_amdgcn_permlane32_swap(pack2(c[p + 2], c[p + 3]), pack2(c[p + 6], c[p + 7]), false, false);
+          q[k] = U128{{w0[0], w1[0], w0[1], w1[1]}};
+        }
+      };
+      if constexpr (EPI == kWidePlain) {
+        sums();
+      } else {
+        if constexpr (EPI == kWideGelu) {
+          sums();
+          leave(g.epi.gelu_out, g.epi.ldgo, i, q);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          __builtin_amdgcn_sched_barrier(0);
+          float v[8], t8[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int p = 8 * (k & 1) + e;
+            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][k >> 1][p]),
+                                                            __float_as_uint(acc[i][k >> 1][p + 4]), false, false);
+            v[e] = __uint_as_float(w[0]);
+            v[4 + e] = __uint_as_float(w[1]);
+          }
+          if constexpr (EPI != kWideGelu) unpack(__builtin_bit_cast(U128, ops[k]), t8, (bf16*)nullptr);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = EPI == kWideGelu ? gelu_f(v[e]) : EPI == kWideRes ? v[e] + t8[e] : v[e] * gelu_grad_f(t8[e]);
+          q[k] = pack8(v);
+        }
+        if constexpr (i < 3) fetch(std::integral_constant<int, i + 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      leave(g.C, g.ldc, i, q);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    fetch(std::integral_constant<int, 0>{});
+    rows(std::integral_constant<int, 0>{});
+    rows(std::integral_constant<int, 1>{});
+    rows(std::integral_constant<int, 2>{});
+    rows(std::integral_constant<int, 3>{});
+    // the next tile
+    par ^= nk & 1;
+    epar ^= ((nk + 3) >> 2) & 1;
+    bpar ^= 1;
+    cur = nxt;
+    nxt = tile_at(lin + 2 * gridDim.x);
+  }
+  wait_vmcnt<0>();
+}
+
 // Up to 16 MT rows of A. A block of 8 waves takes 16 columns (rows of B); its waves
 // take the K blocks in turn, 128 k to an instruction, and add their sums through
 // LDS. Lane l holds row l & 15 and k 32 (l >> 4) .. +31 of either operand, and of
@@ -310,7 +799,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) fp8_thin_kernel(Fp8Args g) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n0 = blockIdx.x * 16, lr = lane & 15, kc = (lane >> 4) * 32;
   const int split = blockIdx.z;
-  const int b0 = split * (g.per_split >> 1), b1 = min(g.slices >> 1, b0 + (g.per_split >> 1));  // K blocks
+  const int b0 = fp8_split_at(g, split), b1 = fp8_split_at(g, split + 1);  // K blocks
   // rows past the operands read row 0 again: their results are not stored
   const bool bv = n0 + lr < g.N;
   const int64_t br = bv ? n0 + lr : 0;
@@ -399,10 +888,10 @@ __global__ void __launch_bounds__(kThinWaves * 64) fp8_thin_kernel(Fp8Args g) {
   }
 }
 
-enum Fp8Tile { kThin, kQuarter, kHalf, kFull };
+enum Fp8Tile { kThin, kTile, kFull };
 struct Fp8Choice { Fp8Tile tile; int splits; };
 
-Fp8Choice pick_fp8(int M, int N, int K) {
+Fp8Choice pick_fp8(int M, int N, int K, bool out_f32) {
   const int64_t slices = fp8_wide(K) / 64;
   if (M <= 64) {
     // a block per CU at least
@@ -411,32 +900,65 @@ Fp8Choice pick_fp8(int M, int N, int K) {
     return {kThin, sp};
   }
   const int64_t t256 = cdiv(M, 256) * cdiv(N, 256), t128 = cdiv(M, 128) * cdiv(N, 128);
-  if (t256 >= 192) return {kFull, 1};
-  int sp = 1;
-  while (sp < 8 && t128 * sp < 256 && slices / (2 * sp) >= 16) sp *= 2;
-  return {kQuarter, sp};
+  // (wide: two stages at least; exact: see there)
+  if (t256 >= 192 && slices >= (out_f32 ? 32 : 4)) return {kFull, 1};
+  // Split K costs the second launch and writing and reading a partial sum per split, about
+  // 0.75 us for each MB of these (1024 x 1024 x 1024 in 1, 2, 4 parts: 9.6, 14.0, 19.0 us),
+  // and saves slices of 0.27 us (float32 results: 0.42); in units of slices:
+  const double fix = out_f32 ? 4 : 6, per = out_f32 ? 0.12 : 0.18;
+  Fp8Choice c{kTile, 1};
+  double best = (double)slices;
+  for (int sp = 2; sp <= 8 && t128 * sp <= 256 && 2 * sp <= slices; sp *= 2) {
+    const double t = (double)slices / sp + fix + per * (double)(sp * t128);
+    if (t < best) { best = t; c.splits = sp; }
+  }
+  return c;
 }
 
-// slices of a split, whole E words
-int per_split_of(int64_t slices, int splits) { return (int)cdiv(cdiv(slices, splits), 8) * 8; }
-
-template <typename T, typename OutT, typename CF>
-orbit_status run_fp8(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
-  const char* name = CF::BM == 128 ? (sizeof(OutT) == 2 ? "gemm_fp8<128x128,bf16>" : "gemm_fp8<128x128,f32>")
-                     : CF::BN == 128 ? (sizeof(OutT) == 2 ? "gemm_fp8<256x128,bf16>" : "gemm_fp8<256x128,f32>")
-                                     : (sizeof(OutT) == 2 ? "gemm_fp8<256x256,bf16>" : "gemm_fp8<256x256,f32>");
-  KernelInfo ki{name, 2.0 * f.M * f.N * (double)f.K,
-                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + (double)f.M * f.N * sizeof(OutT)};
-  constexpr int lds = fp8_lds<CF>();
+template <typename T>
+orbit_status run_exact(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
+  KernelInfo ki{"gemm_fp8_exact", 2.0 * f.M * f.N * (double)f.K,
+                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + 4.0 * f.M * f.N};
   static const bool attr = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_kernel<T, OutT, CF>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_exact_kernel<T>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, kExactLds);
+    (void)hipGetLastError();
+    return true;
+  }();
+  (void)attr;
+  const dim3 grid((unsigned)(cdiv(a.M, ExactCfg::BM) * cdiv(a.N, ExactCfg::BN)));
+  return launch(ki, gemm_fp8_exact_kernel<T>, grid, dim3(ExactCfg::NT), (size_t)kExactLds, s, a);
+}
+
+template <typename T, typename OutT, int NS>
+orbit_status run_tile(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
+  KernelInfo ki{sizeof(OutT) == 2 ? "gemm_fp8_tile<bf16>" : "gemm_fp8_tile<f32>", 2.0 * f.M * f.N * (double)f.K,
+                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + (double)f.M * f.N * sizeof(OutT)};
+  constexpr int lds = TileCfg<NS>::LDS;
+  static const bool attr = [] {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_tile_kernel<T, OutT, NS>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     (void)hipGetLastError();
     return true;
   }();
   (void)attr;
-  const dim3 grid((unsigned)(cdiv(a.M, CF::BM) * cdiv(a.N, CF::BN)), 1, (unsigned)a.splits);
-  return launch(ki, gemm_fp8_kernel<T, OutT, CF>, grid, dim3(CF::NT), (size_t)lds, s, a);
+  const dim3 grid((unsigned)(cdiv(a.M, 128) * cdiv(a.N, 128)), 1, (unsigned)a.splits);
+  return launch(ki, gemm_fp8_tile_kernel<T, OutT, NS>, grid, dim3(256), (size_t)lds, s, a);
+}
+
+template <WideEpi EPI>
+orbit_status run_wide(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
+  KernelInfo ki{"gemm_fp8_wide", 2.0 * f.M * f.N * (double)f.K,
+                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + 2.0 * f.M * f.N};
+  static const bool attr = [] {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_wide_kernel<EPI>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, kWideLds);
+    (void)hipGetLastError();
+    return true;
+  }();
+  (void)attr;
+  const dim3 grid((unsigned)std::min<int64_t>(cdiv(a.M, 256) * cdiv(a.N, 256), 256));
+  return launch(ki, gemm_fp8_wide_kernel<EPI>, grid, dim3(256), (size_t)kWideLds, s, a);
 }
 
 template <typename T, typename OutT>
@@ -453,21 +975,32 @@ template <typename T, typename OutT>
 orbit_status run_typed8(const Fp8Gemm& f, const Fp8Args& a, Fp8Tile t, hipStream_t s) {
   switch (t) {
     case kThin: return run_thin<T, OutT>(f, a, s);
-    case kQuarter: return run_fp8<T, OutT, DmaQuarter>(f, a, s);
-    case kHalf: return run_fp8<T, OutT, DmaHalf>(f, a, s);
-    default: return run_fp8<T, OutT, DmaPP>(f, a, s);
+    case kTile:
+      if constexpr (sizeof(OutT) == 2)
+        if (cdiv(a.M, 128) * cdiv(a.N, 128) * a.splits <= 256) return run_tile<T, OutT, 4>(f, a, s);
+      return run_tile<T, OutT, 2>(f, a, s);
+    default:
+      if constexpr (sizeof(OutT) == 2) {
+        if (f.epi.gelu_out) return run_wide<kWideGelu>(f, a, s);
+        if (f.epi.gelu_in) return run_wide<kWideGeluGrad>(f, a, s);
+        return f.epi.res ? run_wide<kWideRes>(f, a, s) : run_wide<kWidePlain>(f, a, s);
+      } else {
+        return run_exact<T>(f, a, s);
+      }
   }
 }
 
 }  // namespace
 
 size_t fp8_gemm_workspace_bytes(int M, int N, int K) {
-  const Fp8Choice c = pick_fp8(M, N, K);
-  return c.splits > 1 ? align_up((size_t)c.splits * (size_t)M * (size_t)N * sizeof(float)) : 0;
+  const int sp = std::max(pick_fp8(M, N, K, false).splits, pick_fp8(M, N, K, true).splits);
+  return sp > 1 ? align_up((size_t)sp * (size_t)M * (size_t)N * sizeof(float)) : 0;
 }
 
 orbit_status fp8_gemm(const Fp8Gemm& f, void* ws, size_t ws_bytes, hipStream_t s) {
-  Fp8Choice c = pick_fp8(f.M, f.N, f.K);
+  Fp8Choice c = pick_fp8(f.M, f.N, f.K, f.out_f32 || f.dtype == ORBIT_F32);
+  // the wide kernel's 32 rows of results lie within 31-bit offsets
+  if (c.tile == kFull && !f.out_f32 && f.ldc >= (1 << 24)) c.tile = kTile;
   Fp8Args a{};
   a.A = static_cast<const uint8_t*>(f.A); a.Ae = a.A + fp8_exp_offset(f.M, f.K);
   a.B = static_cast<const uint8_t*>(f.B); a.Be = a.B + fp8_exp_offset(f.N, f.K);
@@ -477,16 +1010,13 @@ orbit_status fp8_gemm(const Fp8Gemm& f, void* ws, size_t ws_bytes, hipStream_t s
   a.M = f.M; a.N = f.N; a.slices = (int)(a.lda / 64);
   a.epi = f.epi;
   a.epi.alpha = 1.f;
-  a.splits = 1;
-  a.per_split = (int)align_up((size_t)a.slices, 8);
+  a.splits = c.splits;
   if (c.splits > 1) {
     if (ws_bytes < fp8_gemm_workspace_bytes(f.M, f.N, f.K)) {
       set_error("fp8 product: workspace of %zu bytes is smaller than the %zu required", ws_bytes,
                 fp8_gemm_workspace_bytes(f.M, f.N, f.K));
       return ORBIT_E_ARG;
     }
-    a.per_split = per_split_of(a.slices, c.splits);
-    a.splits = (int)cdiv(a.slices, a.per_split);
     a.partial = static_cast<float*>(ws);
   }
   if (f.dtype == ORBIT_F32) ORBIT_TRY((run_typed8<float, float>(f, a, c.tile, s)));

@@ -251,3 +251,29 @@ def test_full_size_block(lib):
         if k == "b_qkv":
             continue  # its key part vanishes but for rounding
         assert float((u.double() - v.double()).norm()) <= 0.15 * float(v.double().norm()), k
+
+
+def test_block_fp8_of_many_tokens(lib):
+    """Enough tokens that every product of the block takes the tiles for large ones, with each of their epilogues:
+    the samples are the same in parts that take the small tiles. Sums in another order round some bf16 values to
+    their neighbours, 2^-8 away, and such a value takes the next code one time in 2^-4 / 2^-8 = 16, moving by up to
+    2^-3. Were every value so moved, that is 2^-3 / sqrt(16) = 2^-5 in the root mean square for an operand, and a row
+    passes four products forward and four back with two operands that moved at most: sqrt(16) 2^-5 = 2^-3. A row
+    that were wrong or lost differs by its own size."""
+    case = ("bf16", 48, 257, 1024, 16, 64, 4096, 1)
+    big = _Block(lib, case, True, None)
+    y, dx, g = big.run()
+    part = _Block(lib, (case[0], 6) + case[2:], True, None)
+    part.P, part.w8, part.opt = big.P, big.w8, big.opt
+    rows = lambda t: t.double().norm(dim=-1)
+    total = {k: torch.zeros_like(v) for k, v in g.items()}
+    for i in range(0, 48, 6):
+        part.gx, part.gdy = big.gx[i:i + 6].contiguous(), big.gdy[i:i + 6].contiguous()
+        py, pdx, pg = part.run()
+        for got, want in ((y[i:i + 6], py), (dx[i:i + 6], pdx)):
+            assert (rows(got.double() - want.double()) <= 2.0 ** -3 * rows(want)).all()
+        for k in total:
+            total[k] += pg[k]
+    for k in g:
+        if k not in ("b_qkv", "qn_g", "qn_b", "kn_g", "kn_b"):  # sums that cancel
+            assert float((g[k] - total[k]).norm()) <= 2.0 ** -3 * float(total[k].norm()), k

@@ -332,17 +332,18 @@ def test_linear_graph_and_streams(lib):
             assert all(torch.equal(x, y) for x, y in zip(got, outs(t)))
 
 
-@pytest.mark.slow
-def test_full_size(lib):
-    """A product over every kind of tile at a block's size, against float64 on the device."""
-    M, N, K = 4096, 2056, 4104
-    x, w = _data(M, K, "bf16", 1).cuda(), _data(N, K, "bf16", 2).cuda()
+@pytest.mark.parametrize("M,N,K", [(4096, 2056, 4104), (3500, 3336, 64), (3500, 3336, 129), (3500, 3336, 700), (3500, 3336, 1030),
+                                   (2000, 8200, 2056)])
+def test_full_size(lib, M, N, K):
+    """Products of many tiles, of every length of the pipeline's start and end, against float64 on the device."""
+    ld = -(-K // 8) * 8
+    x, w = (torch.nn.functional.pad(_data(r, K, "bf16", i), (0, ld - K)).cuda() for i, r in ((1, M), (2, N)))
     a, b = _bytes(lib.orbit_fp8_bytes(M, K)), _bytes(lib.orbit_fp8_bytes(N, K))
-    lib.orbit_fp8_pack(1, M, K, 1, x, K, a)
-    lib.orbit_fp8_pack(1, N, K, 128, w, K, b)
-    va, vb = torch.empty(M, K, device="cuda"), torch.empty(N, K, device="cuda")
-    lib.orbit_fp8_unpack(0, M, K, a, va, K)
-    lib.orbit_fp8_unpack(0, N, K, b, vb, K)
+    lib.orbit_fp8_pack(1, M, K, 1, x, ld, a)
+    lib.orbit_fp8_pack(1, N, K, 128, w, ld, b)
+    va, vb = torch.zeros(M, ld, device="cuda"), torch.zeros(N, ld, device="cuda")
+    lib.orbit_fp8_unpack(0, M, K, a, va, ld)
+    lib.orbit_fp8_unpack(0, N, K, b, vb, ld)
     ref = va.double() @ vb.double().t()
     s = va.abs().double() @ vb.abs().double().t()
     ws = _bytes(lib.orbit_fp8_gemm_workspace_bytes(M, N, K))
@@ -350,7 +351,13 @@ def test_full_size(lib):
     lib.orbit_fp8_gemm(1, M, N, K, a, b, C, N, 1, None, 0, ws)
     assert ((C.double() - ref).abs() <= (K + 24) * F.U32 * s).all()
     # errors of independent roundings: far below that
-    assert float((C.double() - ref).norm() / ref.norm()) < 4 * F.U32 * (K / 16) ** 0.5
-    H = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
-    lib.orbit_fp8_gemm(1, M, N, K, a, b, H, N, 0, None, 0, ws)
-    assert float((H.double() - ref).norm() / ref.norm()) < F.HALF["bf16"]
+    assert float((C.double() - ref).norm() / ref.norm()) < 4 * F.U32 * max(1.0, K / 16) ** 0.5
+    H = torch.full((M, N + 8), 3.0, dtype=torch.bfloat16, device="cuda")
+    bias = _data(1, N, "bf16", 3).cuda()
+    lib.orbit_fp8_gemm(1, M, N, K, a, b, H, N + 8, 0, bias, 0, ws)
+    assert (H[:, N:] == 3.0).all()
+    H, ref = H[:, :N].double(), ref + bias.double()
+    assert float((H - ref).norm() / ref.norm()) < F.HALF["bf16"]
+    # the largest product of a step is at most va.max vb.max: each of K loses less than 2^-13 of it
+    lost = K * 2.0 ** -13 * va.abs().amax(1, keepdim=True).double() * vb.abs().amax(1).double()
+    assert ((H - ref).abs() <= lost + F.HALF["bf16"] * ref.abs() * 1.01).all()
