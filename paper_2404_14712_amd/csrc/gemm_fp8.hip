@@ -12,16 +12,18 @@
 // turned into bf16 with their scales in the fragments, which is exact, and the bf16
 // instructions keep every bit a float32 sum can, at half the rate.
 //
-// Results of more than 64 rows go through LDS, whose rings are filled by copies without
+// The other products go through LDS, whose rings are filled by copies without
 // registers (dma.h). Three kernels share that work:
 //   wide   256 x 256 on 4 waves, one block per CU that walks over tiles: bf16 results of
 //          192 tiles of 256 x 256 on;
 //   exact  256 x 256 on two groups of 4 waves that take turns at decoding and multiplying:
 //          float32 results of as many tiles and K of 2048 on;
-//   tile   128 x 128 on 4 waves, K split where there are few tiles: the rest.
+//   tile   128 x 128, 64 x 128 or 64 x 64 on 4 waves, the smallest that leaves a block per CU,
+//          K split where there are few: the rest.
 //
-// Up to 64 rows of A (single tokens) the product is bound by reading B once:
-// fp8_thin_kernel streams it past 16x16x128 instructions without LDS.
+// A few rows of A (single tokens) read B once, and what counts is the latency of that one
+// read: fp8_thin_kernel spreads it over the waves of many small blocks, past 16x16x128
+// instructions without LDS.
 #include <algorithm>
 #include <type_traits>
 
@@ -309,23 +311,29 @@ __global__ void __launch_bounds__(ExactCfg::NT, ExactCfg::OCC) gemm_fp8_exact_ke
   fp8_epilogue<T, float, CF>(g, acc, smem, wave, lane, m0, n0, 0);
 }
 
-// Tiles of 128 x 128 on 4 waves of 64 x 64. A stage is a block of 128 k: rows of 128 bytes,
-// whole cache lines, as in the wide kernel below; its halves of 64 k pass through two sets
-// of registers, so that products cover the reads, and one barrier serves 128 k (stages of
-// 64 k and rows of 64 bytes: 8192 x 1024 x 4096 46 us against 39, 2048 x 4096 x 2048 25.7
-// against 22.8). Two stages leave room for two blocks per CU; up to 256 blocks there is one
-// per CU anyway and bf16 results take four (1024 x 4096 x 4096 24.8 us against 28.0, and with
-// 512 tiles 48.9 against 39.2); float32 results, which are bound by decoding, do not gain
-// (1024 x 1024 x 1024 13.1 us against 12.5).
-template <int NS>
+// Tiles of 128 x 128, 64 x 128 or 64 x 64 on 4 waves. A stage is a block of 128 k: rows of
+// 128 bytes, whole cache lines, as in the wide kernel below; its halves of 64 k pass through
+// two sets of registers, so that products cover the reads, and one barrier serves 128 k
+// (stages of 64 k and rows of 64 bytes: 8192 x 1024 x 4096 46 us against 39, 2048 x 4096 x 2048
+// 25.7 against 22.8).
+//
+// What a lone block per CU takes is the latency of its stages one after another, so that few
+// tiles are cut small, while there are at most 256: 1024 x 1024 x 1024 on 128 x 128, 64 x 128,
+// 64 x 64 9.6, 7.2, 6.3 us (float32 results 12.4, 9.9, 8.5), 1770 x 1000 x 2056 15.2, 10.9.
+// Two stages leave room for two blocks per CU; up to 256 blocks there is one per CU anyway and
+// four are taken (128 x 128: 1024 x 4096 x 4096 24.8 us against 28.0, and with 512 tiles 48.9
+// against 39.2; 64 x 128: 2048 x 1024 x 4096 17.3 against 22.5). Float32 results on 128 x 128,
+// bound by decoding, keep two (1024 x 1024 x 1024 13.1 us against 12.5).
+template <int BM_, int BN_, int NS>
 struct TileCfg {
-  static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, TM = 2, TN = 2;
+  static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, TM = BM / 64, TN = BN / 64;
   static constexpr int OPA = BM * 128, STB = OPA + BN * 128, E = NS * STB, LDS = E + 2 * (BM + BN) * 4;
   static_assert(LDS >= 4 * 32 * (TN * 32 + 8) * 4, "the epilogue's rows");
 };
-template <typename T, typename OutT, int NS>
+template <typename T, typename OutT, int BM_, int BN_, int NS>
 __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8Args g) {
-  using CF = TileCfg<NS>;
+  using CF = TileCfg<BM_, BN_, NS>;
+  constexpr int NA = CF::BM / 32, NB = CF::BN / 32;  // copies of a wave per stage
   constexpr int BM = CF::BM, BN = CF::BN, TM = CF::TM, TN = CF::TN;
   constexpr bool EXACT = sizeof(OutT) == 4;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -344,29 +352,33 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
   const uint8_t* Aeb = g.Ae + (int64_t)m0 * g.gpa;
   const uint8_t* Beb = g.Be + (int64_t)n0 * g.gpb;
 
-  // copy c of a wave: rows 8 (4 wave + c) + lane / 8 of the operand; rows behind its last
-  // one read zeros
-  unsigned va[4], vb[4];
+  // copy c of a wave's n: rows 8 (n wave + c) + lane / 8 of the operand; rows behind its
+  // last one read zeros
+  unsigned va[NA], vb[NB];
+  auto offsets = [&](unsigned* v, int n, int64_t ld, int rows) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int r = (wave * 4 + c) * 8 + (lane >> 3), k = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
-    va[c] = r < rm ? (unsigned)(r * (int)g.lda + k) : kOobOffset;
-    vb[c] = r < rn ? (unsigned)(r * (int)g.ldb + k) : kOobOffset;
-  }
-  // E words: wave w copies those of 64 rows, of A (w < 2) or of B
-  const int er = (wave & 1) * 64 + lane;
-  const unsigned ve = wave < 2 ? (er < rm ? (unsigned)(er * g.gpa) : kOobOffset) : (er < rn ? (unsigned)(er * g.gpb) : kOobOffset);
+    for (int c = 0; c < n; ++c) {
+      const int r = (wave * n + c) * 8 + (lane >> 3), k = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+      v[c] = r < rows ? (unsigned)(r * (int)ld + k) : kOobOffset;
+    }
+  };
+  offsets(va, NA, g.lda, rm);
+  offsets(vb, NB, g.ldb, rn);
+  // E words, of A's rows and then of B's: wave w copies 64 of them
+  const bool ofa = wave < BM / 64;
+  const int er = wave * 64 + lane - (ofa ? 0 : BM);
+  const unsigned ve = er < (ofa ? rm : rn) ? (unsigned)(er * (ofa ? g.gpa : g.gpb)) : kOobOffset;
   const unsigned lds0 = (unsigned)(uintptr_t)(ORBIT_LDS void*)smem;
   auto issue = [&](int st) {
     const int b = b0 + st;
-    if ((b & 3) == 0 || st == 0)  // before the stage's codes: landed when these have
-      dma4(buffer_rsrc((wave < 2 ? Aeb : Beb) + (b >> 2) * 4), lds0 + CF::E + ((b >> 2) & 1) * ((BM + BN) * 4) + wave * 256, ve);
-    const unsigned at = lds0 + (st % NS) * CF::STB + wave * 4096;
+    if (((b & 3) == 0 || st == 0) && wave < (BM + BN) / 64)  // before the stage's codes: landed when these have
+      dma4(buffer_rsrc((ofa ? Aeb : Beb) + (b >> 2) * 4), lds0 + CF::E + ((b >> 2) & 1) * ((BM + BN) * 4) + wave * 256, ve);
+    const unsigned at = lds0 + (st % NS) * CF::STB;
     const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(Ab + (int64_t)st * 128), rb = buffer_rsrc(Bb + (int64_t)st * 128);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) dma16(ra, at + c * 1024, va[c]);
+    for (int c = 0; c < NA; ++c) dma16(ra, at + (wave * NA + c) * 1024, va[c]);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) dma16(rb, at + CF::OPA + c * 1024, vb[c]);
+    for (int c = 0; c < NB; ++c) dma16(rb, at + CF::OPA + (wave * NB + c) * 1024, vb[c]);
   };
   int ea[TM], eb[TN];
   auto scales = [&](int st) {
@@ -375,9 +387,9 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
       const int* E = reinterpret_cast<const int*>(smem + CF::E + ((b >> 2) & 1) * ((BM + BN) * 4));
       const int by = (b & 3) * 8;
 #pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)E[wm * 64 + i * 32 + (lane & 31)] >> by);
+      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)E[wm * TM * 32 + i * 32 + (lane & 31)] >> by);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)E[BM + wn * 64 + j * 32 + (lane & 31)] >> by);
+      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)E[BM + wn * TN * 32 + j * 32 + (lane & 31)] >> by);
     } else {
 #pragma unroll
       for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)ea[i] >> 8);
@@ -386,7 +398,7 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
     }
   };
   const int lr = lane & 31;
-  const unsigned oa = (unsigned)((wm * 64 + lr) * 128), ob = (unsigned)(CF::OPA + (wn * 64 + lr) * 128);
+  const unsigned oa = (unsigned)((wm * TM * 32 + lr) * 128), ob = (unsigned)(CF::OPA + (wn * TN * 32 + lr) * 128);
   unsigned x[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) x[q] = (unsigned)(((2 * q + (lane >> 5)) ^ ((lr >> 1) & 7)) << 4);
@@ -412,7 +424,7 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
 #pragma unroll
   for (int st = 0; st < NS; ++st)
     if (st < nk) issue(st);
-  wait_stage<8, NS + 1>(min(nk - 1, NS - 1));
+  wait_stage<NA + NB, NS + 1>(min(nk - 1, NS - 1));
   __syncthreads();
   i32x8 fa[TM], fb[TN], ga[TM], gb[TN];
   read(fa, fb, smem, 0);
@@ -423,7 +435,7 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
     mma_slice<TM, TN, EXACT>(acc, fa, fb, ea, eb);
     // the stage is in registers everywhere and the next one has landed
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    wait_stage<8, NS + 1>(max(min(nk - kt - 2, NS - 2), 0));
+    wait_stage<NA + NB, NS + 1>(max(min(nk - kt - 2, NS - 2), 0));
     __syncthreads();
     // past the last stage this reads a stale but in-bounds slot
     read(fa, fb, smem + ((kt + 1) % NS) * CF::STB, 0);
@@ -801,50 +813,39 @@ __global__ void __launch_bounds__(kThinWaves * 64) fp8_thin_kernel(Fp8Args g) {
   const int split = blockIdx.z;
   const int b0 = fp8_split_at(g, split), b1 = fp8_split_at(g, split + 1);  // K blocks
   // rows past the operands read row 0 again: their results are not stored
-  const bool bv = n0 + lr < g.N;
-  const int64_t br = bv ? n0 + lr : 0;
-  const uint8_t* pb = g.B + br * g.ldb + kc;
-  const uint8_t* pbe = g.Be + br * g.gpb;
+  const int64_t br = n0 + lr < g.N ? n0 + lr : 0;
+  const uint8_t *pb = g.B + br * g.ldb + kc, *pbe = g.Be + br * g.gpb;
   const uint8_t *pa[MT], *pae[MT];
+  f32x4 acc[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int64_t ar = t * 16 + lr < g.M ? t * 16 + lr : 0;
     pa[t] = g.A + ar * g.lda + kc;
     pae[t] = g.Ae + ar * g.gpa;
+    acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  f32x4 acc[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto ld32 = [](const uint8_t* p) {
     const i32x4 a = *reinterpret_cast<const i32x4*>(p), b = *reinterpret_cast<const i32x4*>(p + 16);
     return i32x8(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  // U blocks at a time, the next ones' loads in flight
-  constexpr int U = MT > 2 ? 1 : 2;
-  i32x8 fb[U], fa[U][MT];
-  int eb[U], ea[U][MT];
-  auto fetch = [&](int kb, i32x8* vb, i32x8 (*va)[MT], int* web, int (*wea)[MT]) {
+  // n blocks, all their loads in flight
+  auto blocks = [&](int kb, auto n) {
+    constexpr int NU = decltype(n)::value;
+    i32x8 fb[NU], fa[NU][MT];
+    int eb[NU], ea[NU][MT];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      // past the range the last block again: not used
-      const int k = min(kb + u * kThinWaves, b1 - 1);
-      vb[u] = ld32(pb + (int64_t)k * 128);
-      web[u] = pbe[k];
+    for (int u = 0; u < NU; ++u) {
+      const int k = kb + u * kThinWaves;
+      fb[u] = ld32(pb + (int64_t)k * 128);
+      eb[u] = pbe[k];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        va[u][t] = ld32(pa[t] + (int64_t)k * 128);
-        wea[u][t] = pae[t][k];
+        fa[u][t] = ld32(pa[t] + (int64_t)k * 128);
+        ea[u][t] = pae[t][k];
       }
     }
-  };
-  if (b0 + wave < b1) fetch(b0 + wave, fb, fa, eb, ea);
-  for (int kb = b0 + wave; kb < b1; kb += U * kThinWaves) {
-    i32x8 nb[U], na[U][MT];
-    int neb[U], nea[U][MT];
-    fetch(kb + U * kThinWaves, nb, na, neb, nea);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (kb + u * kThinWaves >= b1) break;
+    for (int u = 0; u < NU; ++u) {
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
         if constexpr (sizeof(OutT) == 2) {
@@ -858,22 +859,15 @@ __global__ void __launch_bounds__(kThinWaves * 64) fp8_thin_kernel(Fp8Args g) {
         }
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      fb[u] = nb[u];
-      eb[u] = neb[u];
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        fa[u][t] = na[u][t];
-        ea[u][t] = nea[u][t];
-      }
-    }
-  }
+  };
+  constexpr int U = 4;  // all of a wave's up to K = 4096 (2 and their next ones: 7.7 us against 6.0 at 1 x 4096 x 4096)
+  int kb = b0 + wave;
+  for (; kb + (U - 1) * kThinWaves < b1; kb += U * kThinWaves) blocks(kb, std::integral_constant<int, U>{});
+  for (; kb < b1; kb += kThinWaves) blocks(kb, std::integral_constant<int, 1>{});
 #pragma unroll
   for (int t = 0; t < MT; ++t) sum[wave][t][lane] = acc[t];
   __syncthreads();
-  // a thread per value: row t * 16 + (l & 15), column 4 (l >> 4) + v, the waves'
-  // sums in wave order
+  // a thread per value of row i / 16, column i & 15: the waves' sums in wave order
   const float* fs = reinterpret_cast<const float*>(&sum[0][0][0]);
   for (int i = threadIdx.x; i < MT * 256; i += kThinWaves * 64) {
     const int r = i >> 4, c = i & 15;
@@ -893,23 +887,30 @@ struct Fp8Choice { Fp8Tile tile; int splits; };
 
 Fp8Choice pick_fp8(int M, int N, int K, bool out_f32) {
   const int64_t slices = fp8_wide(K) / 64;
-  if (M <= 64) {
-    // a block per CU at least
+  // Thin, by the block's columns and what a wave has to read of A: 1 x 4096 x 1024 2.7 us against
+  // 5.1 on tiles, 16 x 4096 x 1024 3.2 against 5.1, 16 x 8192 x 1024 4.7 against 5.6, 32 x 4096 x
+  // 1024 3.9 against 5.3; but 8 x 16384 x 4096 21.5 against 17.7, 32 x 8192 x 1024 6.0 against 5.8,
+  // 32 x 4096 x 4096 10.6 against 9.5.
+  if (M <= 16 ? N <= 8192 : M <= 32 && N <= 4096 && slices <= 32) {
+    // in parts of 16 blocks (K = 2048) from K = 8192 on, up to a block per CU (1 x 1024 x 8192
+    // 7.1 us against 9.1 in one part, 1 x 1024 x 4096 5.7 against 5.3)
     int sp = 1;
-    while (sp < 16 && cdiv(N, 16) * sp < 256 && slices / (2 * sp) >= 32) sp *= 2;
+    while (slices >= 128 && sp < 16 && cdiv(N, 16) * sp < 256 && slices / (2 * sp) >= 32) sp *= 2;
     return {kThin, sp};
   }
-  const int64_t t256 = cdiv(M, 256) * cdiv(N, 256), t128 = cdiv(M, 128) * cdiv(N, 128);
+  const int64_t t256 = cdiv(M, 256) * cdiv(N, 256);
   // (wide: two stages at least; exact: see there)
   if (t256 >= 192 && slices >= (out_f32 ? 32 : 4)) return {kFull, 1};
-  // Split K costs the second launch and writing and reading a partial sum per split, about
-  // 0.75 us for each MB of these (1024 x 1024 x 1024 in 1, 2, 4 parts: 9.6, 14.0, 19.0 us),
-  // and saves slices of 0.27 us (float32 results: 0.42); in units of slices:
-  const double fix = out_f32 ? 4 : 6, per = out_f32 ? 0.12 : 0.18;
+  // Split K saves slices, of 0.135 us each (float32 results: 0.233), and costs the second
+  // launch, 3.5 us, and writing and reading the partial sums, 0.7 us per MB of them: 100 x 512 x
+  // 8192 10.9 us in 8 parts and 20.7 in one, 512 x 1024 x 4096 14.2 in 4 and 12.2 in one. Only
+  // where it leaves one block of 64 x 64 per CU.
+  const int64_t t64 = cdiv(M, 64) * cdiv(N, 64);
+  const double slice = out_f32 ? 0.233 : 0.135, part = 0.7e-6 * 4 * (double)M * N;
   Fp8Choice c{kTile, 1};
-  double best = (double)slices;
-  for (int sp = 2; sp <= 8 && t128 * sp <= 256 && 2 * sp <= slices; sp *= 2) {
-    const double t = (double)slices / sp + fix + per * (double)(sp * t128);
+  double best = slice * (double)slices;
+  for (int sp = 2; sp <= 8 && t64 * sp <= 256 && 2 * sp <= slices; sp *= 2) {
+    const double t = slice * (double)slices / sp + 3.5 + part * sp;
     if (t < best) { best = t; c.splits = sp; }
   }
   return c;
@@ -930,20 +931,20 @@ orbit_status run_exact(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
   return launch(ki, gemm_fp8_exact_kernel<T>, grid, dim3(ExactCfg::NT), (size_t)kExactLds, s, a);
 }
 
-template <typename T, typename OutT, int NS>
+template <typename T, typename OutT, int BM, int BN, int NS>
 orbit_status run_tile(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
   KernelInfo ki{sizeof(OutT) == 2 ? "gemm_fp8_tile<bf16>" : "gemm_fp8_tile<f32>", 2.0 * f.M * f.N * (double)f.K,
                 ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + (double)f.M * f.N * sizeof(OutT)};
-  constexpr int lds = TileCfg<NS>::LDS;
+  constexpr int lds = TileCfg<BM, BN, NS>::LDS;
   static const bool attr = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_tile_kernel<T, OutT, NS>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_tile_kernel<T, OutT, BM, BN, NS>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     (void)hipGetLastError();
     return true;
   }();
   (void)attr;
-  const dim3 grid((unsigned)(cdiv(a.M, 128) * cdiv(a.N, 128)), 1, (unsigned)a.splits);
-  return launch(ki, gemm_fp8_tile_kernel<T, OutT, NS>, grid, dim3(256), (size_t)lds, s, a);
+  const dim3 grid((unsigned)(cdiv(a.M, BM) * cdiv(a.N, BN)), 1, (unsigned)a.splits);
+  return launch(ki, gemm_fp8_tile_kernel<T, OutT, BM, BN, NS>, grid, dim3(256), (size_t)lds, s, a);
 }
 
 template <WideEpi EPI>
@@ -967,8 +968,7 @@ orbit_status run_thin(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
                 ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + (double)f.M * f.N * sizeof(OutT)};
   const dim3 grid((unsigned)cdiv(a.N, 16), 1, (unsigned)a.splits), block(kThinWaves * 64);
   if (a.M <= 16) return launch(ki, fp8_thin_kernel<T, OutT, 1>, grid, block, 0, s, a);
-  if (a.M <= 32) return launch(ki, fp8_thin_kernel<T, OutT, 2>, grid, block, 0, s, a);
-  return launch(ki, fp8_thin_kernel<T, OutT, 4>, grid, block, 0, s, a);
+  return launch(ki, fp8_thin_kernel<T, OutT, 2>, grid, block, 0, s, a);
 }
 
 template <typename T, typename OutT>
@@ -976,9 +976,11 @@ orbit_status run_typed8(const Fp8Gemm& f, const Fp8Args& a, Fp8Tile t, hipStream
   switch (t) {
     case kThin: return run_thin<T, OutT>(f, a, s);
     case kTile:
+      if (cdiv(a.M, 64) * cdiv(a.N, 64) * a.splits <= 256) return run_tile<T, OutT, 64, 64, 4>(f, a, s);
+      if (cdiv(a.M, 64) * cdiv(a.N, 128) * a.splits <= 256) return run_tile<T, OutT, 64, 128, 4>(f, a, s);
       if constexpr (sizeof(OutT) == 2)
-        if (cdiv(a.M, 128) * cdiv(a.N, 128) * a.splits <= 256) return run_tile<T, OutT, 4>(f, a, s);
-      return run_tile<T, OutT, 2>(f, a, s);
+        if (cdiv(a.M, 128) * cdiv(a.N, 128) * a.splits <= 256) return run_tile<T, OutT, 128, 128, 4>(f, a, s);
+      return run_tile<T, OutT, 128, 128, 2>(f, a, s);
     default:
       if constexpr (sizeof(OutT) == 2) {
         if (f.epi.gelu_out) return run_wide<kWideGelu>(f, a, s);
