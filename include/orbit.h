@@ -482,7 +482,7 @@ orbit_status orbit_fp8_unpack(int32_t dtype, int64_t rows, int64_t n, const void
  * multiples of 8, M and K any; K below 2^22. For y = x W take the store of x and the
  * transposed one of W; for dx = dy W^T the stores of dy and of W; for dw = x^T dy the
  * transposed stores of both. Sums are formed in an order that depends on the
- * sizes alone (bitwise reproducible). */
+ * sizes, the types and ldc alone (bitwise reproducible). */
 size_t orbit_fp8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K); /* may be 0; ws may then be NULL */
 orbit_status orbit_fp8_gemm(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* A, size_t a_bytes,
                             const void* B, size_t b_bytes, void* C, int64_t ldc, int32_t c_f32, const void* bias,
