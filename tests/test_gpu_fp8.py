@@ -369,3 +369,57 @@ def test_full_size(lib, M, N, K):
     # the largest product of a step is at most va.max vb.max: each of K loses less than 2^-13 of it
     lost = K * 2.0 ** -13 * va.abs().amax(1, keepdim=True).double() * vb.abs().amax(1).double()
     assert ((H - ref).abs() <= lost + F.HALF["bf16"] * ref.abs() * 1.01).all()
+
+
+def test_beyond_32_bits(lib):
+    """Codes, input and results whose offsets pass 2^31 and 2^32 bytes."""
+    M, N, K, ld, ldc = 530000, 16, 4100, 4104, 4104
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(M, ld, dtype=torch.bfloat16, device="cuda", generator=g)
+    w = torch.randn(N, ld, dtype=torch.bfloat16, device="cuda", generator=g)
+    a, b = _bytes(lib.orbit_fp8_bytes(M, K)), _bytes(lib.orbit_fp8_bytes(N, K))
+    lib.orbit_fp8_pack(1, M, K, 1, x, ld, a)
+    lib.orbit_fp8_pack(1, N, K, 1, w, ld, b)
+    back = torch.empty_like(x)
+    lib.orbit_fp8_unpack(1, M, K, a, back, ld)
+    sel = torch.cat([torch.arange(5), torch.arange(M // 2 - 130, M // 2 + 130), torch.arange(M - 300, M)]).cuda()
+    va, vx = back[sel, :K].double(), x[sel, :K].double()
+    assert ((va - vx).abs() <= 2.0 ** -4 * vx.abs() + 2.0 ** -10 * vx.abs().amax(1, keepdim=True) / 128).all()
+    vb = F.values(w[:, :K].double().cpu()).cuda()
+    ref, s = va @ vb.t(), va.abs() @ vb.abs().t()
+    ws = _bytes(lib.orbit_fp8_gemm_workspace_bytes(M, N, K))
+    del x, back
+    C = torch.zeros(M, ldc, dtype=torch.bfloat16, device="cuda")
+    lib.orbit_fp8_gemm(1, M, N, K, a, b, C, ldc, 0, None, 0, ws)
+    lost = 64 * 2.0 ** -13 * va.abs().amax(1, keepdim=True) * vb.abs().amax(1) * -(-K // 64)
+    assert ((C[sel, :N].double() - ref).abs() <= lost + F.HALF["bf16"] * ref.abs() * 1.01).all()
+    assert float((C[sel, :N].double() - ref).norm() / ref.norm()) < F.HALF["bf16"]
+    assert not C[sel, N:].any()
+    del C
+    D = torch.zeros(M, 2056, device="cuda")
+    lib.orbit_fp8_gemm(1, M, N, K, a, b, D, 2056, 1, None, 0, ws)
+    assert ((D[sel, :N].double() - ref).abs() <= (K + 24) * F.U32 * s).all() and not D[sel, N:].any()
+
+
+def test_products_on_two_streams(lib):
+    """The same stores read by products of every kernel that run side by side, each with its own workspace."""
+    N, K = 3336, 1100
+    cases = [(4096, 0), (4096, 1), (600, 0), (100, 1), (20, 0), (3, 1)]
+    b, _ = _pack(lib, _data(N, K, "bf16", 2))
+    runs = []
+    for M, f32 in cases:
+        a, _ = _pack(lib, _data(M, K, "bf16", M))
+        runs.append((M, f32, a, [_bytes(lib.orbit_fp8_gemm_workspace_bytes(M, N, K)) for _ in range(3)],
+                     [torch.empty(M, N, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda") for _ in range(3)]))
+    call = lambda r, i, s: lib.orbit_fp8_gemm(1, r[0], N, K, r[2], b, r[4][i], N, r[1], None, 0, r[3][i], s)
+    for r in runs:
+        call(r, 0, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            for r in runs if i else runs[::-1]:
+                call(r, i + 1, s)
+    torch.cuda.synchronize()
+    for r in runs:
+        assert torch.equal(r[4][0], r[4][1]) and torch.equal(r[4][0], r[4][2])
