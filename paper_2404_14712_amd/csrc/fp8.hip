@@ -307,7 +307,9 @@ struct UnpackArgs {
   int tx_log2;
 };
 
-// 8 values per thread; 2^tx_log2 threads of a block along a row
+// 8 values per thread; 2^tx_log2 threads of a block along a row, a wave at most: a row's
+// last block is then short by less (float32 1000 x 2056 4.3 us, against 5.8 with 256 along
+// the row; bf16 4096 x 8192 19.5 against 20.5)
 template <typename T>
 __global__ void __launch_bounds__(256) fp8_unpack_kernel(UnpackArgs a) {
   const int tx = 1 << a.tx_log2, ty = 256 >> a.tx_log2;
@@ -374,7 +376,7 @@ orbit_status fp8_unpack(orbit_dtype dt, const void* store, int64_t rows, int64_t
   a.x = x; a.ldx = ldx; a.rows = rows; a.n = n; a.wide = fp8_wide(n); a.groups = fp8_groups(n);
   const int64_t pieces = cdiv(n, 8);
   a.tx_log2 = 2;
-  while (a.tx_log2 < 8 && (1ll << a.tx_log2) < pieces) ++a.tx_log2;
+  while (a.tx_log2 < 6 && (1ll << a.tx_log2) < pieces) ++a.tx_log2;
   const double v = (double)rows * (double)n;
   KernelInfo ki{dt == ORBIT_BF16 ? "fp8_unpack<bf16>" : "fp8_unpack<f32>", 2.0 * v,
                 v * ((dt == ORBIT_BF16 ? 2.0 : 4.0) + 1.0 + 1.0 / kFp8Block)};
