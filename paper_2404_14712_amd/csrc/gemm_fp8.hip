@@ -320,32 +320,42 @@ __global__ void __launch_bounds__(ExactCfg::NT, ExactCfg::OCC) gemm_fp8_exact_ke
 // What a lone block per CU takes is the latency of its stages one after another, so that few
 // tiles are cut small, while there are at most 256: 1024 x 1024 x 1024 on 128 x 128, 64 x 128,
 // 64 x 64 9.6, 7.2, 6.3 us (float32 results 12.4, 9.9, 8.5), 1770 x 1000 x 2056 15.2, 10.9.
-// Two stages leave room for two blocks per CU; up to 256 blocks there is one per CU anyway and
-// four are taken (128 x 128: 1024 x 4096 x 4096 24.8 us against 28.0, and with 512 tiles 48.9
-// against 39.2; 64 x 128: 2048 x 1024 x 4096 17.3 against 22.5). Float32 results on 128 x 128,
-// bound by decoding, keep two (1024 x 1024 x 1024 13.1 us against 12.5).
-template <int BM_, int BN_, int NS>
+// Long K is shared by two groups of waves, whose sums meet in LDS at the end: bf16 results
+// 1024 x 1024 x 4096 12.8 -> 11.5 us, 1024 x 4096 x 4096 25.1 -> 23.6, 512 x 512 x 2048 8.0 -> 7.8,
+// but 512 x 4096 x 1536 9.2 -> 9.6 (on 128 x 128 from K = 1024: 2048 x 2048 x 1024 11.7 -> 11.2); float32 results, which have more to do on a stage, 1024 x 1024
+// x 1024 8.6 -> 8.1, 150 x 768 x 1000 7.0 -> 6.5, but 512 x 512 x 256 4.26 -> 4.58 and none on
+// 128 x 128. One group has three stages in flight (64 x 128 on two: 2048 x 1024 x 4096 22.5 us
+// against 17.3), except where two blocks share a CU (8192 x 1024 x 4096 39.2 us with two stages
+// and two blocks, 48.9 with four and one).
+// BM x BN by KG groups of 4 waves, each with its part of K and its own ring of NS stages
+template <int BM_, int BN_, int NS, int KG>
 struct TileCfg {
-  static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, TM = BM / 64, TN = BN / 64;
-  static constexpr int OPA = BM * 128, STB = OPA + BN * 128, E = NS * STB, LDS = E + 2 * (BM + BN) * 4;
-  static_assert(LDS >= 4 * 32 * (TN * 32 + 8) * 4, "the epilogue's rows");
+  static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, TM = BM / 64, TN = BN / 64, NT = KG * 256;
+  static constexpr int OPA = BM * 128, STB = OPA + BN * 128, E = NS * STB, RING = E + 2 * (BM + BN) * 4;
+  static constexpr int EPB = 4 * 32 * (TN * 32 + 8) * 4;              // epilogue's rows
+  static constexpr int SUM = (KG - 1) * 4 * TM * TN * 16 * 64 * 4;    // the other groups' sums, behind these
+  static constexpr int LDS = KG * RING;
+  static_assert(LDS >= EPB + SUM && LDS <= 160 * 1024, "LDS");
 };
-template <typename T, typename OutT, int BM_, int BN_, int NS>
-__global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8Args g) {
-  using CF = TileCfg<BM_, BN_, NS>;
+template <typename T, typename OutT, int BM_, int BN_, int NS, int KG>
+__global__ void __launch_bounds__(KG * 256, KG == 1 && NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8Args g) {
+  using CF = TileCfg<BM_, BN_, NS, KG>;
   constexpr int NA = CF::BM / 32, NB = CF::BN / 32;  // copies of a wave per stage
   constexpr int BM = CF::BM, BN = CF::BN, TM = CF::TM, TN = CF::TN;
   constexpr bool EXACT = sizeof(OutT) == 4;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  extern __shared__ __attribute__((aligned(1024))) char shared[];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, grp = __builtin_amdgcn_readfirstlane(tid >> 8);
+  char* smem = shared + grp * CF::RING;
   const int wm = wave % CF::WM, wn = wave / CF::WM;
   int m0, n0, split;
   fp8_tile<BM, BN>(g, m0, n0, split);
   m0 = __builtin_amdgcn_readfirstlane(m0);
   n0 = __builtin_amdgcn_readfirstlane(n0);
   split = __builtin_amdgcn_readfirstlane(split);
-  const int b0 = fp8_split_at(g, split), nk = fp8_split_at(g, split + 1) - b0;  // stages
+  const int beg = fp8_split_at(g, split), nb = fp8_split_at(g, split + 1) - beg;
+  const int b0 = beg + nb * grp / KG, nk = beg + nb * (grp + 1) / KG - b0;  // the group's stages
+  const int steps = (nb + KG - 1) / KG;                                      // the longest group's
   const int rm = min(g.M - m0, BM), rn = min(g.N - n0, BN);
   const uint8_t* Ab = g.A + (int64_t)m0 * g.lda + (int64_t)b0 * 128;
   const uint8_t* Bb = g.B + (int64_t)n0 * g.ldb + (int64_t)b0 * 128;
@@ -424,15 +434,18 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
 #pragma unroll
   for (int st = 0; st < NS; ++st)
     if (st < nk) issue(st);
-  wait_stage<NA + NB, NS + 1>(min(nk - 1, NS - 1));
+  wait_stage<NA + NB, NS + 1>(max(min(nk - 1, NS - 1), 0));
   __syncthreads();
   i32x8 fa[TM], fb[TN], ga[TM], gb[TN];
   read(fa, fb, smem, 0);
-  for (int kt = 0; kt < nk; ++kt) {
+  for (int kt = 0; kt < steps; ++kt) {
+    const bool on = KG == 1 || kt < nk;
     const char* here = smem + (kt % NS) * CF::STB;
-    scales(kt);
-    read(ga, gb, here, 1);
-    mma_slice<TM, TN, EXACT>(acc, fa, fb, ea, eb);
+    if (on) {
+      scales(kt);
+      read(ga, gb, here, 1);
+      mma_slice<TM, TN, EXACT>(acc, fa, fb, ea, eb);
+    }
     // the stage is in registers everywhere and the next one has landed
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     wait_stage<NA + NB, NS + 1>(max(min(nk - kt - 2, NS - 2), 0));
@@ -440,11 +453,39 @@ __global__ void __launch_bounds__(256, NS == 2 ? 2 : 1) gemm_fp8_tile_kernel(Fp8
     // past the last stage this reads a stale but in-bounds slot
     read(fa, fb, smem + ((kt + 1) % NS) * CF::STB, 0);
     if (kt + NS < nk) issue(kt + NS);
-    mma_slice<TM, TN, EXACT>(acc, ga, gb, ea, eb);
+    if (on) mma_slice<TM, TN, EXACT>(acc, ga, gb, ea, eb);
   }
   wait_vmcnt<0>();
   __syncthreads();
-  fp8_epilogue<T, OutT, CF>(g, acc, smem, wave, lane, m0, n0, split);
+  if constexpr (KG > 1) {
+    // the groups' sums in their order
+    f32x4* sums = reinterpret_cast<f32x4*>(shared + CF::EPB);
+    auto at = [&](int q, int i, int j, int v) { return ((((q - 1) * 4 + wave) * TM * TN + i * TN + j) * 4 + v) * 64 + lane; };
+    if (grp) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            sums[at(grp, i, j, v)] = f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+    }
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int q = 1; q < KG; ++q)
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const f32x4 t = sums[at(q, i, j, v)];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][4 * v + e] += t[e];
+          }
+  }
+  fp8_epilogue<T, OutT, CF>(g, acc, shared, wave, lane, m0, n0, split);
 }
 
 // bf16 results of many tiles: 256 x 256 on 4 waves of 128 x 128, one per SIMD. A
@@ -931,20 +972,20 @@ orbit_status run_exact(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
   return launch(ki, gemm_fp8_exact_kernel<T>, grid, dim3(ExactCfg::NT), (size_t)kExactLds, s, a);
 }
 
-template <typename T, typename OutT, int BM, int BN, int NS>
+template <typename T, typename OutT, int BM, int BN, int NS, int KG>
 orbit_status run_tile(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
   KernelInfo ki{sizeof(OutT) == 2 ? "gemm_fp8_tile<bf16>" : "gemm_fp8_tile<f32>", 2.0 * f.M * f.N * (double)f.K,
                 ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + (double)f.M * f.N * sizeof(OutT)};
-  constexpr int lds = TileCfg<BM, BN, NS>::LDS;
+  constexpr int lds = TileCfg<BM, BN, NS, KG>::LDS;
   static const bool attr = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_tile_kernel<T, OutT, BM, BN, NS>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_tile_kernel<T, OutT, BM, BN, NS, KG>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     (void)hipGetLastError();
     return true;
   }();
   (void)attr;
   const dim3 grid((unsigned)(cdiv(a.M, BM) * cdiv(a.N, BN)), 1, (unsigned)a.splits);
-  return launch(ki, gemm_fp8_tile_kernel<T, OutT, BM, BN, NS>, grid, dim3(256), (size_t)lds, s, a);
+  return launch(ki, gemm_fp8_tile_kernel<T, OutT, BM, BN, NS, KG>, grid, dim3(KG * 256), (size_t)lds, s, a);
 }
 
 template <WideEpi EPI>
@@ -975,12 +1016,15 @@ template <typename T, typename OutT>
 orbit_status run_typed8(const Fp8Gemm& f, const Fp8Args& a, Fp8Tile t, hipStream_t s) {
   switch (t) {
     case kThin: return run_thin<T, OutT>(f, a, s);
-    case kTile:
-      if (cdiv(a.M, 64) * cdiv(a.N, 64) * a.splits <= 256) return run_tile<T, OutT, 64, 64, 4>(f, a, s);
-      if (cdiv(a.M, 64) * cdiv(a.N, 128) * a.splits <= 256) return run_tile<T, OutT, 64, 128, 4>(f, a, s);
+    case kTile: {
+      auto tiles = [&](int bm, int bn) { return cdiv(a.M, bm) * cdiv(a.N, bn) * a.splits; };
+      const bool two = a.slices / a.splits >= (sizeof(OutT) == 2 ? 32 : 8);  // groups of waves
+      if (tiles(64, 64) <= 256) return two ? run_tile<T, OutT, 64, 64, 4, 2>(f, a, s) : run_tile<T, OutT, 64, 64, 4, 1>(f, a, s);
+      if (tiles(64, 128) <= 256) return two ? run_tile<T, OutT, 64, 128, 3, 2>(f, a, s) : run_tile<T, OutT, 64, 128, 4, 1>(f, a, s);
       if constexpr (sizeof(OutT) == 2)
-        if (cdiv(a.M, 128) * cdiv(a.N, 128) * a.splits <= 256) return run_tile<T, OutT, 128, 128, 4>(f, a, s);
-      return run_tile<T, OutT, 128, 128, 2>(f, a, s);
+        if (a.slices >= 16 && tiles(128, 128) <= 256) return run_tile<T, OutT, 128, 128, 2, 2>(f, a, s);
+      return run_tile<T, OutT, 128, 128, 2, 1>(f, a, s);
+    }
     default:
       if constexpr (sizeof(OutT) == 2) {
         if (f.epi.gelu_out) return run_wide<kWideGelu>(f, a, s);
