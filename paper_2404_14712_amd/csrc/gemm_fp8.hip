@@ -322,11 +322,12 @@ __global__ void __launch_bounds__(ExactCfg::NT, ExactCfg::OCC) gemm_fp8_exact_ke
 // 64 x 64 9.6, 7.2, 6.3 us (float32 results 12.4, 9.9, 8.5), 1770 x 1000 x 2056 15.2, 10.9.
 // Long K is shared by two groups of waves, whose sums meet in LDS at the end: bf16 results
 // 1024 x 1024 x 4096 12.8 -> 11.5 us, 1024 x 4096 x 4096 25.1 -> 23.6, 512 x 512 x 2048 8.0 -> 7.8,
-// but 512 x 4096 x 1536 9.2 -> 9.6 (on 128 x 128 from K = 1024: 2048 x 2048 x 1024 11.7 -> 11.2); float32 results, which have more to do on a stage, 1024 x 1024
-// x 1024 8.6 -> 8.1, 150 x 768 x 1000 7.0 -> 6.5, but 512 x 512 x 256 4.26 -> 4.58 and none on
-// 128 x 128. One group has three stages in flight (64 x 128 on two: 2048 x 1024 x 4096 22.5 us
-// against 17.3), except where two blocks share a CU (8192 x 1024 x 4096 39.2 us with two stages
-// and two blocks, 48.9 with four and one).
+// but 512 x 4096 x 1536 9.2 -> 9.6 (on 128 x 128 from K = 1024: 2048 x 2048 x 1024 11.7 -> 11.2);
+// float32 results, which have more to do on a stage, 1024 x 1024 x 1024 8.6 -> 8.1, 150 x 768 x
+// 1000 7.0 -> 6.5, but 512 x 512 x 256 4.26 -> 4.58 and none on 128 x 128. One group has three
+// stages in flight (64 x 128 on two: 2048 x 1024 x 4096 22.5 us against 17.3), except where two
+// blocks share a CU (8192 x 1024 x 4096 39.2 us with two stages and two blocks, 48.9 with four
+// and one).
 // BM x BN by KG groups of 4 waves, each with its part of K and its own ring of NS stages
 template <int BM_, int BN_, int NS, int KG>
 struct TileCfg {
