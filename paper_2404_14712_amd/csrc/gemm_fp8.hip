@@ -13,11 +13,9 @@
 // instructions keep every bit a float32 sum can, at half the rate.
 //
 // The other products go through LDS, whose rings are filled by copies without
-// registers (dma.h). Three kernels share that work:
-//   wide   256 x 256 on 4 waves, one block per CU that walks over tiles: bf16 results of
-//          192 tiles of 256 x 256 on;
-//   exact  256 x 256 on two groups of 4 waves that take turns at decoding and multiplying:
-//          float32 results of as many tiles and K of 2048 on;
+// registers (dma.h). Two kernels share that work:
+//   wide   256 x 256 on 4 waves, one block per CU that walks over tiles: more than 512 tiles
+//          of 128 x 128;
 //   tile   128 x 128, 64 x 128 or 64 x 64 on 4 waves, the smallest that leaves a block per CU,
 //          K split where there are few: the rest.
 //
@@ -71,28 +69,6 @@ ORBIT_DEV bf16x8 fp8_bf16x8(int lo, int hi, float s) {
   const bf16x2 p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
   return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
-
-// Fragments of a slice: row row0 + 32 i + (lane & 31), chunks h and h + 2 of 16 k,
-// h = lane / 32. Both operands take the same chunks, so the order of the k within
-// an instruction does not matter; all of a slice's k share a block.
-template <int NF>
-struct Fp8Frag {
-  unsigned off, x[2];
-  ORBIT_DEV void init(int row0, int lane) {
-    const int f = (lane >> 2) & 3, h = lane >> 5;
-    x[0] = (unsigned)((h ^ f) << 4);
-    x[1] = (unsigned)(((h + 2) ^ f) << 4);
-    off = (unsigned)((row0 + (lane & 31)) * 64);
-  }
-  ORBIT_DEV void read(i32x8* f, const char* S) const {
-#pragma unroll
-    for (int i = 0; i < NF; ++i) {
-      const i32x4 a = *reinterpret_cast<const i32x4*>(S + off + i * 2048 + x[0]);
-      const i32x4 b = *reinterpret_cast<const i32x4*>(S + off + i * 2048 + x[1]);
-      f[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-  }
-};
 
 // The products of a slice's fragments, ea and eb holding the rows' E in their low bytes.
 template <int TM, int TN, bool EXACT>
@@ -196,119 +172,6 @@ ORBIT_DEV void fp8_epilogue(const Fp8Args& g, f32x16 (&acc)[CF::TM][CF::TN], cha
     }
     __builtin_amdgcn_wave_barrier();
   }
-}
-
-// Float32 results of long K and many tiles. Decoding the fragments takes about as many
-// cycles as their products, so the block's two groups of waves, one wave of each per SIMD,
-// work half a slice apart: one decodes and multiplies while the other reads and copies
-// (measured against one group of 4 waves, tile kernel below: 4096 x 4096 x 8192 206 us
-// against 239, 4096 x 8192 x 2048 136 against 139, but 8192 x 8192 x 1024 182 against 166).
-using ExactCfg = DmaPP;
-constexpr int kExactE = ExactCfg::NS * ExactCfg::STB;
-constexpr int kExactLds = std::max(kExactE + 2 * (ExactCfg::BM + ExactCfg::BN) * 4, ExactCfg::EPB);
-template <typename T>
-__global__ void __launch_bounds__(ExactCfg::NT, ExactCfg::OCC) gemm_fp8_exact_kernel(Fp8Args g) {
-  using CF = ExactCfg;
-  constexpr int BM = CF::BM, BN = CF::BN, WM = CF::WM, NS = CF::NS;
-  constexpr int TM = CF::TM, TN = CF::TN, OPA = CF::OPA, STB = CF::STB;
-  using PA = DmaPlan<true, BM, CF::NW>;
-  using PB = DmaPlan<true, BN, CF::NW>;
-  constexpr int NLS = PA::NL + PB::NL;  // copies of codes per stage per wave
-  constexpr int EW = BM + BN;           // E words of 8 slices
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave % WM, wn = wave / WM;
-  int m0, n0;
-  fp8_tile<BM, BN>(g, blockIdx.x, gridDim.x, m0, n0);
-  const int nk = g.slices;
-
-  const uint8_t* Ab = g.A + (int64_t)m0 * g.lda;
-  const uint8_t* Bb = g.B + (int64_t)n0 * g.ldb;
-  const uint8_t* Aeb = g.Ae + (int64_t)m0 * g.gpa;
-  const uint8_t* Beb = g.Be + (int64_t)n0 * g.gpb;
-
-  PA pa;
-  PB pb;
-  pa.init(g.lda >> 1, m0, g.M, wave, lane);
-  pb.init(g.ldb >> 1, n0, g.N, wave, lane);
-  Fp8Frag<TM> ra;
-  Fp8Frag<TN> rb;
-  ra.init(wm * TM * 32, lane);
-  rb.init(wn * TN * 32, lane);
-
-  f32x16 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-
-  const unsigned lds0 = (unsigned)(uintptr_t)(ORBIT_LDS void*)smem;
-  auto issue = [&](int st) {
-    if ((st & 7) == 0) {
-      // E words first: they have landed when the slice's codes have
-      for (int w = wave; w < EW / 64; w += CF::NW) {
-        const bool isa = w < BM / 64;
-        const int r = (isa ? w : w - BM / 64) * 64 + lane;
-        const unsigned vo = isa ? (m0 + r < g.M ? (unsigned)(r * g.gpa) : kOobOffset)
-                                : (n0 + r < g.N ? (unsigned)(r * g.gpb) : kOobOffset);
-        dma4(buffer_rsrc((isa ? Aeb : Beb) + (st >> 1)), lds0 + kExactE + ((st >> 3) & 1) * (EW * 4) + w * 256, vo);
-      }
-    }
-    const unsigned b = lds0 + (st % NS) * STB;
-    pa.template issue<false>(reinterpret_cast<const bf16*>(Ab + st * 64), 0, DBK, b, wave, lane);
-    pb.template issue<false>(reinterpret_cast<const bf16*>(Bb + st * 64), 0, DBK, b + OPA, wave, lane);
-  };
-  int ea[TM], eb[TN];
-  auto scales = [&](int st) {
-    if ((st & 7) == 0) {
-      const int* E = reinterpret_cast<const int*>(smem + kExactE + ((st >> 3) & 1) * (EW * 4));
-#pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] = E[wm * TM * 32 + i * 32 + (lane & 31)];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = E[BM + wn * TN * 32 + j * 32 + (lane & 31)];
-    } else if ((st & 1) == 0) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] = (int)((unsigned)ea[i] >> 8);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = (int)((unsigned)eb[j] >> 8);
-    }
-  };
-  // prologue: stages 0 .. NS-2 in flight, then wait for stage 0
-#pragma unroll
-  for (int st = 0; st < NS - 1; ++st)
-    if (st < nk) issue(st);
-  wait_stage<NLS, NS>(min(nk - 1, NS - 2));
-  __syncthreads();
-
-  i32x8 fa[TM], fb[TN];
-  const int grp = wave >> 2;
-  if (grp) __builtin_amdgcn_s_barrier();
-  for (int kt = 0; kt < nk; ++kt) {
-    const char* cur = smem + (kt % NS) * STB;
-    ra.read(fa, cur);
-    rb.read(fb, cur + OPA);
-    scales(kt);
-    if (kt + NS - 1 < nk) issue(kt + NS - 1);
-    wait_stage<NLS, NS>(min(nk - kt - 2, NS - 2));
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_setprio(1);
-    mma_slice<TM, TN, true>(acc, fa, fb, ea, eb);
-    __builtin_amdgcn_s_setprio(0);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  if (!grp) __builtin_amdgcn_s_barrier();
-  wait_vmcnt<0>();
-  __syncthreads();
-
-  fp8_epilogue<T, float, CF>(g, acc, smem, wave, lane, m0, n0, 0);
 }
 
 // Tiles of 128 x 128, 64 x 128 or 64 x 64 on 4 waves. A stage is a block of 128 k: rows of
@@ -489,7 +352,7 @@ __global__ void __launch_bounds__(KG * 256, KG == 1 && NS == 2 ? 2 : 1) gemm_fp8
   fp8_epilogue<T, OutT, CF>(g, acc, shared, wave, lane, m0, n0, split);
 }
 
-// bf16 results of many tiles: 256 x 256 on 4 waves of 128 x 128, one per SIMD. A
+// Results of many tiles: 256 x 256 on 4 waves of 128 x 128, one per SIMD. A
 // fragment is then read for four products instead of two or four (half of the LDS
 // time that the MFMAs take), and a wave's own order of instructions overlaps
 // everything: after an MFMA, which takes 64 cycles, come reads of the next
@@ -510,22 +373,29 @@ __global__ void __launch_bounds__(KG * 256, KG == 1 && NS == 2 ? 2 : 1) gemm_fp8
 // have to do without a spill: one would wait for every copy and store in flight (22
 // spilled registers: 4 to 14 us a round of tiles).
 //
-// Measured: 8192 x 8192 x 8192 415 us (2650 TFLOP/s; two groups of 4 waves that take turns,
-// as in the exact kernel, 456), 4096 x 4096 x 8192 114 (121), 4096 x 8192 x 4096 109 (123),
-// 8192 x 8192 x 1024 75 (92). A stage takes 1.49 us, 2880 TFLOP/s, near what the matrix
-// cores reach on random codes at the card's power limit (3200); a round of tiles costs 9 to
-// 18 us beside its stages, of which 7 are 32 MB of results at the memory's rate: there is
-// no room in LDS or registers to let the next tile's sums begin before these are out.
+// Measured: 8192 x 8192 x 8192 415 us (2650 TFLOP/s; two groups of 4 waves of 128 x 64 that
+// take turns at reading and multiplying 456), 4096 x 4096 x 8192 112 (121), 4096 x 8192 x 4096
+// 109 (123), 8192 x 8192 x 1024 75 (92). A stage takes 1.49 us, 2880 TFLOP/s, near what the
+// matrix cores reach on random codes at the card's power limit (3200); a round of tiles costs
+// 9 to 18 us beside its stages, of which 7 are 32 MB of results at the memory's rate: there
+// is no room in LDS or registers to let the next tile's sums begin before these are out.
+//
+// Float32 results take four bf16 instructions of 32 cycles for one of 64, and a wave has
+// time to decode between them: 8192 x 8192 x 8192 775 us (1420 TFLOP/s), 4096 x 4096 x 8192
+// 200, 8192 x 8192 x 2048 227, 8192 x 4096 x 4096 207 (two groups of 4 waves, one decoding and
+// multiplying while the other reads: 810, 212, 272, 229; a bf16 library product of the first
+// 859), and 8192 x 8192 x 1024 142 (tiles of 128 x 128: 168).
 constexpr int kWideStage = 2 * 256 * 128;
 constexpr int kWideE = 2 * kWideStage, kWideBias = kWideE + 2 * 512 * 4, kWideOut = kWideBias + 2 * 1024;
 constexpr int kWidePitch = 272, kWideLds = kWideOut + 4 * 16 * kWidePitch;  // 16 rows of 128 bf16 per wave
 static_assert(kWideLds <= 160 * 1024, "LDS");
 
 // what happens to a sum (with its bias) before it is stored
-enum WideEpi { kWidePlain, kWideGelu, kWideGeluGrad, kWideRes };
+enum WideEpi { kWidePlain, kWideGelu, kWideGeluGrad, kWideRes, kWideF32 };
 
-template <WideEpi EPI>
+template <typename T, WideEpi EPI>
 __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
+  constexpr bool EXACT = EPI == kWideF32;
   constexpr int OPA = 256 * 128;  // bytes of A in a stage
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -636,7 +506,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  copy_bias(cur, 0);
+  if constexpr (!EXACT) copy_bias(cur, 0);
   copy_e(0);
   {
     const Src s = source(0);
@@ -662,7 +532,23 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
     }
     // the sums begin with the bias: lane l holds columns 8 q + 4 (l >> 5) .. +3
     f32x16 acc[4][4];
-    {
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = cur.n0 + wn * 128 + j * 32 + q * 8 + (lane >> 5) * 4;
+          float b[4] = {0.f, 0.f, 0.f, 0.f};
+          if (g.epi.bias && c < g.N) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = to_f(static_cast<const T*>(g.epi.bias)[c + e]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = b[e];
+        }
+    } else {
       const char* bias = smem + kWideBias + bpar * 1024 + (wn * 128 + (lane >> 5) * 4) * 2;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -678,11 +564,30 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
           }
         }
     }
-    copy_bias(nxt, bpar ^ 1);
-    auto product = [&](const Set& s, int m) {
-      const int i = m / 4, j = m % 4;
-      // B's rows first: a lane then holds four consecutive columns of a row of C
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(s.f[4 + j], s.f[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+    if constexpr (!EXACT) copy_bias(nxt, bpar ^ 1);
+    // a half stage's products in 16 steps. The 8-bit instruction takes a tile's 64 k at
+    // once; decoded, a step is 16 k of four tiles (row i), while the next 16 k of two
+    // fragments are decoded, at the end those of the stage's other half.
+    bf16x8 dec[2][8];
+    float sc[8];
+    auto decode = [&](const Set& s, int k, int f) {
+      dec[k & 1][f] = fp8_bf16x8(s.f[f][2 * (k & 3)], s.f[f][2 * (k & 3) + 1], sc[f]);
+    };
+    auto product = [&](const Set& s, const Set* after, int m) {
+      if constexpr (EXACT) {
+        const int k = m >> 2, i = m & 3;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dec[k & 1][4 + j], dec[k & 1][i], acc[i][j], 0, 0, 0);
+        if (k < 3 || after) {
+          decode(k < 3 ? s : *after, k + 1, 2 * i);
+          decode(k < 3 ? s : *after, k + 1, 2 * i + 1);
+        }
+      } else {
+        const int i = m / 4, j = m % 4;
+        // B's rows first: a lane then holds four consecutive columns of a row of C
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(s.f[4 + j], s.f[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+      }
     };
     int t = 0;
 #pragma unroll 1
@@ -699,6 +604,13 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
         }
       }
       const Src s = source(t + 2);
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+          sc[f] = fp8_scale(f < 4 ? ea[f] : eb[f - 4]);
+          decode(X, 0, f);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < 16; ++m) {
@@ -707,7 +619,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           meet();
         }
-        product(X, m);
+        product(X, &Y, m);
         if (m < 8) {
           read(Y, here, 1, m, 0);
           read(Y, here, 1, m, 1);
@@ -721,7 +633,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
       copy_e(t + 2);
 #pragma unroll
       for (int m = 0; m < 16; ++m) {
-        product(Y, m);
+        product(Y, nullptr, m);
         if (m < 8) {
           read(X, then, 0, m, 0);
           read(X, then, 0, m, 1);
@@ -739,13 +651,14 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
     const int mw = cur.m0 + wm * 128, nc = cur.n0 + wn * 128;
     // rows mw + 32 i .. of a matrix from column nc: offsets behind the last row are out of
     // bounds, which reads zeros and stores nothing
+    constexpr int ES = EXACT ? 4 : 2;
     auto matrix = [&](const void* D, int64_t ld, int i) {
       const int mr = mw + i * 32;
-      const uint64_t p = (uint64_t)(uintptr_t)(static_cast<const bf16*>(D) + (int64_t)mr * ld + nc);
+      const uint64_t p = (uint64_t)(uintptr_t)(static_cast<const char*>(D) + ((int64_t)mr * ld + nc) * ES);
       // (uniform, as the compiler does not see)
       const unsigned lo = __builtin_amdgcn_readfirstlane((int)p), hi = __builtin_amdgcn_readfirstlane((int)(p >> 32));
       return buffer_rsrc(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo),
-                         __builtin_amdgcn_readfirstlane(max(min(g.M - mr, 32), 0) * (int)ld * 2));
+                         __builtin_amdgcn_readfirstlane(max(min(g.M - mr, 32), 0) * (int)ld * ES));
     };
     auto leave = [&](void* D, int64_t ld, int i, const U128* q) {
       const __amdgpu_buffer_rsrc_t to = matrix(D, ld, i);
@@ -780,11 +693,45 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
         }
       }
     };
+    // float32 results: a lane's fours as they are, 8 rows at a time, in runs of 512 bytes
+    auto leave_f32 = [&](auto at) {
+      constexpr int i = decltype(at)::value;
+      constexpr int pitch = 528;
+      static_assert(4 * 8 * pitch <= kWideLds - kWideOut, "LDS");
+      const __amdgpu_buffer_rsrc_t to = matrix(g.C, g.ldc, i);
+      char* o = smem + kWideOut + wave * 8 * pitch;
+      const unsigned col = nc + (lane & 31) * 4 < g.N ? (unsigned)((lane >> 5) * (int)g.ldc * 4 + (lane & 31) * 16) : kOobOffset;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        if ((lr >> 3) == h) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<f32x4*>(o + (lr & 7) * pitch + (j * 32 + q * 8 + (lane >> 5) * 4) * 4) =
+                  f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          f32x4 v = *reinterpret_cast<const f32x4*>(o + (it * 2 + (lane >> 5)) * pitch + (lane & 31) * 16);
+          const unsigned off = col + (unsigned)((h * 8 + it * 2) * 4 * (int)g.ldc);
+          if (g.epi.accumulate) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(to, off, 0, 0));
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, off, 0, 0);
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    };
     auto rows = [&](auto at) {
       constexpr int i = decltype(at)::value;
       // (from here on, not before: moved up, these rows' sums would not fit the registers)
 #pragma unroll
       for (int j = 0; j < 4; ++j) asm volatile("" : "+a"(acc[i][j]));
+      if constexpr (EXACT) {
+        leave_f32(at);
+        __builtin_amdgcn_sched_barrier(0);
+        return;
+      }
       U128 q[8];
       // the sums as they are, rounded before the halves swap: half the swaps
       auto sums = [&] {
@@ -924,7 +871,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) fp8_thin_kernel(Fp8Args g) {
   }
 }
 
-enum Fp8Tile { kThin, kTile, kFull };
+enum Fp8Tile { kThin, kTile, kWide };
 struct Fp8Choice { Fp8Tile tile; int splits; };
 
 Fp8Choice pick_fp8(int M, int N, int K, bool out_f32) {
@@ -940,9 +887,11 @@ Fp8Choice pick_fp8(int M, int N, int K, bool out_f32) {
     while (slices >= 128 && sp < 16 && cdiv(N, 16) * sp < 256 && slices / (2 * sp) >= 32) sp *= 2;
     return {kThin, sp};
   }
-  const int64_t t256 = cdiv(M, 256) * cdiv(N, 256);
-  // (wide: two stages at least; exact: see there)
-  if (t256 >= 192 && slices >= (out_f32 ? 32 : 4)) return {kFull, 1};
+  // Wide, with two stages at least, where tiles of 128 x 128, two to a CU, would take a second
+  // round (in us, against those: 4608 x 2048 x 4096 44.9 and 58.0, float32 results 87.2 and 89.5;
+  // 5632 x 2048 x 1024 19.0 and 23.4, float32 34.5 and 34.4), but not
+  // where they fit one (8192 x 1024 x 4096 47.3 and 40.2, 2048 x 3584 x 4096 45.2 and 36.4).
+  if (cdiv(M, 128) * cdiv(N, 128) > 512 && slices >= 4) return {kWide, 1};
   // Split K saves slices, of 0.135 us each (float32 results: 0.233), and costs the second
   // launch, 3.5 us, and writing and reading the partial sums, 0.7 us per MB of them: 100 x 512 x
   // 8192 10.9 us in 8 parts and 20.7 in one, 512 x 1024 x 4096 14.2 in 4 and 12.2 in one. Only
@@ -956,21 +905,6 @@ Fp8Choice pick_fp8(int M, int N, int K, bool out_f32) {
     if (t < best) { best = t; c.splits = sp; }
   }
   return c;
-}
-
-template <typename T>
-orbit_status run_exact(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
-  KernelInfo ki{"gemm_fp8_exact", 2.0 * f.M * f.N * (double)f.K,
-                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + 4.0 * f.M * f.N};
-  static const bool attr = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_exact_kernel<T>),
-                              hipFuncAttributeMaxDynamicSharedMemorySize, kExactLds);
-    (void)hipGetLastError();
-    return true;
-  }();
-  (void)attr;
-  const dim3 grid((unsigned)(cdiv(a.M, ExactCfg::BM) * cdiv(a.N, ExactCfg::BN)));
-  return launch(ki, gemm_fp8_exact_kernel<T>, grid, dim3(ExactCfg::NT), (size_t)kExactLds, s, a);
 }
 
 template <typename T, typename OutT, int BM, int BN, int NS, int KG>
@@ -989,19 +923,19 @@ orbit_status run_tile(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
   return launch(ki, gemm_fp8_tile_kernel<T, OutT, BM, BN, NS, KG>, grid, dim3(KG * 256), (size_t)lds, s, a);
 }
 
-template <WideEpi EPI>
+template <typename T, WideEpi EPI>
 orbit_status run_wide(const Fp8Gemm& f, const Fp8Args& a, hipStream_t s) {
-  KernelInfo ki{"gemm_fp8_wide", 2.0 * f.M * f.N * (double)f.K,
-                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + 2.0 * f.M * f.N};
+  KernelInfo ki{EPI == kWideF32 ? "gemm_fp8_wide<f32>" : "gemm_fp8_wide<bf16>", 2.0 * f.M * f.N * (double)f.K,
+                ((double)f.M + f.N) * f.K * (1.0 + 1.0 / kFp8Block) + (EPI == kWideF32 ? 4.0 : 2.0) * f.M * f.N};
   static const bool attr = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_wide_kernel<EPI>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_wide_kernel<T, EPI>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, kWideLds);
     (void)hipGetLastError();
     return true;
   }();
   (void)attr;
   const dim3 grid((unsigned)std::min<int64_t>(cdiv(a.M, 256) * cdiv(a.N, 256), 256));
-  return launch(ki, gemm_fp8_wide_kernel<EPI>, grid, dim3(256), (size_t)kWideLds, s, a);
+  return launch(ki, gemm_fp8_wide_kernel<T, EPI>, grid, dim3(256), (size_t)kWideLds, s, a);
 }
 
 template <typename T, typename OutT>
@@ -1028,11 +962,11 @@ orbit_status run_typed8(const Fp8Gemm& f, const Fp8Args& a, Fp8Tile t, hipStream
     }
     default:
       if constexpr (sizeof(OutT) == 2) {
-        if (f.epi.gelu_out) return run_wide<kWideGelu>(f, a, s);
-        if (f.epi.gelu_in) return run_wide<kWideGeluGrad>(f, a, s);
-        return f.epi.res ? run_wide<kWideRes>(f, a, s) : run_wide<kWidePlain>(f, a, s);
+        if (f.epi.gelu_out) return run_wide<bf16, kWideGelu>(f, a, s);
+        if (f.epi.gelu_in) return run_wide<bf16, kWideGeluGrad>(f, a, s);
+        return f.epi.res ? run_wide<bf16, kWideRes>(f, a, s) : run_wide<bf16, kWidePlain>(f, a, s);
       } else {
-        return run_exact<T>(f, a, s);
+        return run_wide<T, kWideF32>(f, a, s);
       }
   }
 }
@@ -1047,7 +981,7 @@ size_t fp8_gemm_workspace_bytes(int M, int N, int K) {
 orbit_status fp8_gemm(const Fp8Gemm& f, void* ws, size_t ws_bytes, hipStream_t s) {
   Fp8Choice c = pick_fp8(f.M, f.N, f.K, f.out_f32 || f.dtype == ORBIT_F32);
   // the wide kernel's 32 rows of results lie within 31-bit offsets
-  if (c.tile == kFull && !f.out_f32 && f.ldc >= (1 << 24)) c.tile = kTile;
+  if (c.tile == kWide && f.ldc >= (1 << 24)) c.tile = kTile;
   Fp8Args a{};
   a.A = static_cast<const uint8_t*>(f.A); a.Ae = a.A + fp8_exp_offset(f.M, f.K);
   a.B = static_cast<const uint8_t*>(f.B); a.Be = a.B + fp8_exp_offset(f.N, f.K);

@@ -179,7 +179,7 @@ def test_gemm(lib, M, N, K, form):
 
 @pytest.mark.parametrize("form", ["bf16", "bf16-f32", "f32"])
 @pytest.mark.parametrize("M,N,K", [(16, 264, 1024), (16, 136, 4200), (24, 4104, 260), (30, 72, 2048), (30, 72, 2049), (32, 4096, 130),
-                                   (9, 8200, 512), (3, 1032, 9000), (700, 1400, 520), (1030, 1032, 513), (130, 72, 260)])
+                                   (9, 8200, 512), (3, 1032, 9000), (700, 1400, 520), (1030, 1032, 513), (2000, 4200, 300), (130, 72, 260)])
 def test_gemm_kernels(lib, M, N, K, form):
     """As above, at the sizes where one kernel, tile or number of parts gives way to another."""
     test_gemm(lib, M, N, K, form)
