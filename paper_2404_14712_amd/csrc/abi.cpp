@@ -313,7 +313,7 @@ orbit_status block_linear(const BlockDims& z, const char* tag, const void* x, in
                           const void* bias, void* xt, void* y, int out, const void* res, void* gelu_out,
                           const BlockWs& ws, hipStream_t s) {
   if (z.fp8) {
-    ORBIT_TRY(fp8_pack(z.dt, x, in, z.T, in, false, ws.q8, xt, nullptr, s));
+    ORBIT_TRY(fp8_pack(z.dt, x, in, z.T, in, false, ws.q8, xt, true, nullptr, s));
     Fp8Gemm g; g.dtype = z.dt; g.tag = tag;
     g.A = ws.q8; g.B = w8t; g.C = y; g.ldc = out; g.M = (int)z.T; g.N = out; g.K = in;
     g.epi.bias = bias; g.epi.res = res; g.epi.ldr = out; g.epi.gelu_out = gelu_out; g.epi.ldgo = out;
@@ -372,7 +372,7 @@ orbit_status block_forward_steps(const BlockDims& z, const BlockExt& ext, const 
     ORBIT_TRY(block_linear(z, "fc2", sv.g, z.F, p->w_fc2, z.w8.w_fc2_t, p->b_fc2, sv.gt, ext.normed() ? f2 : y, z.d,
                            ext.normed() ? nullptr : sv.x1, nullptr, w, s));
   else if (z.fp8)  // the backward reads its input's store
-    ORBIT_TRY(fp8_pack(dt, sv.g, z.F, T, z.F, false, nullptr, sv.gt, nullptr, s));
+    ORBIT_TRY(fp8_pack(dt, sv.g, z.F, T, z.F, false, nullptr, sv.gt, false, nullptr, s));
   // the recompute runs this norm too where the backward reads its statistics;
   // its output then goes to an idle buffer
   if (ext.normed() && (y || ext.post))
@@ -720,7 +720,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   // orientations, and leaves its column sums (the bias gradient) where part is given
   auto linear8 = [&](const char* tag_dx, const char* tag_dw, const void* g_out, int out, const void* xt, int in,
                      const void* w8, void* g_in, const void* gelu_in, float* dw, float* part, float* db) -> orbit_status {
-    ORBIT_TRY(fp8_pack(dt, g_out, out, T, out, false, w.q8, w.q8t, part, s));
+    ORBIT_TRY(fp8_pack(dt, g_out, out, T, out, false, w.q8, w.q8t, false, part, s));
     if (part) fin.add(part, out, (int)cdiv(T, 128), out, db);
     Fp8Gemm g; g.dtype = dt; g.tag = tag_dw;
     g.A = xt; g.B = w.q8t; g.C = dw; g.ldc = out; g.M = in; g.N = out; g.K = T; g.out_f32 = true;

@@ -98,7 +98,7 @@ orbit_status orbit_fp8_pack(int32_t dtype, int64_t rows, int64_t n, int32_t tile
   PTR(x, "x");
   REQ(ldx >= n && ldx % 8 == 0, ORBIT_E_ARG, "%s: ldx must be >= n and a multiple of 8", fn);
   REQ(store != store_t && x != store && x != store_t, ORBIT_E_ARG, "%s: x and the stores must not alias", fn);
-  return fp8_pack((orbit_dtype)dtype, x, ldx, rows, n, tile_rows == 128, store, store_t, nullptr, S(stream));
+  return fp8_pack((orbit_dtype)dtype, x, ldx, rows, n, tile_rows == 128, store, store_t, false, nullptr, S(stream));
 }
 
 orbit_status orbit_fp8_unpack(int32_t dtype, int64_t rows, int64_t n, const void* store, size_t store_bytes, void* x,
@@ -170,7 +170,7 @@ orbit_status orbit_fp8_linear_fwd(const orbit_fp8_linear_desc* desc, const void*
   REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes, need);
   hipStream_t s = S(stream);
   const orbit_dtype dt = (orbit_dtype)d.dtype;
-  ORBIT_TRY(fp8_pack(dt, x, ldx, d.rows, d.in, false, w.q, saved, nullptr, s));
+  ORBIT_TRY(fp8_pack(dt, x, ldx, d.rows, d.in, false, w.q, saved, true, nullptr, s));
   Fp8Gemm g;
   g.dtype = dt; g.tag = "linear";
   g.A = w.q; g.B = w_t; g.C = y; g.ldc = ldy; g.M = d.rows; g.N = d.out; g.K = d.in; g.epi.bias = bias;
@@ -195,7 +195,7 @@ orbit_status orbit_fp8_linear_bwd(const orbit_fp8_linear_desc* desc, const void*
   REQ(ws_bytes >= need, ORBIT_E_ARG, "%s: workspace of %zu bytes is smaller than the %zu required", fn, ws_bytes, need);
   hipStream_t s = S(stream);
   const orbit_dtype dt = (orbit_dtype)d.dtype;
-  ORBIT_TRY(fp8_pack(dt, dy, lddy, d.rows, d.out, false, dx ? t.q : nullptr, t.qt, db ? t.part : nullptr, s));
+  ORBIT_TRY(fp8_pack(dt, dy, lddy, d.rows, d.out, false, dx ? t.q : nullptr, t.qt, false, db ? t.part : nullptr, s));
   if (dx) {
     Fp8Gemm g;
     g.dtype = dt; g.tag = "linear_dx";

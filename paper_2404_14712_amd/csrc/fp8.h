@@ -73,9 +73,9 @@ ORBIT_DEV void fp8_decode8(uint2 q, uint32_t e, float* f) {
 // x[rows, n] -> its store and / or its transposed one ([n, rows], blocks along the
 // rows; either may be null). tiled: 128 x 128 tiles share their E. part (may be
 // null; not with tiles, and with store_t): float32 column sums of x, one row of n
-// per 128 rows.
+// per 128 rows. later: store_t is for another pass (so are the stores of tiles).
 orbit_status fp8_pack(orbit_dtype dt, const void* x, int64_t ldx, int64_t rows, int64_t n, bool tiled, void* store,
-                      void* store_t, float* part, hipStream_t s);
+                      void* store_t, bool later, float* part, hipStream_t s);
 orbit_status fp8_unpack(orbit_dtype dt, const void* store, int64_t rows, int64_t n, void* x, int64_t ldx,
                         hipStream_t s);
 

@@ -129,7 +129,11 @@ template <> struct PackTile<float> {
 // floats, with clamps and tests on every value, it took 47. Tiles walked down the
 // columns instead of along the rows: 38.9 against 36.5 us before the loads were
 // streamed; a contiguous share of them for each XCD: 43.5.
-template <typename T, bool TILED, bool ROWS, bool COLS, bool SUM>
+// LATER: the transposed codes pass the caches, which leaves the room to what is read next
+// (the forward of a 1B block with 8-bit products 415 -> 407 us; the weights' stores of a
+// 113B block 196 -> 175); read at once they would come from memory (4096 x 8192, packed and
+// read back: 63 -> 67 us).
+template <typename T, bool TILED, bool ROWS, bool COLS, bool SUM, bool LATER>
 __global__ void __launch_bounds__(256) fp8_pack_kernel(PackArgs a) {
   using Z = PackTile<T>;
   constexpr int P = 136;  // pitch of a column's 128 codes in LDS
@@ -294,7 +298,9 @@ __global__ void __launch_bounds__(256) fp8_pack_kernel(PackArgs a) {
       if (c < cols) {
         const uint2 lo = *reinterpret_cast<const uint2*>(tt + c * P + k);
         const uint2 hi = *reinterpret_cast<const uint2*>(tt + c * P + k + 8);
-        *reinterpret_cast<uint4*>(a.codes_t + (c0 + c) * a.wide_t + r0 + k) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        u32v4* to = reinterpret_cast<u32v4*>(a.codes_t + (c0 + c) * a.wide_t + r0 + k);
+        if constexpr (LATER) __builtin_nontemporal_store(u32v4{lo.x, lo.y, hi.x, hi.y}, to);
+        else *to = u32v4{lo.x, lo.y, hi.x, hi.y};
       }
     }
   }
@@ -328,22 +334,27 @@ __global__ void __launch_bounds__(256) fp8_unpack_kernel(UnpackArgs a) {
   }
 }
 
-template <typename T, bool TILED>
+template <typename T, bool TILED, bool LATER>
 orbit_status pack_t(const KernelInfo& ki, const PackArgs& a, dim3 grid, hipStream_t s) {
   const dim3 block(256);
-  if constexpr (!TILED) {  // sums are those of output gradients, packed in rows
-    if (a.part && a.codes) return launch(ki, fp8_pack_kernel<T, false, true, true, true>, grid, block, 0, s, a);
-    if (a.part) return launch(ki, fp8_pack_kernel<T, false, false, true, true>, grid, block, 0, s, a);
+  if constexpr (!LATER) {  // sums are those of output gradients, packed in rows for this pass
+    if (a.part && a.codes) return launch(ki, fp8_pack_kernel<T, false, true, true, true, false>, grid, block, 0, s, a);
+    if (a.part) return launch(ki, fp8_pack_kernel<T, false, false, true, true, false>, grid, block, 0, s, a);
   }
-  if (a.codes && a.codes_t) return launch(ki, fp8_pack_kernel<T, TILED, true, true, false>, grid, block, 0, s, a);
-  if (a.codes) return launch(ki, fp8_pack_kernel<T, TILED, true, false, false>, grid, block, 0, s, a);
-  return launch(ki, fp8_pack_kernel<T, TILED, false, true, false>, grid, block, 0, s, a);
+  if (a.codes && a.codes_t) return launch(ki, fp8_pack_kernel<T, TILED, true, true, false, LATER>, grid, block, 0, s, a);
+  if (a.codes) return launch(ki, fp8_pack_kernel<T, TILED, true, false, false, LATER>, grid, block, 0, s, a);
+  return launch(ki, fp8_pack_kernel<T, TILED, false, true, false, LATER>, grid, block, 0, s, a);
+}
+template <typename T>
+orbit_status pack_pick(const KernelInfo& ki, const PackArgs& a, dim3 grid, bool tiled, bool later, hipStream_t s) {
+  if (tiled) return pack_t<T, true, true>(ki, a, grid, s);
+  return later ? pack_t<T, false, true>(ki, a, grid, s) : pack_t<T, false, false>(ki, a, grid, s);
 }
 
 }  // namespace
 
 orbit_status fp8_pack(orbit_dtype dt, const void* x, int64_t ldx, int64_t rows, int64_t n, bool tiled, void* store,
-                      void* store_t, float* part, hipStream_t s) {
+                      void* store_t, bool later, float* part, hipStream_t s) {
   PackArgs a{};
   a.x = x; a.ldx = ldx; a.rows = rows; a.n = n; a.part = part;
   a.wide = fp8_wide(n); a.groups = fp8_groups(n);
@@ -364,8 +375,7 @@ orbit_status fp8_pack(orbit_dtype dt, const void* x, int64_t ldx, int64_t rows, 
   // orientations: 36.5 -> 31.0 us)
   a.stream = ki.bytes >= 96e6;
   const dim3 grid(a.tiles_m * a.tiles_n);
-  if (dt == ORBIT_BF16) return tiled ? pack_t<bf16, true>(ki, a, grid, s) : pack_t<bf16, false>(ki, a, grid, s);
-  return tiled ? pack_t<float, true>(ki, a, grid, s) : pack_t<float, false>(ki, a, grid, s);
+  return dt == ORBIT_BF16 ? pack_pick<bf16>(ki, a, grid, tiled, later, s) : pack_pick<float>(ki, a, grid, tiled, later, s);
 }
 
 orbit_status fp8_unpack(orbit_dtype dt, const void* store, int64_t rows, int64_t n, void* x, int64_t ldx,

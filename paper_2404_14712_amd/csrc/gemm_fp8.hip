@@ -647,6 +647,12 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
     // such fours, so that a lane has 8 consecutive columns; rounded to bf16 they pass
     // through the wave's LDS, 16 rows at a time, and leave as runs of 256 bytes (runs of
     // 128 take the memory half as long again).
+    //
+    // Stores that nothing reads soon pass the caches, which keep the operands of tiles still
+    // to come: 4096 x 4096 x 8192 113 -> 104 us, 8192 x 8192 x 1024 78 -> 75, float32 results
+    // 8192 x 4096 x 4096 209 -> 202. The next kernel of a block reads what GELU' and the residual
+    // leave and GELU's value (a 115M block's backward: 900 us, and 917 with all past the caches).
+    constexpr int kStream = 2;
     char* out = smem + kWideOut + wave * 16 * kWidePitch;
     const int mw = cur.m0 + wm * 128, nc = cur.n0 + wn * 128;
     // rows mw + 32 i .. of a matrix from column nc: offsets behind the last row are out of
@@ -660,7 +666,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
       return buffer_rsrc(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo),
                          __builtin_amdgcn_readfirstlane(max(min(g.M - mr, 32), 0) * (int)ld * ES));
     };
-    auto leave = [&](void* D, int64_t ld, int i, const U128* q) {
+    auto leave = [&](void* D, int64_t ld, int i, const U128* q, auto aux) {
       const __amdgpu_buffer_rsrc_t to = matrix(D, ld, i);
       const unsigned at = nc + (lane & 15) * 8 < g.N ? (unsigned)((lane >> 4) * (int)ld * 2 + (lane & 15) * 16) : kOobOffset;
 #pragma unroll
@@ -673,7 +679,8 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
           const u32x4 v = *reinterpret_cast<const u32x4*>(out + (it * 4 + (lane >> 4)) * kWidePitch + (lane & 15) * 16);
-          __builtin_amdgcn_raw_buffer_store_b128(v, to, at + (unsigned)((h * 16 + it * 4) * 2 * (int)ld), 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(v, to, at + (unsigned)((h * 16 + it * 4) * 2 * (int)ld), 0,
+                                                 decltype(aux)::value);
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -717,7 +724,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
           f32x4 v = *reinterpret_cast<const f32x4*>(o + (it * 2 + (lane >> 5)) * pitch + (lane & 31) * 16);
           const unsigned off = col + (unsigned)((h * 8 + it * 2) * 4 * (int)g.ldc);
           if (g.epi.accumulate) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(to, off, 0, 0));
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, off, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, off, 0, kStream);
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -749,7 +756,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
       } else {
         if constexpr (EPI == kWideGelu) {
           sums();
-          leave(g.epi.gelu_out, g.epi.ldgo, i, q);
+          leave(g.epi.gelu_out, g.epi.ldgo, i, q, std::integral_constant<int, kStream>{});
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -771,7 +778,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_wide_kernel(Fp8Args g) {
         if constexpr (i < 3) fetch(std::integral_constant<int, i + 1>{});
         __builtin_amdgcn_sched_barrier(0);
       }
-      leave(g.C, g.ldc, i, q);
+      leave(g.C, g.ldc, i, q, std::integral_constant<int, EPI == kWidePlain ? kStream : 0>{});
       __builtin_amdgcn_sched_barrier(0);
     };
     fetch(std::integral_constant<int, 0>{});
