@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(KG * 256, KG == 1 && NS == 2 ? 2 : 1) gemm_fp8
 // spilled registers: 4 to 14 us a round of tiles).
 //
 // Measured: 8192 x 8192 x 8192 415 us (2650 TFLOP/s; two groups of 4 waves of 128 x 64 that
-// take turns at reading and multiplying 456), 4096 x 4096 x 8192 112 (121), 4096 x 8192 x 4096
+// take turns at reading and multiplying 456), 4096 x 4096 x 8192 104 (121), 4096 x 8192 x 4096
 // 109 (123), 8192 x 8192 x 1024 75 (92). A stage takes 1.49 us, 2880 TFLOP/s, near what the
 // matrix cores reach on random codes at the card's power limit (3200); a round of tiles costs
 // 9 to 18 us beside its stages, of which 7 are 32 MB of results at the memory's rate: there
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(KG * 256, KG == 1 && NS == 2 ? 2 : 1) gemm_fp8
 //
 // Float32 results take four bf16 instructions of 32 cycles for one of 64, and a wave has
 // time to decode between them: 8192 x 8192 x 8192 775 us (1420 TFLOP/s), 4096 x 4096 x 8192
-// 200, 8192 x 8192 x 2048 227, 8192 x 4096 x 4096 207 (two groups of 4 waves, one decoding and
+// 200, 8192 x 8192 x 2048 227, 8192 x 4096 x 4096 202 (two groups of 4 waves, one decoding and
 // multiplying while the other reads: 810, 212, 272, 229; a bf16 library product of the first
 // 859), and 8192 x 8192 x 1024 142 (tiles of 128 x 128: 168).
 constexpr int kWideStage = 2 * 256 * 128;
