@@ -423,3 +423,69 @@ def test_products_on_two_streams(lib):
     torch.cuda.synchronize()
     for r in runs:
         assert torch.equal(r[4][0], r[4][1]) and torch.equal(r[4][0], r[4][2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_full_size_float32_results(lib, dtype):
+    """Products of many tiles with a bias, onto what was there, with gaps between rows; a NaN stays in its row and an
+    infinity's in its column, bit for bit."""
+    M, N, K, ldc = 2950, 2840, 700, 2856
+    code = R.CODE[dtype]
+    x, w = _data(M, K, dtype, 1), _data(N, K, dtype, 2)
+    bias, c0 = _data(1, N, dtype, 3), _data(M, ldc, "f32", 4)
+    va, vb = F.values(x.double()).cuda(), F.values(w.double()).cuda()
+    ref, s = va @ vb.t(), va.abs() @ vb.abs().t()
+    ref, s = ref + bias.double().cuda() + c0[:, :N].double().cuda(), s + bias.abs().double().cuda() + c0[:, :N].abs().double().cuda()
+    ws = _bytes(lib.orbit_fp8_gemm_workspace_bytes(M, N, K))
+    out = []
+    for spoil in (False, True):
+        if spoil:
+            x[1234, 5], w[2000, 7] = float("nan"), float("inf")
+        (a, _), (b, _) = _pack(lib, x), _pack(lib, w)
+        C = c0.cuda()
+        lib.orbit_fp8_gemm(code, M, N, K, a, b, C, ldc, 1, bias.cuda(), 1, ws)
+        assert torch.equal(C[:, N:].cpu(), c0[:, N:])
+        out.append(C[:, :N])
+    clean, spoilt = out
+    assert ((clean.double() - ref).abs() <= (K + 32) * F.U32 * s).all()
+    hit = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    hit[1234], hit[:, 2000] = True, True
+    assert torch.isnan(spoilt[hit]).all() and torch.equal(spoilt[~hit], clean[~hit])
+
+
+def test_full_size_non_finite(lib):
+    """The same for bf16 results."""
+    M, N, K = 2950, 2840, 260
+    x, w = _data(M, K, "bf16", 1), _data(N, K, "bf16", 2)
+    ws = _bytes(lib.orbit_fp8_gemm_workspace_bytes(M, N, K))
+    out = []
+    for spoil in (False, True):
+        if spoil:
+            x[2949, 5], w[0, 259] = float("-inf"), float("nan")
+        (a, _), (b, _) = _pack(lib, x), _pack(lib, w)
+        C = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+        lib.orbit_fp8_gemm(1, M, N, K, a, b, C, N, 0, None, 0, ws)
+        out.append(C)
+    hit = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    hit[2949], hit[:, 0] = True, True
+    assert torch.isnan(out[1][hit]).all() and torch.equal(out[1][~hit], out[0][~hit]) and torch.isfinite(out[0]).all()
+
+
+@pytest.mark.parametrize("f32", [0, 1])
+def test_rows_of_results_far_apart(lib, f32):
+    """130 x 33000, wide enough for the large tiles, whole and with rows 2^24 apart, where offsets pass 31 bits."""
+    M, N, K, ldc = 130, 33000, 300, 1 << 24
+    (a, _), (b, _) = _pack(lib, _data(M, K, "bf16", 1)), _pack(lib, _data(N, K, "bf16", 2))
+    t = torch.float32 if f32 else torch.bfloat16
+    ws = _bytes(lib.orbit_fp8_gemm_workspace_bytes(M, N, K))
+    C, D = torch.empty(M, N, dtype=t, device="cuda"), torch.zeros(M, ldc, dtype=t, device="cuda")
+    lib.orbit_fp8_gemm(1, M, N, K, a, b, C, N, f32, None, 0, ws)
+    lib.orbit_fp8_gemm(1, M, N, K, a, b, D, ldc, f32, None, 0, ws)
+    va, vb = torch.zeros(M, 304, device="cuda"), torch.zeros(N, 304, device="cuda")
+    lib.orbit_fp8_unpack(0, M, K, a, va, 304)
+    lib.orbit_fp8_unpack(0, N, K, b, vb, 304)
+    ref = va.double() @ vb.double().t()
+    bound = 2.0 ** -22 if f32 else F.HALF["bf16"]
+    for R_ in (C, D[:, :N]):
+        assert float((R_.double() - ref).norm() / ref.norm()) < bound
+    assert not D[:, N:].any()
