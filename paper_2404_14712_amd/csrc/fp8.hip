@@ -342,8 +342,10 @@ orbit_status pack_t(const KernelInfo& ki, const PackArgs& a, dim3 grid, hipStrea
     if (a.part) return launch(ki, fp8_pack_kernel<T, false, false, true, true, false>, grid, block, 0, s, a);
   }
   if (a.codes && a.codes_t) return launch(ki, fp8_pack_kernel<T, TILED, true, true, false, LATER>, grid, block, 0, s, a);
-  if (a.codes) return launch(ki, fp8_pack_kernel<T, TILED, true, false, false, LATER>, grid, block, 0, s, a);
-  return launch(ki, fp8_pack_kernel<T, TILED, false, true, false, LATER>, grid, block, 0, s, a);
+  if constexpr (TILED || !LATER) {  // the forward's later store comes with the other
+    if (!a.codes) return launch(ki, fp8_pack_kernel<T, TILED, false, true, false, LATER>, grid, block, 0, s, a);
+  }
+  return launch(ki, fp8_pack_kernel<T, TILED, true, false, false, false>, grid, block, 0, s, a);
 }
 template <typename T>
 orbit_status pack_pick(const KernelInfo& ki, const PackArgs& a, dim3 grid, bool tiled, bool later, hipStream_t s) {
