@@ -896,6 +896,17 @@ __global__ void __launch_bounds__(kThinWaves * 64) fp8_thin_kernel(Fp8Args g) {
 enum Fp8Tile { kThin, kTile, kWide };
 struct Fp8Choice { Fp8Tile tile; int splits; };
 
+// What the wide kernel's end has: of GELU with its input kept, GELU' and the residual one,
+// with bf16 results, or onto what is there with float32 ones; 32 rows within 31-bit offsets.
+// The other kernels end in epi_apply, which has everything.
+bool wide_has(const Fp8Gemm& f, bool out_f32) {
+  const Epi& e = f.epi;
+  const int fused = (e.gelu_out ? 1 : 0) + (e.gelu_in ? 1 : 0) + (e.res ? 1 : 0);
+  const auto near = [](const void* p, int64_t ld) { return !p || ld < (1 << 24); };
+  return (out_f32 ? fused == 0 : fused <= 1 && !e.accumulate) && e.res_row_mod == 0 && near(f.C, f.ldc) &&
+         near(e.gelu_out, e.ldgo) && near(e.gelu_in, e.ldgi) && near(e.res, e.ldr);
+}
+
 Fp8Choice pick_fp8(int M, int N, int K, bool out_f32) {
   const int64_t slices = fp8_wide(K) / 64;
   // Thin, by the block's columns and what a wave has to read of A: 1 x 4096 x 1024 2.7 us against
@@ -983,6 +994,10 @@ orbit_status run_typed8(const Fp8Gemm& f, const Fp8Args& a, Fp8Tile t, hipStream
       return run_tile<T, OutT, 128, 128, 2, 1>(f, a, s);
     }
     default:
+      if (!wide_has(f, sizeof(OutT) == 4)) {
+        set_error("fp8 product: no large tiles with this epilogue");
+        return ORBIT_E_UNSUPPORTED;
+      }
       if constexpr (sizeof(OutT) == 2) {
         if (f.epi.gelu_out) return run_wide<bf16, kWideGelu>(f, a, s);
         if (f.epi.gelu_in) return run_wide<bf16, kWideGeluGrad>(f, a, s);
@@ -1001,9 +1016,9 @@ size_t fp8_gemm_workspace_bytes(int M, int N, int K) {
 }
 
 orbit_status fp8_gemm(const Fp8Gemm& f, void* ws, size_t ws_bytes, hipStream_t s) {
-  Fp8Choice c = pick_fp8(f.M, f.N, f.K, f.out_f32 || f.dtype == ORBIT_F32);
-  // the wide kernel's 32 rows of results lie within 31-bit offsets
-  if (c.tile == kWide && f.ldc >= (1 << 24)) c.tile = kTile;
+  const bool out_f32 = f.out_f32 || f.dtype == ORBIT_F32;
+  Fp8Choice c = pick_fp8(f.M, f.N, f.K, out_f32);
+  if (c.tile == kWide && !wide_has(f, out_f32)) c.tile = kTile;
   Fp8Args a{};
   a.A = static_cast<const uint8_t*>(f.A); a.Ae = a.A + fp8_exp_offset(f.M, f.K);
   a.B = static_cast<const uint8_t*>(f.B); a.Be = a.B + fp8_exp_offset(f.N, f.K);

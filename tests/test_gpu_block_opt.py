@@ -277,3 +277,27 @@ def test_block_fp8_of_many_tokens(lib):
     for k in g:
         if k not in ("b_qkv", "qn_g", "qn_b", "kn_g", "kn_b"):  # sums that cancel
             assert float((g[k] - total[k]).norm()) <= 2.0 ** -3 * float(total[k].norm()), k
+
+
+def test_block_fp8_of_many_float32_tokens(lib):
+    """The same samples in float32, where the products of all four layers have more than 512 tiles of 128 x 128 (97 x 8
+    at the least) and those of the parts have not (13 x 32 at the most). The bound is the one above: a float32 sum in
+    another order moves few values to the next code at first (2^-22 / 2^-4 = 2^-18 of them), but a row that holds one
+    is 2^-3 / sqrt(1024) = 2^-8 of its size off, as a bf16 rounding is, and goes on as such a row does."""
+    case = ("f32", 48, 257, 1024, 16, 64, 4096, 1)
+    big = _Block(lib, case, True, None)
+    y, dx, g = big.run()
+    part = _Block(lib, (case[0], 6) + case[2:], True, None)
+    part.P, part.w8, part.opt = big.P, big.w8, big.opt
+    rows = lambda t: t.double().norm(dim=-1)
+    total = {k: torch.zeros_like(v) for k, v in g.items()}
+    for i in range(0, 48, 6):
+        part.gx, part.gdy = big.gx[i:i + 6].contiguous(), big.gdy[i:i + 6].contiguous()
+        py, pdx, pg = part.run()
+        for got, want in ((y[i:i + 6], py), (dx[i:i + 6], pdx)):
+            assert (rows(got.double() - want.double()) <= 2.0 ** -3 * rows(want)).all()
+        for k in total:
+            total[k] += pg[k]
+    for k in g:
+        if k not in ("b_qkv", "qn_g", "qn_b", "kn_g", "kn_b"):  # sums that cancel
+            assert float((g[k] - total[k]).norm()) <= 2.0 ** -3 * float(total[k].norm()), k
