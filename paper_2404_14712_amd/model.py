@@ -75,7 +75,7 @@ def _code(dt: str) -> int:
 class Rope:
     """Rotary positions of the blocks' queries and keys: pair i of a head turns by
     pos[token % len(pos), axis[i]] * freq[i] (see orbit_qk_rope_desc in orbit.h)."""
-    pos: torch.Tensor     # [rows, axes] float32, rows dividing the tokens
+    pos: torch.Tensor     # [rows, axes] float32, rows dividing the tokens; both contiguous, on the pass's device
     freq: torch.Tensor    # [head_dim / 2] float32
     axis: List[int]       # [head_dim / 2]
     near: bool = False    # pairs (2i, 2i + 1) instead of (i, i + head_dim / 2)
@@ -119,10 +119,7 @@ class ViTPass:
         self.bext = BlockExt(int(act8), z.post_norm, z.gate_rows, z.res_scale)
         self.fp8, self.rope, self.opts = fp8, rope, None
         if fp8 or rope is not None:
-            if rope is not None and not (len(rope.axis) == rope.freq.numel() == z.head_dim // 2):
-                raise ValueError(f"rope needs a frequency and an axis for each of {z.head_dim // 2} pairs")
-            r = None if rope is None else BlockRope.of(rope.axis, rope.pos.shape[1], rope.pos.shape[0], rope.pos,
-                                                       rope.freq, rope.near)
+            r = None if rope is None else self._block_rope(rope)
             self.w8 = [{n + t: torch.empty(lib.orbit_fp8_bytes(*(bp[n].shape[::-1] if t else bp[n].shape)),
                                            dtype=torch.uint8, device=self.dev)
                         for n in BLOCK_FP8_WEIGHTS for t in ("", "_t")} if fp8 else None for bp in params["blocks"]]
@@ -171,6 +168,20 @@ class ViTPass:
         self.ws = torch.empty(ws, dtype=torch.uint8, device=self.dev)
 
     # ------------------------------------------------------------------------
+    def _block_rope(self, rope: Rope) -> BlockRope:
+        # the kernels get plain pointers, kept valid here also where the caller's Rope changes
+        here = torch.empty(0, device=self.dev).device
+        for n in ("pos", "freq"):
+            t = getattr(rope, n)
+            if not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.is_contiguous() and t.device == here):
+                raise ValueError(f"rope.{n} must be a contiguous float32 tensor on {here}")
+        if rope.pos.dim() != 2:
+            raise ValueError(f"rope.pos must be [rows, axes], not {tuple(rope.pos.shape)}")
+        if not (len(rope.axis) == rope.freq.numel() == self.z.head_dim // 2):
+            raise ValueError(f"rope needs a frequency and an axis for each of {self.z.head_dim // 2} pairs")
+        self.rope_tensors = (rope.pos, rope.freq)
+        return BlockRope.of(rope.axis, rope.pos.shape[1], rope.pos.shape[0], rope.pos, rope.freq, rope.near)
+
     def pack_weights(self):
         """The blocks' weights into their 8-bit stores, in both orientations."""
         for bp, w8 in zip(self.params["blocks"], self.w8):

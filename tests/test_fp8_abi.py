@@ -222,3 +222,30 @@ def test_rope_reference_by_differences(near):
             a, b = (2 * i, 2 * i + 1) if near else (i, i + 4)
             z = complex(src[tok, 1, a], src[tok, 1, b]) * np.exp(1j * float(pos[tok % 2, axis[i]].double() * freq[i].double()))
             assert abs(z - complex(t[tok, 1, a], t[tok, 1, b])) < 1e-12
+
+
+def test_pass_refuses_positions_the_kernels_cannot_read(lib):
+    """ViTPass hands positions and frequencies on as pointers to packed float32 on its device."""
+    from paper_2404_14712_amd.model import PassDims, Rope, ViTPass
+    z = PassDims(mode="blocks", dtype="f32", B=1, L=6, d=64, blocks=1, heads=2, head_dim=32, mlp=64)
+    E = lambda *s: torch.zeros(*s)
+    block = {"w_qkv": E(64, 192), "b_qkv": E(192), "w_proj": E(64, 64), "b_proj": E(64), "w_fc1": E(64, 64), "b_fc1": E(64),
+             "w_fc2": E(64, 64), "b_fc2": E(64)}
+    block.update({n + s: E(w) for n, w in (("ln1", 64), ("ln2", 64), ("qn", 32), ("kn", 32)) for s in ("_g", "_b")})
+    make = lambda r: ViTPass(lib, z, {"blocks": [block]}, device="cpu", rope=r)
+    pos, freq, axis = torch.rand(6, 2), torch.rand(16), [0] * 8 + [1] * 8
+    p = make(Rope(pos, freq, axis))
+    assert p.opts[0].rope.contents.pos == pos.data_ptr() and p.opts[0].rope.contents.freq == freq.data_ptr()
+    for bad, what in ((Rope(pos.double(), freq, axis), "pos"), (Rope(pos.long(), freq, axis), "pos"),
+                      (Rope(torch.rand(2, 6).t(), freq, axis), "pos"), (Rope(torch.rand(1, 2).expand(6, 2), freq, axis), "pos"),
+                      (Rope(torch.rand(12), freq, axis), "pos"), (Rope(pos.to("meta"), freq, axis), "pos"),
+                      (Rope(pos, freq.double(), axis), "freq"), (Rope(pos, torch.rand(32)[::2], axis), "freq"),
+                      (Rope(pos, freq.to("meta"), axis), "freq"), (Rope(pos.numpy(), freq, axis), "pos")):
+        with pytest.raises(ValueError, match="rope." + what):
+            make(bad)
+    for bad in (Rope(pos, freq, axis[:15]), Rope(pos, freq[:8], axis[:8])):
+        with pytest.raises(ValueError, match="16 pairs"):
+            make(bad)
+    for bad, what in ((Rope(torch.rand(4, 2), freq, axis), "pos_rows"), (Rope(pos, freq, [2] * 16), "axis")):
+        with pytest.raises(ValueError, match=what):
+            make(bad)
