@@ -13,16 +13,21 @@ using namespace orbit;
 namespace {
 
 constexpr int64_t kFp8Codes = 1ll << 34;  // a store's codes stay below
-constexpr int64_t kFp8Tiles = 1ll << 24;  // blocks of 256 threads in a launch of fewer than 2^32
+constexpr int64_t kFp8Tiles = 1ll << 24;  // and its tiles: blocks of 256 threads in a launch of fewer than 2^32
 constexpr int64_t kFp8Side = 1ll << 22;   // K: 256 rows of codes within 31-bit offsets
 
-bool fp8_sizes(int64_t rows, int64_t n) {
-  return rows > 0 && n > 0 && rows < kFp8Codes && n < kFp8Codes && rows <= (kFp8Codes - 1) / fp8_wide(n);
+bool fp8_codes_fit(int64_t rows, int64_t n) {
+  return rows < kFp8Codes && n < kFp8Codes && rows <= (kFp8Codes - 1) / fp8_wide(n);
+}
+bool fp8_tiles_fit(int64_t rows, int64_t n) {  // of sizes whose codes fit
+  return cdiv(rows, 128) * cdiv(n, 128) < kFp8Tiles;
 }
 
 orbit_status fp8_store_check(const char* fn, const char* name, int64_t rows, int64_t n, const void* store, size_t bytes) {
   REQ(rows > 0 && n > 0, ORBIT_E_ARG, "%s: bad sizes %lld x %lld of %s", fn, (long long)rows, (long long)n, name);
-  REQ(fp8_sizes(rows, n), ORBIT_E_UNSUPPORTED, "%s: %s of %lld x %lld values reaches 2^34 codes", fn, name,
+  REQ(fp8_codes_fit(rows, n), ORBIT_E_UNSUPPORTED, "%s: %s of %lld x %lld values reaches 2^34 codes", fn, name,
+      (long long)rows, (long long)n);
+  REQ(fp8_tiles_fit(rows, n), ORBIT_E_UNSUPPORTED, "%s: %s of %lld x %lld values reaches 2^24 tiles", fn, name,
       (long long)rows, (long long)n);
   PTR(store, name);
   REQ(bytes >= fp8_store_bytes(rows, n), ORBIT_E_ARG, "%s: %s of %zu bytes is smaller than the %zu required", fn, name,
@@ -76,7 +81,7 @@ size_t linear_ws(const orbit_fp8_linear_desc& d, void* base, LinearWs* w) {
 extern "C" {
 
 size_t orbit_fp8_bytes(int64_t rows, int64_t n) {
-  if (!fp8_sizes(rows, n)) {
+  if (!(rows > 0 && n > 0 && fp8_codes_fit(rows, n) && fp8_tiles_fit(rows, n))) {
     set_error("orbit_fp8_bytes: bad sizes rows=%lld n=%lld", (long long)rows, (long long)n);
     return 0;
   }
@@ -93,8 +98,6 @@ orbit_status orbit_fp8_pack(int32_t dtype, int64_t rows, int64_t n, int32_t tile
   REQ(store || store_t, ORBIT_E_ARG, "%s: both stores are NULL", fn);
   if (store) ORBIT_TRY(fp8_store_check(fn, "store", rows, n, store, store_bytes));
   if (store_t) ORBIT_TRY(fp8_store_check(fn, "store_t", n, rows, store_t, store_t_bytes));
-  REQ(cdiv(rows, 128) < kFp8Tiles && cdiv(n, 128) < kFp8Tiles && cdiv(rows, 128) * cdiv(n, 128) < kFp8Tiles,
-      ORBIT_E_UNSUPPORTED, "%s: %lld x %lld values reach 2^24 tiles", fn, (long long)rows, (long long)n);
   PTR(x, "x");
   REQ(ldx >= n && ldx % 8 == 0, ORBIT_E_ARG, "%s: ldx must be >= n and a multiple of 8", fn);
   REQ(store != store_t && x != store && x != store_t, ORBIT_E_ARG, "%s: x and the stores must not alias", fn);

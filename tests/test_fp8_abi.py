@@ -249,3 +249,18 @@ def test_pass_refuses_positions_the_kernels_cannot_read(lib):
     for bad, what in ((Rope(torch.rand(4, 2), freq, axis), "pos_rows"), (Rope(pos, freq, [2] * 16), "axis")):
         with pytest.raises(ValueError, match=what):
             make(bad)
+
+
+def test_stores_of_2_24_tiles_are_refused(lib):
+    """The limit of a store that pack can write holds wherever a store is named: its size, and reading it back (rows
+    of 2^33 columns would be a launch of 2^32 threads)."""
+    c = lib.lib
+    for n in (1 << 31, (1 << 33) - 5, 1 << 33, (1 << 34) - 128):
+        assert lib.orbit_fp8_bytes(1, n) == 0 and lib.orbit_fp8_bytes(1, (1 << 31) - 128) > 0
+        assert c.orbit_fp8_unpack(1, 1, n, 0x100, BIG, 0x200, 1 << 34, None) == L.ORBIT_E_UNSUPPORTED
+        assert "2^24 tiles" in lib.last_error()
+        assert c.orbit_fp8_pack(1, 1, n, 1, 0x100, 1 << 34, 0x200, BIG, None, 0, None) == L.ORBIT_E_UNSUPPORTED
+        assert "2^24 tiles" in lib.last_error()
+    # just below both limits: the store is checked, not refused
+    n = (1 << 31) - 128
+    assert c.orbit_fp8_unpack(1, 1, n, 0x100, F.layout(1, n)[3] - 1, 0x200, n, None) == L.ORBIT_E_ARG and "store of" in lib.last_error()
