@@ -264,3 +264,12 @@ def test_stores_of_2_24_tiles_are_refused(lib):
     # just below both limits: the store is checked, not refused
     n = (1 << 31) - 128
     assert c.orbit_fp8_unpack(1, 1, n, 0x100, F.layout(1, n)[3] - 1, 0x200, n, None) == L.ORBIT_E_ARG and "store of" in lib.last_error()
+
+
+def test_grid_rope_written_out():
+    from paper_2404_14712_amd.model import grid_rope
+    r = grid_rope(2, 3, 32, theta=16.0, device="cpu")
+    assert r.pos.tolist() == [[0, 0], [0, 1], [0, 2], [1, 0], [1, 1], [1, 2]] and r.pos.dtype == torch.float32
+    assert r.axis == [0] * 8 + [1] * 8 and not r.near
+    want = [1.0, 2.0 ** -0.5, 0.5, 2.0 ** -1.5, 0.25, 2.0 ** -2.5, 0.125, 2.0 ** -3.5] * 2
+    assert r.freq.dtype == torch.float32 and all(abs(float(f) - w) <= F.U32 * w for f, w in zip(r.freq, want))

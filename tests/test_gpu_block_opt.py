@@ -301,3 +301,131 @@ def test_block_fp8_of_many_float32_tokens(lib):
     for k in g:
         if k not in ("b_qkv", "qn_g", "qn_b", "kn_g", "kn_b"):  # sums that cancel
             assert float((g[k] - total[k]).norm()) <= 2.0 ** -3 * float(total[k].norm()), k
+
+
+def _qk_terms(b, fp8):
+    """What each token and head adds to the gradients of the norms of q and k, float64 [tokens, heads, head_dim]."""
+    dtype, B, L, d, H, dh, mlp, qk = b.case
+    P = {k: v.double() for k, v in b.p.items()}
+    P.update({k: P[k].expand(B * L, H, dh).clone().requires_grad_(True) for k in ("qn_g", "qn_b", "kn_g", "kn_b")})
+    y = F.block_ref(b.x.double(), P, H, True, fp8, b.rope, b.z)
+    y.backward(b.dy.double())
+    return {k: P[k].grad for k in ("qn_g", "qn_b", "kn_g", "kn_b")}
+
+
+@pytest.mark.parametrize("fp8,rope", [(False, "half"), (False, "near"), (True, None), (True, "half")])
+@pytest.mark.parametrize("case", [c for c in CASES if c[7]])
+def test_gradients_of_the_norms_of_q_and_k(lib, case, fp8, rope):
+    """Sums over tokens and heads whose terms nearly cancel, so that they are held to the terms: roundings of terms
+    are independent and add in squares, each of at most the type's bound of its size. 8-bit codes move a term by
+    noise = |reference - exact|, two independent roundings by sqrt(2) of that. The bounds are four and twice those: a
+    sum over 32 columns and more is off by a quarter more than expected at most. A gradient that were missing or of
+    another sign differs by about sqrt(sum of the squares of its terms)."""
+    b = _Block(lib, case, fp8, rope, seed=3)
+    _, _, g = b.run()
+    ref, ex = _qk_terms(b, fp8), _qk_terms(b, False)
+    floor = float(b.ref(fp8=False)[2]["ln1_b"].norm())
+    for k in ref:
+        got = torch.from_numpy(host(g[k]))
+        err = float((got - ref[k].sum((0, 1))).norm())
+        size, noise = float(ex[k].norm()), float((ref[k] - ex[k]).norm())
+        if size <= 1e-9 * floor:  # a softmax of one key
+            assert err <= TOL[case[0]] * floor, (k, err / floor)
+        else:
+            assert err <= 4 * TOL[case[0]] * size + 2 * 2.0 ** 0.5 * noise, (k, err / size, noise / size)
+
+
+@pytest.mark.parametrize("ext", ["plain", "scale", "gate"])
+@pytest.mark.parametrize("case", CASES)
+def test_block_rope_act8(lib, case, ext):
+    """Rotary positions with the saved tensors in 8 bits: the forward as without the stores, bit for bit, and the
+    gradients of the formulas at the stored values (each store passes the gradient straight through). A value whose
+    own rounding differs from the reference's may be stored a step aside: half of max|reference - exact| is allowed
+    for that in float32, three halves in bf16, beside the type's bound."""
+    dtype, B, L, d, H, dh, mlp, qk = case
+    b = _Block(lib, case, False, "half", "plain" if ext == "gate" else ext, seed=4)
+    if ext == "gate":
+        gen = torch.Generator().manual_seed(6)
+        b.z = dict(post_norm=0, gate_rows=1, scale=1.0)
+        for n in ("gate1", "gate2"):
+            b.p[n] = (torch.randn(1, d, generator=gen) * 0.2 + 0.5).to(R.TORCH[dtype])
+            b.P[n] = b.p[n].cuda()
+    b.ext = BlockExt(0, 0, b.z["gate_rows"], b.z["scale"])
+    y0, _, _ = b.run()
+    b.ext = BlockExt(1, 0, b.z["gate_rows"], b.z["scale"])
+    y, dx, g = b.run()
+    assert torch.equal(y, y0)
+
+    def grads(keep):
+        """Autograd of the block whose kept tensors take the values keep() makes of the exact ones."""
+        P = {k: v.double().requires_grad_(True) for k, v in b.p.items()}
+        x = b.x.double().requires_grad_(True)
+        T, A = B * L, H * dh
+        gate = lambda s: P["gate" + s].expand(T, d) if b.z["gate_rows"] else 1.0
+        heads = lambda t: t.reshape(B, L, H, dh).transpose(1, 2).contiguous()
+
+        def chain(kept):
+            # exact with kept None; else each kept tensor is replaced, the gradient going on through the formula
+            c = {}
+
+            def at(n, t):
+                c[n] = t.detach()
+                return t if kept is None else t + (keep(kept[n]) - t).detach()
+
+            xf = x.reshape(T, d)
+            qkv = at("qkv", R.ln_ref(xf, P["ln1_g"], P["ln1_b"], 1e-5) @ P["w_qkv"] + P["b_qkv"])
+            t = qkv[:, :2 * A].reshape(T, 2 * H, dh)
+            if qk:
+                t = torch.cat([R.ln_ref(t[:, :H], P["qn_g"], P["qn_b"], 1e-5), R.ln_ref(t[:, H:], P["kn_g"], P["kn_b"], 1e-5)], 1)
+            t = F.turn(t, *b.rope)
+            q, k, v = heads(t[:, :H]), heads(t[:, H:]), heads(qkv[:, 2 * A:])
+            o = torch.softmax(q @ k.transpose(-1, -2).contiguous() / dh ** 0.5, -1) @ v
+            o = at("o", o.transpose(1, 2).reshape(T, A))
+            x1 = xf + b.z["scale"] * gate("1") * at("f1", o @ P["w_proj"] + P["b_proj"])
+            u = at("u", R.ln_ref(x1, P["ln2_g"], P["ln2_b"], 1e-5) @ P["w_fc1"] + P["b_fc1"])
+            f2 = at("f2", R.gelu_ref(u) @ P["w_fc2"] + P["b_fc2"])
+            return x1 + b.z["scale"] * gate("2") * f2, c
+
+        exact, c = chain(None)
+        chain(c)[0].backward(b.dy.double().reshape(T, d))
+        return exact.detach().reshape(B, L, d), x.grad, {k: torch.zeros_like(v) if v.grad is None else v.grad for k, v in P.items()}
+
+    ry, rdx, rg = grads(R.act8_values)
+    _, edx, eg = grads(lambda t: t)
+    tol, share = TOL[dtype], 0.5 if dtype == "f32" else 1.5
+    check("y", host(y), ry.numpy(), tol)
+    floor = float(rg["ln1_b"].abs().max())
+    for k, got, ref, exact in [("x", dx, rdx, edx)] + [(k, g[k], rg[k], eg[k]) for k in g]:
+        if k in ("qn_g", "qn_b", "kn_g", "kn_b"):
+            continue  # sums that nearly cancel
+        size = max(float(exact.abs().max()), 1e-3 * floor)
+        noise = float((ref - exact).abs().max())
+        err = float((torch.from_numpy(host(got)) - ref).abs().max())
+        assert err <= share * noise + tol * size, (k, err / size, noise / size)
+        assert noise <= 0.1 * size, (k, noise / size)
+    # scratch contents do not matter
+    _, dx2, g2 = b.run(fill=0)
+    assert torch.equal(dx, dx2) and all(torch.equal(g[k], g2[k]) for k in g)
+
+
+def test_pass_with_rope_against_the_reference(lib):
+    """Two blocks of a ViTPass on a grid of 3 x 5 patches, with positions and frequencies written out here."""
+    from paper_2404_14712_amd.model import PassDims, ViTPass, grid_rope
+    rows, cols, d, H, dh = 3, 5, 128, 2, 64
+    case = ("f32", 2, rows * cols, d, H, dh, 256, 1)
+    blocks = [_Block(lib, case, False, None, seed=s) for s in (7, 8)]
+    z = PassDims(mode="blocks", dtype="f32", B=2, L=rows * cols, d=d, blocks=2, heads=H, head_dim=dh, mlp=256)
+    vp = ViTPass(lib, z, {"blocks": [b.P for b in blocks]}, rope=grid_rope(rows, cols, dh, theta=50.0))
+    dx = vp.forward_backward({"x": blocks[0].gx, "dy": blocks[0].gdy})
+    pos = torch.tensor([[float(r), float(c)] for r in range(rows) for c in range(cols)])
+    freq = torch.tensor([50.0 ** (-(i % 16) / 16) for i in range(32)])
+    rope = (pos, freq, [0] * 16 + [1] * 16, False)
+    x = blocks[0].x.double().requires_grad_(True)
+    P = [{k: v.double().requires_grad_(True) for k, v in b.p.items()} for b in blocks]
+    y = F.block_ref(F.block_ref(x, P[0], H, True, False, rope), P[1], H, True, False, rope)
+    y.backward(blocks[0].dy.double())
+    check("y", host(vp.xs[-1]), y.detach().numpy(), TOL["f32"])
+    check("dx", host(dx), x.grad.numpy(), TOL["f32"])
+    for i, p in enumerate(P):
+        for k in p:
+            check(f"d{k}", host(vp.grads["blocks"][i][k]), p[k].grad.numpy(), TOL["f32"], floor_ref=p["ln1_b"].grad.numpy())
