@@ -314,7 +314,7 @@ orbit_status block_linear(const BlockDims& z, const char* tag, const void* x, in
                           const BlockWs& ws, hipStream_t s) {
   if (z.fp8) {
     ORBIT_TRY(fp8_pack(z.dt, x, in, z.T, in, false, ws.q8, xt, true, nullptr, s));
-    Fp8Gemm g; g.dtype = z.dt; g.tag = tag;
+    Fp8Gemm g; g.dtype = z.dt;
     g.A = ws.q8; g.B = w8t; g.C = y; g.ldc = out; g.M = (int)z.T; g.N = out; g.K = in;
     g.epi.bias = bias; g.epi.res = res; g.epi.ldr = out; g.epi.gelu_out = gelu_out; g.epi.ldgo = out;
     return fp8_gemm(g, ws.gws, ws.gws_bytes, s);
@@ -718,15 +718,15 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   };
   // a linear layer's backward in 8 bits: the output gradient is packed in both
   // orientations, and leaves its column sums (the bias gradient) where part is given
-  auto linear8 = [&](const char* tag_dx, const char* tag_dw, const void* g_out, int out, const void* xt, int in,
-                     const void* w8, void* g_in, const void* gelu_in, float* dw, float* part, float* db) -> orbit_status {
+  auto linear8 = [&](const void* g_out, int out, const void* xt, int in, const void* w8, void* g_in, const void* gelu_in,
+                     float* dw, float* part, float* db) -> orbit_status {
     ORBIT_TRY(fp8_pack(dt, g_out, out, T, out, false, w.q8, w.q8t, false, part, s));
     if (part) fin.add(part, out, (int)cdiv(T, 128), out, db);
-    Fp8Gemm g; g.dtype = dt; g.tag = tag_dw;
+    Fp8Gemm g; g.dtype = dt;
     g.A = xt; g.B = w.q8t; g.C = dw; g.ldc = out; g.M = in; g.N = out; g.K = T; g.out_f32 = true;
     g.epi.accumulate = accumulate;
     ORBIT_TRY(fp8_gemm(g, w.gws, w.gws_bytes, s));
-    Fp8Gemm h; h.dtype = dt; h.tag = tag_dx;
+    Fp8Gemm h; h.dtype = dt;
     h.A = w.q8; h.B = w8; h.C = g_in; h.ldc = in; h.M = T; h.N = in; h.K = out;
     h.epi.gelu_in = gelu_in; h.epi.ldgi = in;
     return fp8_gemm(h, w.gws, w.gws_bytes, s);
@@ -743,8 +743,8 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   }
   // feed-forward sub-layer
   if (z.fp8) {
-    ORBIT_TRY(linear8("fc2_dx", "fc2_dw", dff, z.d, sv.gt, z.F, z.w8.w_fc2, w.du, sv.u, gr->w_fc2, w.p_fc2, gr->b_fc2));
-    ORBIT_TRY(linear8("fc1_dx", "fc1_dw", w.du, z.F, sv.h2t, z.d, z.w8.w_fc1, w.dh, nullptr, gr->w_fc1, w.p_fc1, gr->b_fc1));
+    ORBIT_TRY(linear8(dff, z.d, sv.gt, z.F, z.w8.w_fc2, w.du, sv.u, gr->w_fc2, w.p_fc2, gr->b_fc2));
+    ORBIT_TRY(linear8(w.du, z.F, sv.h2t, z.d, z.w8.w_fc1, w.dh, nullptr, gr->w_fc1, w.p_fc1, gr->b_fc1));
   } else {
     bool fused_fc2, fused_fc1;
     {
@@ -805,8 +805,8 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   }
   if (z.fp8) {
     // the LN2 backward has formed the bias gradient in the plain residual
-    ORBIT_TRY(linear8("proj_dx", "proj_dw", df1, z.d, sv.ot, z.A, z.w8.w_proj, w.dO, nullptr, gr->w_proj,
-                      plain_ln2 ? nullptr : w.p_proj, gr->b_proj));
+    ORBIT_TRY(linear8(df1, z.d, sv.ot, z.A, z.w8.w_proj, w.dO, nullptr, gr->w_proj, plain_ln2 ? nullptr : w.p_proj,
+                      gr->b_proj));
   } else {
     {
       Gemm g; g.dtype = dt; g.tag = "proj_dw";
@@ -852,8 +852,7 @@ orbit_status block_backward(const char* fn, const BlockDims& z, BlockExt ext, co
   }
   bool fused_qkv = true;
   if (z.fp8) {
-    ORBIT_TRY(linear8("qkv_dx", "qkv_dw", w.dqkv, 3 * z.A, sv.h1t, z.d, z.w8.w_qkv, w.dh, nullptr, gr->w_qkv, w.p_qkv,
-                      gr->b_qkv));
+    ORBIT_TRY(linear8(w.dqkv, 3 * z.A, sv.h1t, z.d, z.w8.w_qkv, w.dh, nullptr, gr->w_qkv, w.p_qkv, gr->b_qkv));
   } else {
     {
       Gemm g; g.dtype = dt; g.tag = "qkv_dw";

@@ -175,7 +175,7 @@ orbit_status orbit_fp8_linear_fwd(const orbit_fp8_linear_desc* desc, const void*
   const orbit_dtype dt = (orbit_dtype)d.dtype;
   ORBIT_TRY(fp8_pack(dt, x, ldx, d.rows, d.in, false, w.q, saved, true, nullptr, s));
   Fp8Gemm g;
-  g.dtype = dt; g.tag = "linear";
+  g.dtype = dt;
   g.A = w.q; g.B = w_t; g.C = y; g.ldc = ldy; g.M = d.rows; g.N = d.out; g.K = d.in; g.epi.bias = bias;
   return fp8_gemm(g, w.gws, w.gws_bytes, s);
 }
@@ -201,12 +201,12 @@ orbit_status orbit_fp8_linear_bwd(const orbit_fp8_linear_desc* desc, const void*
   ORBIT_TRY(fp8_pack(dt, dy, lddy, d.rows, d.out, false, dx ? t.q : nullptr, t.qt, false, db ? t.part : nullptr, s));
   if (dx) {
     Fp8Gemm g;
-    g.dtype = dt; g.tag = "linear_dx";
+    g.dtype = dt;
     g.A = t.q; g.B = w; g.C = dx; g.ldc = lddx; g.M = d.rows; g.N = d.in; g.K = d.out;
     ORBIT_TRY(fp8_gemm(g, t.gws, t.gws_bytes, s));
   }
   Fp8Gemm g;
-  g.dtype = dt; g.tag = "linear_dw";
+  g.dtype = dt;
   g.A = saved; g.B = t.qt; g.C = dw; g.ldc = d.out; g.M = d.in; g.N = d.out; g.K = d.rows;
   g.out_f32 = true; g.epi.accumulate = accumulate;
   ORBIT_TRY(fp8_gemm(g, t.gws, t.gws_bytes, s));

@@ -1,12 +1,13 @@
 // Tiles of the kernels that copy their operands HBM -> LDS through the buffer
-// unit: K slices of 64 bytes a row in an LDS ring, their copy plans, fragment
-// reads and tile configurations (bf16 and 8-bit products).
+// unit: buffer descriptors and the wait for a ring's stage (bf16 and 8-bit products),
+// and the bf16 products' K slices of 64 bytes a row, their copy plans, fragment reads
+// and tile configurations.
 #pragma once
 #include "tile.h"
 
 namespace orbit {
 
-constexpr int DBK = 32;  // bf16 values of a slice's row (64 8-bit ones)
+constexpr int DBK = 32;  // values of a slice's row
 constexpr unsigned kOobOffset = 0x80000000u;    // beyond num_records: the copy reads zeros
 
 #define ORBIT_LDS __attribute__((address_space(3)))

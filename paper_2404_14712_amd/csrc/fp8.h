@@ -90,7 +90,6 @@ struct Fp8Gemm {
   orbit_dtype dtype = ORBIT_BF16;
   bool out_f32 = false;
   Epi epi{};
-  const char* tag = "gemm";
 };
 size_t fp8_gemm_workspace_bytes(int M, int N, int K);
 orbit_status fp8_gemm(const Fp8Gemm& g, void* ws, size_t ws_bytes, hipStream_t s);
