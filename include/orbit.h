@@ -478,7 +478,11 @@ orbit_status orbit_fp8_unpack(int32_t dtype, int64_t rows, int64_t n, const void
 
 /* C[M, N] = A B^T (+ bias[n]) (+ C if accumulate) over the stores of A[M, K] and
  * B[N, K], float32 accumulation. C is float32 if c_f32 or dtype is ORBIT_F32, else
- * bf16 (accumulate needs float32); bias is dtype [N] or NULL. N and ldc >= N are
+ * bf16 (accumulate needs float32); bias is dtype [N] or NULL. For bf16 results the 8-bit
+ * matrix instruction adds 64 or 128 products at a time, and loses of these what lies 2^-14
+ * below the largest: 1e-5 to 4e-5 of the results in the 2-norm, a hundredth of their own
+ * rounding, but more than that of a result that nearly cancels. Float32 results keep every
+ * product to the last bits of a float32 sum. N and ldc >= N are
  * multiples of 8, M and K any; K below 2^22. For y = x W take the store of x and the
  * transposed one of W; for dx = dy W^T the stores of dy and of W; for dw = x^T dy the
  * transposed stores of both. Sums are formed in an order that depends on the

@@ -8,7 +8,8 @@
 // of one step to the largest of them and drops what lies more than 13 bits below
 // (measured: 2^-14 of the largest is lost, where bf16 products keep 2^-23). Sums come
 // out 1e-5 to 4e-5 off in the 2-norm, a hundredth of a bf16 result's own rounding, so
-// bf16 results take it. Float32 results are formed with EXACT instead: the codes are
+// bf16 results take it: at 4096 x 4096 x 8192 2.3% of them are another bf16 value than a
+// float32 sum gives, and the distance to the exact sums is 1.6594e-3 against 1.6591e-3. Float32 results are formed with EXACT instead: the codes are
 // turned into bf16 with their scales in the fragments, which is exact, and the bf16
 // instructions keep every bit a float32 sum can, at half the rate.
 //
@@ -373,15 +374,15 @@ __global__ void __launch_bounds__(KG * 256, KG == 1 && NS == 2 ? 2 : 1) gemm_fp8
 // have to do without a spill: one would wait for every copy and store in flight (22
 // spilled registers: 4 to 14 us a round of tiles).
 //
-// Measured: 8192 x 8192 x 8192 415 us (2650 TFLOP/s; two groups of 4 waves of 128 x 64 that
-// take turns at reading and multiplying 456), 4096 x 4096 x 8192 104 (121), 4096 x 8192 x 4096
+// Measured: 8192 x 8192 x 8192 405 to 415 us by the card (2650 to 2715 TFLOP/s; two groups of 4
+// waves of 128 x 64 that take turns at reading and multiplying 456), 4096 x 4096 x 8192 104 (121), 4096 x 8192 x 4096
 // 109 (123), 8192 x 8192 x 1024 75 (92). A stage takes 1.49 us, 2880 TFLOP/s, near what the
 // matrix cores reach on random codes at the card's power limit (3200); a round of tiles costs
 // 9 to 18 us beside its stages, of which 7 are 32 MB of results at the memory's rate: there
 // is no room in LDS or registers to let the next tile's sums begin before these are out.
 //
 // Float32 results take four bf16 instructions of 32 cycles for one of 64, and a wave has
-// time to decode between them: 8192 x 8192 x 8192 775 us (1420 TFLOP/s), 4096 x 4096 x 8192
+// time to decode between them: 8192 x 8192 x 8192 748 to 775 us (1420 to 1470 TFLOP/s), 4096 x 4096 x 8192
 // 200, 8192 x 8192 x 2048 227, 8192 x 4096 x 4096 202 (two groups of 4 waves, one decoding and
 // multiplying while the other reads: 810, 212, 272, 229; a bf16 library product of the first
 // 859), and 8192 x 8192 x 1024 142 (tiles of 128 x 128: 168).
@@ -898,7 +899,8 @@ struct Fp8Choice { Fp8Tile tile; int splits; };
 
 // What the wide kernel's end has: of GELU with its input kept, GELU' and the residual one,
 // with bf16 results, or onto what is there with float32 ones; 32 rows within 31-bit offsets.
-// The other kernels end in epi_apply, which has everything.
+// The other kernels end in epi_apply, which has everything: a float32 block's layers that
+// need it stay on tiles of 128 x 128 (8192 x 8192 x 1024 168 us there, 142 on the wide ones).
 bool wide_has(const Fp8Gemm& f, bool out_f32) {
   const Epi& e = f.epi;
   const int fused = (e.gelu_out ? 1 : 0) + (e.gelu_in ? 1 : 0) + (e.res ? 1 : 0);
